@@ -109,6 +109,116 @@ size_t ham_op_attention_step_noalloc_max_bytes(void);
  * a macro-step over `rows` sequences use for this slot bound; 0 if invalid. */
 int ham_op_attention_step_splits(int32_t dtype, int32_t rows, int32_t n_kv_heads, int32_t head_dim, int32_t kv_cap);
 
+/* ---------------------------------------------------------------- KV cache in 8 bits
+ * One layer's K and V of `rows` sequences in e4m3 codes with a scale for each
+ * block of 32 slots and kv head (half the bytes of a bf16 cache), its writers
+ * and the attention of one query row per sequence over it, over every block or
+ * over the blocks that ham_op_kv8_select chooses.
+ *
+ * A closed block (32 slots of a kv head) holds K and V apart as
+ *   a = max |x| over its 32 x head_dim values, each first rounded to the storage
+ *   type; scale = a / 448; code = e4m3(x * (1 / scale)), nearest even, at most 448;
+ *   a value stands for code * scale.
+ * All codes are 0 where the scale is below the least normal fp32 value.  A block
+ * with an infinity or NaN has scale NaN: every row that reads it becomes NaN.
+ * The slots past the last full block (kv_len % 32) are in the open block, in the
+ * storage type.  A block is coded once, when its 32nd slot arrives, so the cache
+ * is the same, bit for bit, whether its slots came one by one or together.  A
+ * row may be shortened by slots of its open block, or to a multiple of 32.
+ *
+ * The cache is one caller-owned buffer of ham_op_kv8_cache_bytes bytes, 256-byte
+ * aligned; it needs no clearing.  Regions (ham_op_kv8_info), pair = row *
+ * n_kv_heads + kv head, NB = slots_cap / 32 blocks each:
+ *   codes  [pair][NB][2][32*head_dim]: K, then V; (slot s, channel d) at
+ *     K ((s/4%2*(head_dim/64) + d/64)*64 + d/16%4*16 + s/8*4 + s%4)*16 + d%16
+ *     V ((d/32*4 + s/8)*16 + d%16)*16 + d/16%2*8 + s%8
+ *   scales fp32 [pair][NB][2]: K, V
+ *   bounds [pair][NB][head_dim/8][2][8]: least and greatest K code of each
+ *     channel (for 8 channels: 8 least, then 8 greatest)
+ *   open   [pair][2][32][head_dim], storage type: K, V
+ *
+ * Rows and lengths: a length outside 0..kv_max (append: start and count that do
+ * not fit n_tokens or slots_cap) makes the row one without slots and ORs 8 into
+ * d_err[r] (int32 [rows], in/out, bits are only set).  d_enable[r] = 0: the row
+ * is one without slots.  Other streams or host threads may read one cache at
+ * the same time, with workspaces and outputs of their own; a call that writes
+ * it is ordered against them by the caller.  Nothing is allocated and no call
+ * waits for the GPU: all of them can be captured into a graph. */
+#define HAM_KV8_BLOCK 32
+
+typedef struct ham_kv8_shape {
+  int32_t dtype;      /* storage type of the open block and of activations: HAM_F32 or HAM_BF16 */
+  int32_t rows;       /* sequences, 1..4096 */
+  int32_t n_heads, n_kv_heads;  /* n_heads <= 1024, a multiple (1..16) of n_kv_heads */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t slots_cap;  /* slots of a row, a multiple of 32, at most 2^24 */
+} ham_kv8_shape;
+
+/* Bytes of the cache, and of the workspace that any ham_op_kv8_select or
+ * ham_op_kv8_attention of this shape needs; 0 for an invalid shape. */
+size_t ham_op_kv8_cache_bytes(const ham_kv8_shape* shape);
+size_t ham_op_kv8_workspace_bytes(const ham_kv8_shape* shape);
+/* Byte offsets of the regions in the cache buffer. */
+int ham_op_kv8_info(const ham_kv8_shape* shape, size_t* codes, size_t* scales, size_t* bounds, size_t* open);
+
+/* RoPE and append: count[r] new slots of row r after the start[r] it holds.
+ *  d_qkv         fp32 [rows][n_tokens][(n_heads + 2*n_kv_heads)*head_dim]: all q
+ *                heads, then k, then v, before RoPE (as ham_op_attention_step)
+ *  d_cos, d_sin  fp32 [rows][n_tokens][head_dim/2]; rotate-half RoPE, each
+ *                product and each sum rounded to fp32
+ *  d_start, d_count  int32 [rows]; 0 <= count <= n_tokens, start + count <= slots_cap
+ *  d_q           act rows [rows][n_tokens][n_heads*head_dim]: the rotated q of
+ *                the new slots (the rest is left as it is), or NULL
+ * Codes, scales and bounds of the blocks that fill up, and the open block's new
+ * slots, are written, nothing else.  HAM_EINVAL on a bad shape, null or
+ * misaligned (16 bytes) pointer or n_tokens outside 1..2^24, HAM_ENOMEM if
+ * the cache buffer is too small. */
+int ham_op_kv8_append(const ham_kv8_shape* shape, int32_t n_tokens, const float* d_qkv, const float* d_cos,
+                      const float* d_sin, const int32_t* d_start, const int32_t* d_count, void* d_cache,
+                      size_t cache_bytes, void* d_q, int32_t* d_err, void* hip_stream);
+
+/* A filled cache of the storage type (as a prefill leaves a layer's in the state
+ * buffer, ham_state_info) into the 8-bit cache: slots [0, kv_len[r]) of each row.
+ *  d_k, d_vt  as for ham_op_decode_attention, of src_slots slots a row
+ *  kv_max     host upper bound of kv_len, at most slots_cap and src_slots */
+int ham_op_kv8_pack(const ham_kv8_shape* shape, const void* d_k, const void* d_vt, int32_t src_slots,
+                    const int32_t* d_kv_len, int32_t kv_max, void* d_cache, size_t cache_bytes, int32_t* d_err,
+                    void* hip_stream);
+
+/* For one query row per sequence: the n_blocks closed blocks of each kv head
+ * whose keys may score highest (all of them where a row has no more).  A block's
+ * score is the greatest over the kv head's q-heads of
+ *   scale_K * sum_d max(q_d least_d, q_d greatest_d),
+ * an upper bound of q . k over its keys, summed in fp64 and rounded to fp32:
+ * no key of a block that is left out scores above the least score chosen.
+ * Equal scores: the lower block first; NaN counts as greatest.  The first
+ * keep_first and the last keep_last closed blocks are always chosen.
+ *  d_q         act rows [rows][n_heads*head_dim], RoPE applied
+ *  kv_max      host upper bound of kv_len
+ *  d_blocks    int32 [rows][n_kv_heads][n_blocks], ascending, then -1
+ *  d_n_blocks  int32 [rows][n_kv_heads]
+ * n_blocks in 1..slots_cap/32, keep_first + keep_last <= n_blocks. */
+int ham_op_kv8_select(const ham_kv8_shape* shape, const void* d_q, const void* d_cache, size_t cache_bytes,
+                      const int32_t* d_kv_len, const int32_t* d_enable, int32_t kv_max, int32_t n_blocks,
+                      int32_t keep_first, int32_t keep_last, int32_t* d_blocks, int32_t* d_n_blocks, int32_t* d_err,
+                      void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* GQA attention of one query row per sequence:
+ *   out[r, h] = softmax_j(q[r, h] . K[r, h/(H/Hkv), j] / sqrt(hd)) V[...]
+ * over the slots j < kv_len[r] of every closed block, or with d_blocks of the
+ * listed ones, and of the open block.  A row without slots gets zeros.
+ *  d_blocks, d_n_blocks  lists as ham_op_kv8_select writes them, max_blocks
+ *              entries apart, or both NULL: an entry that is not above the one
+ *              before it or not a closed block of the row is left out, a count
+ *              outside 0..max_blocks counts as 0; both OR 16 into d_err[r]
+ *  kv_max      host upper bound of kv_len (with rows, n_kv_heads and max_blocks
+ *              it chooses the split of the blocks over workgroups)
+ *  d_q, d_out  act rows [rows][n_heads*head_dim] */
+int ham_op_kv8_attention(const ham_kv8_shape* shape, const void* d_q, const void* d_cache, size_t cache_bytes,
+                         const int32_t* d_kv_len, const int32_t* d_enable, int32_t kv_max, const int32_t* d_blocks,
+                         const int32_t* d_n_blocks, int32_t max_blocks, void* d_out, int32_t* d_err,
+                         void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,21 +16,20 @@
 #include <vector>
 
 #include "ham_internal.h"
+#include "host_common.h"
 #include "kernels_misc.h"
 #include "launch_rules.h"
 
 using namespace ham;
 
 namespace ham {
+
 LaunchTiming& launch_timing() {
   static thread_local LaunchTiming t;
   return t;
 }
-}  // namespace ham
 
-namespace {
-
-thread_local std::string g_err;
+static thread_local std::string g_err;
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -42,13 +41,10 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-#define HIP_TRY(call)                                                                       \
-  do {                                                                                      \
-    hipError_t e_ = (call);                                                                 \
-    if (e_ != hipSuccess) return fail(HAM_EHIP, "%s: %s", #call, hipGetErrorString(e_));    \
-  } while (0)
+}  // namespace ham
 
-size_t al(size_t x) { return (x + 255) & ~size_t(255); }
+namespace {
+
 int rup(int x, int m) { return (x + m - 1) / m * m; }
 
 uint64_t sm64(uint64_t s, uint64_t i) {
@@ -767,7 +763,7 @@ size_t attn_part_bytes(int R, int H, int Hk, int hd) {
 // ============================================================================ C ABI
 extern "C" {
 
-const char* ham_last_error(void) { return g_err.c_str(); }
+const char* ham_last_error(void) { return ham::g_err.c_str(); }
 
 size_t ham_weights_bytes(const ham_config* c) { return check_cfg(c) ? 0 : make_layout(c).w_bytes; }
 size_t ham_state_bytes(const ham_config* c) { return check_cfg(c) ? 0 : make_layout(c).st_bytes; }

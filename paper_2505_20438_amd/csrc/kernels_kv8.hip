@@ -1,0 +1,820 @@
+// Operators on a KV cache in 8 bits (layout: kernels_kv8.h).
+//
+// A closed block of 32 slots of a kv head is held as e4m3 codes with one fp32 scale for K and one for V:
+//   a = max |x| over the block's 32 x hd values (rounded to the storage type first), scale = a / 448,
+//   code = e4m3(clamp(x / scale)), nearest even, as x * (1 / scale);
+// a scale below the least normal fp32 value makes every code 0, and a block with an infinity or NaN has scale NaN, so
+// that every row that reads it becomes NaN.  The slots past the last full block are in the open block, in the storage
+// type; a block is coded once, when its 32nd slot arrives, so the cache does not depend on how its tokens arrived.
+//
+// k_kv8_append   RoPE of projection rows, K and V into the cache, q out.
+// k_kv8_pack     a filled cache of the storage type into the 8-bit cache.
+// k_kv8_scores, k_kv8_pick   the blocks whose keys' upper bounds are greatest.
+// k_kv8_attn, k_kv8_combine  attention of one query row per sequence over all or listed blocks and the open one.
+#include <algorithm>
+
+#include "device_common.h"
+#include "kernels_kv8.h"
+#include "launch_rules.h"
+
+namespace ham {
+
+namespace {
+
+// ---------------------------------------------------------------- values and codes
+// four values of the storage type as fp32
+template <typename T> __device__ __forceinline__ f4 ld4(const T* p);
+template <> __device__ __forceinline__ f4 ld4<float>(const float* p) { return *reinterpret_cast<const f4*>(p); }
+template <> __device__ __forceinline__ f4 ld4<bf16>(const bf16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return f4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+            __uint_as_float(u.y & 0xFFFF0000u)};
+}
+template <typename T> __device__ __forceinline__ void st4(T* p, f4 v);
+template <> __device__ __forceinline__ void st4<float>(float* p, f4 v) { *reinterpret_cast<f4*>(p) = v; }
+template <> __device__ __forceinline__ void st4<bf16>(bf16* p, f4 v) {
+  *reinterpret_cast<uint2*>(p) = uint2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+}
+template <typename T> __device__ __forceinline__ f4 stored4(f4 v) {  // rounded to the storage type
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = to_f<T>(from_f<T>(v[e]));
+  return v;
+}
+// four values of an activation row of width W
+template <typename T> __device__ __forceinline__ void put_act4(void* base, size_t row, int W, int i, f4 v) {
+  if constexpr (Act<T>::SPLIT) {
+    T* p = (T*)base + row * 2 * W + i;
+    const f4 hi = stored4<T>(v);
+    st4<T>(p, hi);
+    st4<T>(p + W, v - hi);
+  } else {
+    st4<T>((T*)base + row * W + i, v);
+  }
+}
+template <typename T> __device__ __forceinline__ f4 get_act4(const void* base, size_t row, int W, int i) {
+  const T* p = (const T*)base + row * Act<T>::PL * W + i;
+  f4 v = ld4<T>(p);
+  if constexpr (Act<T>::SPLIT) v += ld4<T>(p + W);
+  return v;
+}
+
+// Rotate-half RoPE of the pair (x, y): products and sums are rounded one by one (no fused multiply-add), so that what is
+// rounded to 8 bits next does not depend on how the compiler contracts.
+__device__ __forceinline__ void rotate(f4& x, f4& y, f4 c, f4 s) {
+#pragma clang fp contract(off)
+  const f4 xc = x * c, ys = y * s, yc = y * c, xs = x * s;
+  x = xc - ys;
+  y = yc + xs;
+}
+
+// Scale of a block from the bits of its greatest magnitude, and what its values are multiplied by.
+__device__ __forceinline__ void block_scale(uint32_t top, float& scale, float& inv) {
+  scale = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top) / KV8_MAX;
+  inv = scale >= 1.17549435e-38f ? 1.0f / scale : 0.0f;
+}
+__device__ __forceinline__ float to_range(float x, float inv) { return fminf(fmaxf(x * inv, -KV8_MAX), KV8_MAX); }
+__device__ __forceinline__ uint32_t code4(const float* x, float inv) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_range(x[0], inv), to_range(x[1], inv), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_range(x[2], inv), to_range(x[3], inv), w, true);
+}
+__device__ __forceinline__ uint32_t top4(uint32_t top, f4 v) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  return top;
+}
+
+// A full block in LDS (fp32 values of the storage type), coded and written.
+constexpr int CODE_THREADS = 256;
+template <int HD>
+struct BlockLds {
+  float k[KV8_BLOCK][HD + 4], v[KV8_BLOCK][HD + 4];
+  uint32_t top[2][CODE_THREADS / 64];
+};
+
+// `tk`, `tv`: bits of the greatest magnitude of K and V that this thread wrote.  Every thread of the workgroup calls it.
+template <int HD>
+__device__ __forceinline__ void code_block(BlockLds<HD>& sh, uint32_t tk, uint32_t tv, const Kv8Cache& c, size_t blk) {
+  const int tid = threadIdx.x, lane = tid & 63;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    tk = max(tk, (uint32_t)__shfl_xor((int)tk, o, WAVE));
+    tv = max(tv, (uint32_t)__shfl_xor((int)tv, o, WAVE));
+  }
+  if (lane == 0) {
+    sh.top[0][tid >> 6] = tk;
+    sh.top[1][tid >> 6] = tv;
+  }
+  __syncthreads();
+  float ks, ki, vs, vi;
+  block_scale(max(max(sh.top[0][0], sh.top[0][1]), max(sh.top[0][2], sh.top[0][3])), ks, ki);
+  block_scale(max(max(sh.top[1][0], sh.top[1][1]), max(sh.top[1][2], sh.top[1][3])), vs, vi);
+  if (tid == 0) {
+    c.scales[2 * blk] = ks;
+    c.scales[2 * blk + 1] = vs;
+  }
+  uint8_t* out = c.codes + blk * (2 * KV8_BLOCK * HD);
+  constexpr int CHUNKS = KV8_BLOCK * HD / 16;
+  for (int q = tid; q < CHUNKS; q += CODE_THREADS) {
+    const int r = q % 16, g = q / 16 % 4, p = q / 64;
+    {  // K: piece (t, i)
+      const int t = p / (HD / 64), i = p % (HD / 64);
+      const float* x = &sh.k[8 * (r / 4) + 4 * t + r % 4][64 * i + 16 * g];
+      u4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = code4(x + 4 * e, ki);
+      *reinterpret_cast<u4*>(out + q * 16) = w;
+    }
+    {  // V: piece p
+      u4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) x[f] = sh.v[8 * g + (4 * e + f) % 8][32 * p + 16 * (e / 2) + r];
+        w[e] = code4(x, vi);
+      }
+      *reinterpret_cast<u4*>(out + KV8_BLOCK * HD + q * 16) = w;
+    }
+  }
+  // coding keeps the order, so the least code is that of the least value
+  if (tid < HD) {
+    float lo = sh.k[0][tid], hi = lo;
+#pragma unroll
+    for (int s = 1; s < KV8_BLOCK; ++s) {
+      lo = fminf(lo, sh.k[s][tid]);
+      hi = fmaxf(hi, sh.k[s][tid]);
+    }
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_range(lo, ki), to_range(hi, ki), 0, false);
+    uint8_t* b = c.bounds + blk * (2 * HD) + tid / 8 * 16 + tid % 8;
+    b[0] = (uint8_t)w;
+    b[8] = (uint8_t)(w >> 8);
+  }
+}
+
+// ---------------------------------------------------------------- append
+// Workgroups x < nb of a (row, kv head): block `first + x` of the row if the new tokens fill it; workgroup 0 also puts the
+// tokens past the last full block into the open one, after it has read what the open block held (so no other workgroup
+// touches it).  The others: q of APPEND_QT tokens each.
+constexpr int APPEND_QT = 32;
+template <typename T, int HD>
+__global__ __launch_bounds__(CODE_THREADS) void k_kv8_append(Kv8AppendArgs a, int nb) {
+  constexpr int B = KV8_BLOCK, HALF = HD / 2, QPS = HALF / 4;  // quads of pairs per head
+  __shared__ BlockLds<HD> sh;
+  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk;
+  const int n0 = a.start[r], cnt = a.count[r];
+  if (n0 < 0 || cnt < 0 || cnt > a.T || (long long)n0 + cnt > a.slots) {
+    if (blockIdx.x == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+    return;
+  }
+  const int ld = (a.H + 2 * a.Hk) * HD;
+  const float* src = a.qkv + (size_t)r * a.T * ld;
+  const float* cs = a.cos + (size_t)r * a.T * HALF;
+  const float* sn = a.sin + (size_t)r * a.T * HALF;
+  if ((int)blockIdx.x >= nb) {  // q
+    const int t0 = ((int)blockIdx.x - nb) * APPEND_QT, t1 = min(cnt, t0 + APPEND_QT), per = grp * QPS;
+    for (int q = tid; q < (t1 - t0) * per; q += CODE_THREADS) {
+      const int t = t0 + q / per, j = q % per / QPS, i = q % QPS * 4, h = kvh * grp + j;
+      const float* p = src + (size_t)t * ld + h * HD + i;
+      f4 x = *reinterpret_cast<const f4*>(p), y = *reinterpret_cast<const f4*>(p + HALF);
+      rotate(x, y, *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + i), *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + i));
+      const size_t row = (size_t)r * a.T + t;
+      put_act4<T>(a.q, row, a.H * HD, h * HD + i, x);
+      put_act4<T>(a.q, row, a.H * HD, h * HD + i + HALF, y);
+    }
+    return;
+  }
+  const int x0 = blockIdx.x, end = n0 + cnt, first = n0 / B, last = end / B;
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  T* open = (T*)a.c.open + pair * 2 * B * HD;  // K, then V
+  const float* ksrc = src + (size_t)(a.H + kvh) * HD;
+  const float* vsrc = ksrc + (size_t)a.Hk * HD;
+  const auto key = [&](int t, int i, f4& x, f4& y) {
+    const float* p = ksrc + (size_t)t * ld + i;
+    x = *reinterpret_cast<const f4*>(p);
+    y = *reinterpret_cast<const f4*>(p + HALF);
+    rotate(x, y, *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + i), *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + i));
+  };
+  if (x0 < last - first) {
+    const int base = (first + x0) * B;
+    uint32_t tk = 0, tv = 0;
+    for (int q = tid; q < B * QPS; q += CODE_THREADS) {
+      const int w = q / QPS, i = q % QPS * 4, t = base + w - n0;
+      f4 x, y;
+      if (t < 0) {
+        x = ld4<T>(open + w * HD + i);
+        y = ld4<T>(open + w * HD + i + HALF);
+      } else {
+        key(t, i, x, y);
+        x = stored4<T>(x);
+        y = stored4<T>(y);
+      }
+      tk = top4(top4(tk, x), y);
+      *reinterpret_cast<f4*>(&sh.k[w][i]) = x;
+      *reinterpret_cast<f4*>(&sh.k[w][i + HALF]) = y;
+    }
+    for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
+      const int w = q / (HD / 4), i = q % (HD / 4) * 4, t = base + w - n0;
+      const f4 x = t < 0 ? ld4<T>(open + (B + w) * HD + i) : stored4<T>(*reinterpret_cast<const f4*>(vsrc + (size_t)t * ld + i));
+      tv = top4(tv, x);
+      *reinterpret_cast<f4*>(&sh.v[w][i]) = x;
+    }
+    code_block<HD>(sh, tk, tv, a.c, pair * a.c.NB + first + x0);
+  }
+  if (x0 == 0) {  // slots of the open block: tokens t of slots max(n0, 32 last) .. end
+    const int s0 = max(n0, last * B), ns = end - s0;
+    for (int q = tid; q < ns * QPS; q += CODE_THREADS) {
+      const int s = s0 + q / QPS, i = q % QPS * 4, w = s - last * B;
+      f4 x, y;
+      key(s - n0, i, x, y);
+      st4<T>(open + w * HD + i, x);
+      st4<T>(open + w * HD + i + HALF, y);
+    }
+    for (int q = tid; q < ns * (HD / 4); q += CODE_THREADS) {
+      const int s = s0 + q / (HD / 4), i = q % (HD / 4) * 4, w = s - last * B;
+      st4<T>(open + (B + w) * HD + i, *reinterpret_cast<const f4*>(vsrc + (size_t)(s - n0) * ld + i));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- pack
+// One workgroup per (block, kv head, row): a full block is coded, the slots past the last full block go to the open one.
+template <typename T, int HD>
+__global__ __launch_bounds__(CODE_THREADS) void k_kv8_pack(Kv8PackArgs a) {
+  constexpr int B = KV8_BLOCK;
+  __shared__ BlockLds<HD> sh;
+  const int tid = threadIdx.x, b = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, n = a.kv_len[r];
+  if (n < 0 || n > a.kv_max) {
+    if (b == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+    return;
+  }
+  const int closed = n / B, ns = min(B, n - b * B);
+  if (ns <= 0) return;
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  const T* K = (const T*)a.K + (pair * a.S + (size_t)b * B) * HD;
+  const T* VT = (const T*)a.VT + (pair * a.S + (size_t)b * B) * HD;  // [hd][32]
+  uint32_t tk = 0, tv = 0;
+  if (b == closed) {  // the open block
+    T* open = (T*)a.c.open + pair * 2 * B * HD;
+    for (int q = tid; q < ns * (HD / 4); q += CODE_THREADS) st4<T>(open + q * 4, ld4<T>(K + q * 4));
+    for (int q = tid; q < ns * HD; q += CODE_THREADS) open[B * HD + q] = VT[q % HD * B + q / HD];
+    return;
+  }
+  for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
+    const f4 x = ld4<T>(K + q * 4);
+    tk = top4(tk, x);
+    *reinterpret_cast<f4*>(&sh.k[q / (HD / 4)][q % (HD / 4) * 4]) = x;
+  }
+  for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
+    const int d = q / (B / 4), s = q % (B / 4) * 4;
+    const f4 x = ld4<T>(VT + q * 4);
+    tv = top4(tv, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sh.v[s + e][d] = x[e];
+  }
+  code_block<HD>(sh, tk, tv, a.c, pair * a.c.NB + b);
+}
+
+// ---------------------------------------------------------------- select
+// Upper bound of q . k over the keys of a block, in each channel by the greater of q lo and q hi:
+//   sum_d max(q_d lo_d, q_d hi_d) = sum_d (q_d (lo_d + hi_d) + |q_d| (hi_d - lo_d)) / 2,
+// the greatest over the kv head's q-heads, times the block's scale.  Products of q (24 bits) and codes (4 bits) and their
+// sums are taken in fp64: blocks are compared by these values, and fp32 sums of another order would order near ones
+// differently.  HD / 8 lanes to a block, 8 channels each.
+constexpr int SCORE_THREADS = 256, SCORE_BLOCKS = 64;  // blocks of a workgroup
+template <typename T, int HD>
+__global__ __launch_bounds__(SCORE_THREADS) void k_kv8_scores(Kv8SelectArgs a, int nb_max) {
+  constexpr int LPB = HD / 8, BPP = SCORE_THREADS / LPB;  // lanes of a block, blocks of a pass
+  __shared__ double sq[KV8_MAX_GROUP][HD];
+  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk, n = a.kv_len[r];
+  const int b0 = blockIdx.x * SCORE_BLOCKS;
+  if (n < 0 || n > a.kv_max || !a.enable[r]) return;
+  const int closed = n / KV8_BLOCK;
+  if (closed <= a.n || b0 >= closed) return;  // every block is taken
+  for (int i = tid * 4; i < grp * HD; i += SCORE_THREADS * 4) {
+    const f4 x = get_act4<T>(a.q, r, a.H * HD, kvh * grp * HD + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sq[i / HD][i % HD + e] = (double)x[e];
+  }
+  __syncthreads();
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  const int c = tid % LPB;
+  for (int b = b0 + tid / LPB; b < min(closed, b0 + SCORE_BLOCKS); b += BPP) {
+    const size_t blk = pair * a.c.NB + b;
+    const u4 w = ld16(a.c.bounds + blk * (2 * HD) + c * 16);
+    double sum[8], dif[8];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const auto lo = p % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[p / 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[p / 2], false);
+      const auto hi = p % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[2 + p / 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[2 + p / 2], false);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        sum[2 * p + e] = (double)lo[e] + (double)hi[e];
+        dif[2 * p + e] = (double)hi[e] - (double)lo[e];
+      }
+    }
+    double best = -INFINITY;
+    for (int j = 0; j < grp; ++j) {
+      double s = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double q = sq[j][c * 8 + e];
+        s = fma(q, sum[e], s);
+        s = fma(fabs(q), dif[e], s);
+      }
+#pragma unroll
+      for (int o = 1; o < LPB; o <<= 1) s += __shfl_xor(s, o, WAVE);
+      best = (s > best || s != s) ? s : best;  // NaN stays
+    }
+    if (c == 0) a.scores[pair * nb_max + b] = (float)(0.5 * best * (double)a.c.scales[2 * blk]) + 0.0f;
+  }
+}
+
+// The n best blocks of a (row, kv head), in the order of their indices.  Equal scores: the lower index.  A NaN (a block
+// with an infinity or NaN) counts as greatest, so that it is read and seen.  Threshold by histograms of 2,048 bins over the
+// range that is left, at most three times; then one pass in the order of the blocks writes what lies above it.
+constexpr int PICK_THREADS = 1024, PICK_BINS = 2048, PICK_LDS_KEYS = 8192;
+__device__ __forceinline__ uint32_t score_key(float s) {
+  const uint32_t u = __float_as_uint(s);
+  return s != s ? 0xFFFFFFFFu : (u & 0x80000000u ? ~u : u | 0x80000000u);
+}
+__global__ __launch_bounds__(PICK_THREADS) void k_kv8_pick(Kv8SelectArgs a, int nb_max) {
+  constexpr int NW = PICK_THREADS / 64;
+  __shared__ uint32_t keys[PICK_LDS_KEYS];
+  __shared__ int hist[PICK_BINS];
+  __shared__ uint32_t wlo[NW], whi[NW];
+  __shared__ int wsum[NW], wsum2[NW];
+  __shared__ uint32_t s_lo, s_hi;
+  __shared__ int s_need;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r];
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  int* out = a.blocks + pair * a.n;
+  const bool bad = n < 0 || n > a.kv_max;
+  if (bad && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+  const int closed = bad || !a.enable[r] ? 0 : n / KV8_BLOCK, take = min(a.n, closed);
+  if (tid == 0) a.n_blocks[pair] = take;
+  for (int i = tid; i < a.n; i += PICK_THREADS)
+    if (i >= take) out[i] = -1;
+    else if (closed <= a.n) out[i] = i;
+  if (closed <= a.n) return;
+  // blocks [f, l) are chosen by score; the first f and those from l on are always taken
+  const int f = a.first, l = closed - a.last;
+  int need = take - a.first - a.last;  // f + last <= n < closed
+  const float* sc = a.scores + pair * nb_max;
+  const bool in_lds = l - f <= PICK_LDS_KEYS;
+  const auto key_at = [&](int b) { return in_lds ? keys[b - f] : score_key(sc[b]); };
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int b = f + tid; b < l; b += PICK_THREADS) {
+    const uint32_t k = score_key(sc[b]);
+    if (in_lds) keys[b - f] = k;
+    lo = min(lo, k);
+    hi = max(hi, k);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, WAVE));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, WAVE));
+  }
+  if (lane == 0) {
+    wlo[w] = lo;
+    whi[w] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    lo = min(lo, wlo[i]);
+    hi = max(hi, whi[i]);
+  }
+  // invariant: every key above hi is taken, `need` of those in [lo, hi] are, none below lo
+  while (need > 0 && lo < hi) {
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
+    for (int i = tid; i < PICK_BINS; i += PICK_THREADS) hist[i] = 0;
+    __syncthreads();
+    for (int b = f + tid; b < l; b += PICK_THREADS) {
+      const uint32_t k = key_at(b);
+      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+    }
+    __syncthreads();
+    // keys in the bins above: thread t holds bins 2047 - 2t and 2046 - 2t
+    const int j = PICK_BINS - 1 - 2 * tid, h0 = hist[j], h1 = hist[j - 1];
+    int inc = h0 + h1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(inc, o, WAVE);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 63) wsum[w] = inc;
+    __syncthreads();
+    int above = inc - h0 - h1;
+    for (int i = 0; i < w; ++i) above += wsum[i];
+    if (above < need && need <= above + h0 + h1) {  // one thread
+      const bool first = need <= above + h0;
+      const uint32_t bin = first ? j : j - 1, b_lo = lo + (bin << shift);
+      s_need = need - above - (first ? 0 : h0);
+      s_lo = b_lo;
+      s_hi = min(hi - b_lo, (1u << shift) - 1) + b_lo;
+    }
+    __syncthreads();
+    lo = s_lo;
+    hi = s_hi;
+    need = s_need;
+  }
+  // keys above hi, and the first `need` of those equal to it (need is 0 only where nothing is chosen by score)
+  int base = 0, base_eq = 0;
+  for (int b0 = 0; b0 < closed; b0 += PICK_THREADS) {
+    const int b = b0 + tid;
+    const bool in = b >= f && b < l;
+    const uint32_t k = in ? key_at(b) : 0;
+    const bool gt = b < closed && (in ? need > 0 && k > hi : true), eq = in && need > 0 && k == hi;
+    const unsigned long long mg = __ballot(gt), me = __ballot(eq), below = (1ull << lane) - 1;
+    __syncthreads();  // the sums of the pass before have been read
+    if (lane == 0) {
+      wsum[w] = __popcll(mg);
+      wsum2[w] = __popcll(me);
+    }
+    __syncthreads();
+    int ng = base + __popcll(mg & below), ne = base_eq + __popcll(me & below);
+    for (int i = 0; i < NW; ++i) {
+      if (i < w) {
+        ng += wsum[i];
+        ne += wsum2[i];
+      }
+      base += wsum[i];
+      base_eq += wsum2[i];
+    }
+    if (gt || (eq && ne < need)) out[ng + min(ne, need)] = b;
+  }
+}
+
+// ---------------------------------------------------------------- attention
+// bf16 planes of an fp32 operand: v = p0 + p1 (+ p2), 16 or 24 significant bits.  A bf16 model's activations are pairs
+// anyway; with three planes the products of an fp32 model lose nothing, as codes are exact in bf16.
+template <typename T> struct Planes;
+template <> struct Planes<bf16> { static constexpr int N = 2; };
+template <> struct Planes<float> { static constexpr int N = 3; };
+
+template <int N>
+__device__ __forceinline__ void to_planes(const float* v, u4* p) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    p[n] = pack_frag_bf16(r);
+    if (n + 1 < N) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] -= bf2f((bf16)((e & 1) ? (p[n][e >> 1] >> 16) : (p[n][e >> 1] & 0xFFFFu)));
+    }
+  }
+}
+
+// eight e4m3 codes as bf16 (exact)
+__device__ __forceinline__ u4 codes_bf16(uint32_t a, uint32_t b) {
+  return u4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false)),
+            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true))};
+}
+
+template <int HD>
+struct CodeBlock {  // a block in registers: 16 bytes a lane of each 1 KB piece
+  u4 k[2][HD / 64], v[HD / 32];
+  float ks, vs;
+};
+template <int HD>
+__device__ __forceinline__ void load_block(CodeBlock<HD>& x, const uint8_t* codes, const float* scales, int blk) {
+  const uint8_t* p = codes + (size_t)blk * (2 * KV8_BLOCK * HD) + (threadIdx.x & 63) * 16;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) x.k[t][i] = ld16_stream(p + (t * (HD / 64) + i) * 1024);
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) x.v[i] = ld16_stream(p + KV8_BLOCK * HD + i * 1024);
+  x.ks = scales[2 * (size_t)blk];
+  x.vs = scales[2 * (size_t)blk + 1];
+}
+
+// Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
+// and P V.  `scale` is log2(e) / sqrt(hd).
+template <int HD, int N>
+__device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*q)[N], float scale, float& m, float& l, f4* o) {
+  const int g = (threadIdx.x & 63) >> 4;
+  float sc[8];
+  const float c = x.ks * scale;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    f4 s = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u4 k = codes_bf16(x.k[t][i][2 * h], x.k[t][i][2 * h + 1]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) Frag<bf16>::mma(s, k, q[2 * i + h][n]);
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sc[4 * t + e] = s[e] * c;
+  }
+  float top = sc[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
+  top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+  top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+  const float mnew = fmaxf(m, top), mz = mnew == -INFINITY ? 0.f : mnew;  // scores of -inf alone: all weights 0
+  float p[8], ps = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(sc[e] - mz);
+    ps += p[e];
+    p[e] *= x.vs;
+  }
+  ps += __shfl_xor(ps, 16, WAVE);
+  ps += __shfl_xor(ps, 32, WAVE);
+  if (__any(mnew != m)) {  // a maximum rarely moves once a row has seen many keys
+    const float alpha = __builtin_amdgcn_exp2f(m - mz);
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float ai = __shfl(alpha, 4 * g + i, WAVE);
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[d][i] *= ai;
+    }
+    m = mnew;
+  }
+  l += ps;
+  u4 pp[N];
+  to_planes<N>(p, pp);
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u4 v = codes_bf16(x.v[i][2 * h], x.v[i][2 * h + 1]);
+#pragma unroll
+      for (int n = 0; n < N; ++n) Frag<bf16>::mma(o[2 * i + h], pp[n], v);
+    }
+}
+
+constexpr int ATT_NW = 8;
+template <int HD, int GR>
+struct AttLds {
+  float o[ATT_NW][GR][HD];
+  float m[ATT_NW][16], l[ATT_NW][16];
+  float q[GR][HD];                 // the open block's part
+  float v[KV8_BLOCK][HD];
+  float p[GR][KV8_BLOCK];
+  float tm[GR], tl[GR];
+};
+
+// One workgroup per (split, kv head, row); its waves take every eighth block of the split's share.  Split 0 attends over
+// the open block too, in fp32 on the vector units (at most 31 slots).
+template <typename T, int HD, int GR>
+__global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
+  constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, CPL = HD / 16;  // channels a lane of the open block
+  __shared__ AttLds<HD, GR> sh;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r16 = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk;
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  int n = a.kv_len[r];
+  if (n < 0 || n > a.kv_max) {
+    if (split == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+    n = 0;
+  }
+  if (!a.enable[r]) n = 0;
+  const int closed = n / B, rest = n % B;
+  int cnt = closed;
+  const int* list = nullptr;
+  if (a.blocks && n > 0) {
+    list = a.blocks + pair * a.max_blocks;
+    cnt = a.n_blocks[pair];
+    if (cnt < 0 || cnt > a.max_blocks) {
+      if (split == 0 && tid == 0) atomicOr(a.err + r, 16);
+      cnt = 0;
+    }
+  }
+  const int per = (cnt + a.nsplit - 1) / a.nsplit, e0 = min(cnt, split * per), e1 = min(cnt, e0 + per);
+  const bool tail = split == 0 && rest > 0;
+  // this thread's share of the open block: slot ts, channels tc ..
+  const int ts = tid / 16, tc = tid % 16 * CPL;
+  f4 tk[CPL / 4], tv[CPL / 4];
+  if (tail && ts < rest) {
+    const T* op = (const T*)a.c.open + pair * 2 * B * HD + ts * HD + tc;
+#pragma unroll
+    for (int i = 0; i < CPL / 4; ++i) {
+      tk[i] = ld4<T>(op + 4 * i);
+      tv[i] = ld4<T>(op + B * HD + 4 * i);
+    }
+  }
+  if (tail)
+    for (int i = tid * 4; i < grp * HD; i += 64 * ATT_NW * 4)
+      *reinterpret_cast<f4*>(&sh.q[i / HD][i % HD]) = get_act4<T>(a.q, r, a.H * HD, kvh * grp * HD + i);
+  // query fragments, channels in the order of the K codes: fragment 2 i + h holds 64 i + 16 g + 8 h ..
+  u4 q[NF][N];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    const int d = 64 * (f / 2) + 16 * g + 8 * (f % 2);
+    if (r16 < grp) {
+      const T* p = (const T*)a.q + (size_t)r * Act<T>::PL * a.H * HD + (size_t)(kvh * grp + r16) * HD + d;
+      if constexpr (Act<T>::SPLIT) {
+        q[f][0] = ld16(p);
+        q[f][1] = ld16(p + a.H * HD);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = p[e];
+        to_planes<N>(v, q[f]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[f][i] = zero16();
+    }
+  }
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  f4 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const uint8_t* codes = a.c.codes + pair * a.c.NB * (2 * B * HD);
+  const float* scales = a.c.scales + pair * a.c.NB * 2;
+  for (int c0 = e0 + w; c0 < e1; c0 += ATT_NW * 64) {  // 64 of the wave's blocks at a time
+    const int mine = min(64, (e1 - c0 + ATT_NW - 1) / ATT_NW);
+    int blk = c0 + lane * ATT_NW;
+    if (list && lane < mine) {
+      const int e = blk, before = e > 0 ? list[e - 1] : -1;
+      blk = list[e];
+      if (blk < 0 || blk <= before || blk >= closed) {  // not ascending or out of range: left out
+        atomicOr(a.err + r, 16);
+        blk = -1;
+      }
+    }
+    CodeBlock<HD> x0, x1;
+    int i0 = __builtin_amdgcn_readlane(blk, 0), i1 = -1;
+    if (i0 >= 0) load_block<HD>(x0, codes, scales, i0);
+    for (int j = 0; j < mine; j += 2) {
+      i1 = j + 1 < mine ? __builtin_amdgcn_readlane(blk, j + 1) : -1;
+      if (i1 >= 0) load_block<HD>(x1, codes, scales, i1);
+      if (i0 >= 0) attend_block<HD, N>(x0, q, scale, m, l, o);
+      i0 = j + 2 < mine ? __builtin_amdgcn_readlane(blk, j + 2) : -1;
+      if (i0 >= 0) load_block<HD>(x0, codes, scales, i0);
+      if (i1 >= 0) attend_block<HD, N>(x1, q, scale, m, l, o);
+    }
+  }
+  // per wave: maximum, sum and unnormalised outputs
+  if (g == 0) {
+    sh.m[w][r16] = m;
+    sh.l[w][r16] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = 4 * g + i;
+    if (j < grp) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) sh.o[w][j][d * 16 + r16] = o[d][i];
+    }
+  }
+  __syncthreads();
+  if (tail) {
+    if (ts < rest) {
+#pragma unroll
+      for (int i = 0; i < CPL / 4; ++i) *reinterpret_cast<f4*>(&sh.v[ts][tc + 4 * i]) = tv[i];
+    }
+    for (int j = 0; j < grp; ++j) {
+      float s = 0.f;
+      if (ts < rest) {
+#pragma unroll
+        for (int i = 0; i < CPL / 4; ++i) {
+          const f4 qv = *reinterpret_cast<const f4*>(&sh.q[j][tc + 4 * i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s += qv[e] * tk[i][e];
+        }
+      }
+#pragma unroll
+      for (int b = 1; b < 16; b <<= 1) s += __shfl_xor(s, b, WAVE);
+      if (tid % 16 == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
+    }
+    __syncthreads();
+    for (int j = w; j < grp; j += ATT_NW) {
+      const float s = lane < B ? sh.p[j][lane] : -INFINITY;
+      const float top = wave_max(s), mz = top == -INFINITY ? 0.f : top;
+      const float p = lane < rest ? __builtin_amdgcn_exp2f(s - mz) : 0.f;
+      const float sum = wave_sum(p);
+      if (lane < B) sh.p[j][lane] = p;
+      if (lane == 0) {
+        sh.tm[j] = top;
+        sh.tl[j] = sum;
+      }
+    }
+    __syncthreads();
+  }
+  for (int t = tid; t < grp * HD; t += 64 * ATT_NW) {
+    const int j = t / HD, d = t % HD;
+    float M = tail ? sh.tm[j] : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < ATT_NW; ++i) M = fmaxf(M, sh.m[i][j]);
+    const float mz = M == -INFINITY ? 0.f : M;
+    float L = 0.f, O = 0.f;
+#pragma unroll
+    for (int i = 0; i < ATT_NW; ++i) {
+      const float e = __builtin_amdgcn_exp2f(sh.m[i][j] - mz);  // 0 for a wave without slots
+      // a wave whose scores are all NaN has maximum -inf and sum NaN, which e = 0 keeps
+      L += e * sh.l[i][j];
+      O += e * sh.o[i][j][d];
+    }
+    if (tail) {
+      const float e = __builtin_amdgcn_exp2f(sh.tm[j] - mz);
+      float x = 0.f;
+      for (int s = 0; s < rest; ++s) x += sh.p[j][s] * sh.v[s][d];
+      L += e * sh.tl[j];
+      O += e * x;
+    }
+    if (a.nsplit == 1) {
+      Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L == 0.f ? 0.f : O / L);
+    } else {
+      const size_t rec = (pair * a.nsplit + split) * grp + j;
+      a.part[rec * HD + d] = O;
+      if (d == 0) {
+        float* ml = a.part + (size_t)a.R * a.Hk * a.nsplit * grp * HD + 2 * rec;
+        ml[0] = M;
+        ml[1] = L;
+      }
+    }
+  }
+}
+
+// Log-sum-exp combine of the splits of one (row, q-head), in split order.
+constexpr int COMB_THREADS = 256;
+template <typename T, int HD>
+__global__ __launch_bounds__(COMB_THREADS) void k_kv8_combine(Kv8AttnArgs a) {
+  constexpr int G = COMB_THREADS / HD;
+  __shared__ float wts[64];
+  __shared__ float acc[COMB_THREADS];
+  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, ns = a.nsplit;
+  const int grp = a.H / a.Hk, kvh = h / grp, j = h % grp;
+  const size_t rec0 = ((size_t)r * a.Hk + kvh) * ns * grp + j;  // record of split s: rec0 + s * grp
+  if (tid < 64) {
+    float ms = -INFINITY, ls = 0.f;
+    if (lane < ns) {
+      const float* ml = a.part + (size_t)a.R * a.Hk * ns * grp * HD + 2 * (rec0 + (size_t)lane * grp);
+      ms = ml[0];
+      ls = ml[1];
+    }
+    const float M = wave_max(ms), mz = M == -INFINITY ? 0.f : M;
+    const float e = __builtin_amdgcn_exp2f(ms - mz);
+    const float L = wave_sum(e * ls);
+    wts[lane] = L == 0.f ? 0.f : e / L;
+  }
+  __syncthreads();
+  const int d = tid % HD, sg = tid / HD;
+  float o = 0.f;
+  for (int s = sg; s < ns; s += G) o += wts[s] * a.part[(rec0 + (size_t)s * grp) * HD + d];
+  acc[tid] = o;
+  __syncthreads();
+  if (tid < HD) {
+    float x = acc[tid];
+#pragma unroll
+    for (int i = 1; i < G; ++i) x += acc[i * HD + tid];
+    Act<T>::put(a.out, r, a.H * HD, h * HD + tid, x);
+  }
+}
+
+template <typename T, int HD>
+int append_t(const Kv8AppendArgs& a, Stream s) {
+  const int nb = std::max(1, (a.T + KV8_BLOCK - 1) / KV8_BLOCK), nq = a.q ? (a.T + APPEND_QT - 1) / APPEND_QT : 0;
+  launch_k((k_kv8_append<T, HD>), dim3(nb + nq, a.Hk, a.R), dim3(CODE_THREADS), 0, s, a, nb);
+  return 0;
+}
+template <typename T, int HD>
+int pack_t(const Kv8PackArgs& a, Stream s) {
+  launch_k((k_kv8_pack<T, HD>), dim3(std::max(1, (a.kv_max + KV8_BLOCK - 1) / KV8_BLOCK), a.Hk, a.R), dim3(CODE_THREADS), 0, s, a);
+  return 0;
+}
+template <typename T, int HD>
+int select_t(const Kv8SelectArgs& a, Stream s) {
+  const int nb = a.kv_max / KV8_BLOCK;
+  if (nb > a.n)
+    launch_k((k_kv8_scores<T, HD>), dim3((nb + SCORE_BLOCKS - 1) / SCORE_BLOCKS, a.Hk, a.R), dim3(SCORE_THREADS), 0, s, a, nb);
+  launch_k(k_kv8_pick, dim3(a.Hk, a.R), dim3(PICK_THREADS), 0, s, a, nb);
+  return 0;
+}
+template <typename T, int HD>
+int attention_t(const Kv8AttnArgs& a, Stream s) {
+  const dim3 grid(a.nsplit, a.Hk, a.R), block(64 * ATT_NW);
+  if (a.H / a.Hk <= 4) launch_k((k_kv8_attn<T, HD, 4>), grid, block, 0, s, a);
+  else launch_k((k_kv8_attn<T, HD, 16>), grid, block, 0, s, a);
+  if (a.nsplit > 1) launch_k((k_kv8_combine<T, HD>), dim3(a.R, a.H), dim3(COMB_THREADS), 0, s, a);
+  return 0;
+}
+
+#define KV8_DISPATCH(fn)                                                    \
+  do {                                                                      \
+    if (hd == 64) return dtype == 1 ? fn<bf16, 64>(a, s) : fn<float, 64>(a, s);    \
+    if (hd == 128) return dtype == 1 ? fn<bf16, 128>(a, s) : fn<float, 128>(a, s); \
+    return -1;                                                              \
+  } while (0)
+
+}  // namespace
+
+int launch_kv8_append(int dtype, int hd, const Kv8AppendArgs& a, Stream s) { KV8_DISPATCH(append_t); }
+int launch_kv8_pack(int dtype, int hd, const Kv8PackArgs& a, Stream s) { KV8_DISPATCH(pack_t); }
+int launch_kv8_select(int dtype, int hd, const Kv8SelectArgs& a, Stream s) { KV8_DISPATCH(select_t); }
+int launch_kv8_attention(int dtype, int hd, const Kv8AttnArgs& a, Stream s) { KV8_DISPATCH(attention_t); }
+
+}  // namespace ham

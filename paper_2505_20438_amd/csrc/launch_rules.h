@@ -72,4 +72,12 @@ inline PromptAttnGrid prompt_attn_grid(int R, int s0, int T, int H, int Hkv) {
   return PromptAttnGrid{keys ? (tiles + half - 1) / half : rows_blocks, seqs, keys};
 }
 
+// Splits of the attention over the 8-bit cache for R rows of Hk kv heads of which the longest reads `blocks` blocks of 32
+// slots: workgroups until every CU has one, eight blocks (one a wave) or more each.
+inline int kv8_attn_splits(int R, int Hk, int blocks) {
+  const long long pairs = (long long)R * Hk;
+  const long long width = (256 + pairs - 1) / pairs;
+  return (int)std::max(1ll, std::min({width, (long long)(blocks + 7) / 8, (long long)MAX_ATTN_SPLIT}));
+}
+
 }  // namespace ham

@@ -20,13 +20,15 @@ HAM_STOP_HEAD, HAM_STOP_TOKEN, HAM_STOP_FORCED, HAM_STOP_FORCED_TOKEN = 0, 1, 2,
 (HAM_PROF_QKV, HAM_PROF_O, HAM_PROF_GU, HAM_PROF_DOWN, HAM_PROF_MICRO, HAM_PROF_EMBED, HAM_PROF_HEAD0, HAM_PROF_HEADK,
  HAM_PROF_ATTN, HAM_PROF_NORM) = range(10)
 HAM_PROF_KINDS = 10
+HAM_KV8_BLOCK = 32
 
 EXPORTED = ("ham_weights_bytes", "ham_state_bytes", "ham_workspace_bytes", "ham_init_weights",
             "ham_prefill", "ham_prefill_embeds", "ham_state_info", "ham_macro_step", "ham_kv_stats", "ham_set_debug", "ham_steps_done",
             "ham_tensor_info", "ham_set_graph", "ham_profile", "ham_profile_read", "ham_last_error", "ham_destroy",
             "ham_op_attention_workspace_bytes", "ham_op_decode_attention", "ham_op_attention_step",
             "ham_op_attention_step_splits", "ham_state_save", "ham_state_restore", "ham_op_attention_step_noalloc",
-            "ham_op_attention_step_noalloc_max_bytes")
+            "ham_op_attention_step_noalloc_max_bytes", "ham_op_kv8_cache_bytes", "ham_op_kv8_workspace_bytes",
+            "ham_op_kv8_info", "ham_op_kv8_append", "ham_op_kv8_pack", "ham_op_kv8_select", "ham_op_kv8_attention")
 
 
 class HamConfig(ctypes.Structure):
@@ -52,6 +54,10 @@ class HamKvStats(ctypes.Structure):
 
 class HamProfT(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int32), ("ms", ctypes.c_double), ("bytes", ctypes.c_double)]
+
+
+class HamKv8Shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "rows", "n_heads", "n_kv_heads", "head_dim", "slots_cap")]
 
 
 class HamError(RuntimeError):
@@ -100,6 +106,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ham_op_attention_step_noalloc_max_bytes.restype = SZ
     lib.ham_op_attention_step_splits.argtypes = [I32, I32, I32, I32, I32]
     lib.ham_op_attention_step_splits.restype = I32
+    k8 = ctypes.POINTER(HamKv8Shape)
+    for n in ("ham_op_kv8_cache_bytes", "ham_op_kv8_workspace_bytes"):
+        getattr(lib, n).argtypes = [k8]
+        getattr(lib, n).restype = SZ
+    lib.ham_op_kv8_info.argtypes = [k8] + [ctypes.POINTER(SZ)] * 4
+    lib.ham_op_kv8_append.argtypes = [k8, I32, P, P, P, P, P, P, SZ, P, P, P]
+    lib.ham_op_kv8_pack.argtypes = [k8, P, P, I32, P, I32, P, SZ, P, P]
+    lib.ham_op_kv8_select.argtypes = [k8, P, P, SZ, P, P, I32, I32, I32, I32, P, P, P, P, SZ, P]
+    lib.ham_op_kv8_attention.argtypes = [k8, P, P, SZ, P, P, I32, P, P, I32, P, P, P, SZ, P]
     lib.ham_state_save.argtypes = [P, P, SZ]
     lib.ham_state_restore.argtypes = [P, P, SZ]
     lib.ham_last_error.restype = ctypes.c_char_p
@@ -107,7 +122,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ham_destroy.restype = None
     for n in ("ham_init_weights", "ham_prefill", "ham_prefill_embeds", "ham_state_info", "ham_macro_step", "ham_kv_stats", "ham_set_debug",
               "ham_steps_done", "ham_tensor_info", "ham_set_graph", "ham_profile", "ham_profile_read",
-              "ham_state_save", "ham_state_restore"):
+              "ham_state_save", "ham_state_restore", "ham_op_kv8_info", "ham_op_kv8_append", "ham_op_kv8_pack",
+              "ham_op_kv8_select", "ham_op_kv8_attention"):
         getattr(lib, n).restype = I32
     _lib = lib
     return lib
@@ -249,6 +265,100 @@ def ham_op_attention_step_splits(dtype: int, rows: int, n_kv_heads: int, head_di
 
 def ham_op_attention_workspace_bytes(rows: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
     return load_library().ham_op_attention_workspace_bytes(rows, n_heads, n_kv_heads, head_dim)
+
+
+def kv8_shape(dtype: int, rows: int, n_heads: int, n_kv_heads: int, head_dim: int, slots_cap: int) -> HamKv8Shape:
+    """Shape of a layer's KV cache in 8 bits (include/ham_ops.h)."""
+    return HamKv8Shape(dtype, rows, n_heads, n_kv_heads, head_dim, slots_cap)
+
+
+def ham_op_kv8_cache_bytes(shape: HamKv8Shape) -> int:
+    return load_library().ham_op_kv8_cache_bytes(ctypes.byref(shape))
+
+
+def ham_op_kv8_workspace_bytes(shape: HamKv8Shape) -> int:
+    return load_library().ham_op_kv8_workspace_bytes(ctypes.byref(shape))
+
+
+def ham_op_kv8_info(shape: HamKv8Shape) -> dict:
+    v = [ctypes.c_size_t() for _ in range(4)]
+    _check(load_library().ham_op_kv8_info(ctypes.byref(shape), *[ctypes.byref(x) for x in v]))
+    return {k: x.value for k, x in zip(("codes", "scales", "bounds", "open"), v)}
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def _holds(shape: HamKv8Shape, **tensors) -> None:
+    """Device tensors against what the call reads and writes of them: name=(tensor, bytes); packed, at least that large."""
+    for name, (t, need) in tensors.items():
+        if not t.is_contiguous():
+            raise HamError(HAM_EINVAL, f"{name} must be contiguous")
+        if _nbytes(t) < need:
+            raise HamError(HAM_EINVAL, f"{name} holds {_nbytes(t)} bytes, the call needs {need}")
+
+
+def _act_bytes(shape: HamKv8Shape, rows: int) -> int:
+    return rows * shape.n_heads * shape.head_dim * 4   # fp32, or a bf16 hi/lo pair
+
+
+def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int) -> None:
+    """RoPE and append of ``count[r]`` slots per row (include/ham_ops.h): qkv fp32 [rows][n_tokens][...], q act rows of
+    the same tokens or None."""
+    n = qkv.numel() // max(1, shape.rows * (shape.n_heads + 2 * shape.n_kv_heads) * shape.head_dim)
+    rope = shape.rows * n * shape.head_dim * 2
+    need = dict(qkv=(qkv, shape.rows * n * (shape.n_heads + 2 * shape.n_kv_heads) * shape.head_dim * 4), cos=(cos, rope),
+                sin=(sin, rope), start=(start, 4 * shape.rows), count=(count, 4 * shape.rows), err=(err, 4 * shape.rows),
+                cache=(cache, 0))
+    if q is not None:
+        need["q"] = (q, _act_bytes(shape, shape.rows * n))
+    _holds(shape, **need)
+    _check(load_library().ham_op_kv8_append(
+        ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), start.data_ptr(), count.data_ptr(),
+        cache.data_ptr(), _nbytes(cache), _ptr(q), err.data_ptr(), stream))
+
+
+def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, stream: int) -> None:
+    """A filled cache of the storage type, k [rows][n_kv_heads][slots][head_dim] and vt its V tiles, into 8 bits."""
+    slots = k.numel() // max(1, shape.rows * shape.n_kv_heads * shape.head_dim)
+    need = shape.rows * shape.n_kv_heads * slots * shape.head_dim * (2 if shape.dtype == HAM_BF16 else 4)
+    _holds(shape, k=(k, need), vt=(vt, need), kv_len=(kv_len, 4 * shape.rows), err=(err, 4 * shape.rows), cache=(cache, 0))
+    _check(load_library().ham_op_kv8_pack(
+        ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), _nbytes(cache),
+        err.data_ptr(), stream))
+
+
+def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int, n_blocks: int, keep_first: int,
+                      keep_last: int, blocks, count, err, workspace, stream: int) -> None:
+    """The ``n_blocks`` closed blocks of each (row, kv head) with the greatest bounds of q . k, ascending, into ``blocks``
+    int32 [rows][n_kv_heads][n_blocks]; how many into ``count`` int32 [rows][n_kv_heads]."""
+    r = 4 * shape.rows
+    _holds(shape, q=(q, _act_bytes(shape, shape.rows)), cache=(cache, 0), kv_len=(kv_len, r), enable=(enable, r), err=(err, r),
+           blocks=(blocks, r * shape.n_kv_heads * max(0, n_blocks)), count=(count, r * shape.n_kv_heads), workspace=(workspace, 0))
+    _check(load_library().ham_op_kv8_select(
+        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), _nbytes(cache), kv_len.data_ptr(), enable.data_ptr(), kv_max,
+        n_blocks, keep_first, keep_last, blocks.data_ptr(), count.data_ptr(), err.data_ptr(), workspace.data_ptr(),
+        _nbytes(workspace), stream))
+
+
+def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int, blocks, count, out, err, workspace,
+                         stream: int) -> None:
+    """Attention of one act row per sequence over an 8-bit cache: every block, or those of ``blocks`` and ``count``
+    (ham_op_kv8_select), and the open one."""
+    r = 4 * shape.rows
+    need = dict(q=(q, _act_bytes(shape, shape.rows)), cache=(cache, 0), kv_len=(kv_len, r), enable=(enable, r), err=(err, r),
+                out=(out, _act_bytes(shape, shape.rows)), workspace=(workspace, 0))
+    most = 0
+    if blocks is not None:
+        most = blocks.numel() // max(1, shape.rows * shape.n_kv_heads)
+        need["blocks"] = (blocks, r * shape.n_kv_heads * most)
+    if count is not None:
+        need["count"] = (count, r * shape.n_kv_heads)
+    _holds(shape, **need)
+    _check(load_library().ham_op_kv8_attention(
+        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), _nbytes(cache), kv_len.data_ptr(), enable.data_ptr(), kv_max,
+        _ptr(blocks), _ptr(count), most, out.data_ptr(), err.data_ptr(), workspace.data_ptr(), _nbytes(workspace), stream))
 
 
 def ham_steps_done(model: int) -> int:

@@ -1,0 +1,174 @@
+"""The operators on a KV cache in 8 bits without a GPU: sizes, regions, refusals of every entry point, and the launch rule.
+
+Every call here is refused before anything is launched; pointers are numbers that nothing reads.
+"""
+import ctypes
+import os
+import subprocess
+import tempfile
+
+import pytest
+import torch
+
+from paper_2505_20438_amd import ham
+from synth.configs import BF16, F32
+from tests import kv8_ref
+
+GOOD = dict(dtype=BF16, rows=3, n_heads=32, n_kv_heads=8, head_dim=128, slots_cap=4096)
+
+
+def shape(**kw):
+    s = dict(GOOD, **kw)
+    return ham.kv8_shape(*(s[k] for k in ("dtype", "rows", "n_heads", "n_kv_heads", "head_dim", "slots_cap")))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(ham.LIB_PATH):
+        pytest.skip("libham.so not built")
+    return ham.load_library()
+
+
+BAD_SHAPES = [("dtype", 2), ("dtype", -1), ("rows", 0), ("rows", 4097), ("n_heads", 0), ("n_heads", 30), ("n_heads", 136),
+              ("n_kv_heads", 0), ("n_kv_heads", 1), ("head_dim", 96), ("head_dim", 32), ("slots_cap", 0), ("slots_cap", 48),
+              ("slots_cap", (1 << 24) + 32), ("slots_cap", -32)]
+
+
+@pytest.mark.parametrize("field,value", BAD_SHAPES)
+def test_bad_shapes_have_no_size_and_no_call(lib, field, value):
+    s = shape(**{field: value})
+    p = ctypes.byref(s)
+    assert ham.ham_op_kv8_cache_bytes(s) == 0 and ham.ham_op_kv8_workspace_bytes(s) == 0
+    with pytest.raises(ham.HamError) as e:
+        ham.ham_op_kv8_info(s)
+    assert e.value.code == ham.HAM_EINVAL
+    big = 1 << 60
+    assert lib.ham_op_kv8_append(p, 1, 256, 256, 256, 256, 256, 256, big, 256, 256, None) == ham.HAM_EINVAL
+    assert lib.ham_op_kv8_pack(p, 256, 256, 4096, 256, 10, 256, big, 256, None) == ham.HAM_EINVAL
+    assert lib.ham_op_kv8_select(p, 256, 256, big, 256, 256, 10, 1, 0, 0, 256, 256, 256, 256, big, None) == ham.HAM_EINVAL
+    assert lib.ham_op_kv8_attention(p, 256, 256, big, 256, 256, 10, None, None, 0, 256, 256, 256, big, None) == ham.HAM_EINVAL
+
+
+def test_a_null_shape_is_refused(lib):
+    assert lib.ham_op_kv8_cache_bytes(None) == 0 and lib.ham_op_kv8_workspace_bytes(None) == 0
+    assert lib.ham_op_kv8_info(None, None, None, None, None) == ham.HAM_EINVAL
+    assert lib.ham_op_kv8_info(ctypes.byref(shape()), None, None, None, None) == ham.HAM_EINVAL
+    assert lib.ham_op_kv8_append(None, 1, 256, 256, 256, 256, 256, 256, 1 << 60, 256, 256, None) == ham.HAM_EINVAL
+
+
+@pytest.mark.parametrize("dtype,rows,H,Hk,hd,slots", [(BF16, 3, 32, 8, 128, 4096), (F32, 1, 4, 2, 64, 32), (BF16, 64, 9, 3, 64, 96),
+                                                      (BF16, 2, 16, 1, 128, 1 << 24)])
+def test_regions_do_not_overlap_and_fit(lib, dtype, rows, H, Hk, hd, slots):
+    s = ham.kv8_shape(dtype, rows, H, Hk, hd, slots)
+    i, total, blocks = ham.ham_op_kv8_info(s), ham.ham_op_kv8_cache_bytes(s), rows * Hk * slots // 32
+    sizes = dict(codes=blocks * 64 * hd, scales=blocks * 8, bounds=blocks * 2 * hd,
+                 open=rows * Hk * 64 * hd * (2 if dtype == BF16 else 4))
+    spans = sorted((i[k], i[k] + n) for k, n in sizes.items())
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and spans[-1][1] <= total
+    assert all(i[k] % 256 == 0 for k in sizes)
+    assert ham.ham_op_kv8_workspace_bytes(s) >= blocks * 4
+
+
+def test_code_positions_fill_a_block():
+    for hd in (64, 128):
+        for at in kv8_ref.code_index(hd):
+            assert sorted(at.reshape(-1).tolist()) == list(range(32 * hd))
+
+
+# argument positions after the shape; a refused value and the error it gives
+@pytest.mark.parametrize("at,value,code", [
+    (0, 0, "EINVAL"), (0, (1 << 24) + 1, "EINVAL"), (0, -1, "EINVAL"), (1, None, "EINVAL"), (1, 260, "EINVAL"), (2, None, "EINVAL"), (2, 264, "EINVAL"),
+    (3, None, "EINVAL"), (4, None, "EINVAL"), (5, None, "EINVAL"), (6, None, "EINVAL"), (6, 128, "EINVAL"), (7, 1000, "ENOMEM"),
+    (8, 8, "EINVAL"), (9, None, "EINVAL")])
+def test_append_refusals(lib, at, value, code):
+    args = [1, 256, 256, 256, 256, 256, 256, 1 << 60, 256, 256]
+    args[at] = value
+    assert lib.ham_op_kv8_append(ctypes.byref(shape()), *args, None) == getattr(ham, "HAM_" + code)
+    assert lib.ham_last_error()
+
+
+@pytest.mark.parametrize("at,value,code", [
+    (0, None, "EINVAL"), (0, 8, "EINVAL"), (1, None, "EINVAL"), (2, 31, "EINVAL"), (2, 0, "EINVAL"), (3, None, "EINVAL"), (4, -1, "EINVAL"),
+    (4, 4097, "EINVAL"), (5, None, "EINVAL"), (6, 5, "ENOMEM"), (7, None, "EINVAL")])
+def test_pack_refusals(lib, at, value, code):
+    args = [256, 256, 8192, 256, 4000, 256, 1 << 60, 256]
+    args[at] = value
+    assert lib.ham_op_kv8_pack(ctypes.byref(shape()), *args, None) == getattr(ham, "HAM_" + code)
+
+
+def test_pack_reads_no_slot_that_the_source_lacks(lib):
+    assert lib.ham_op_kv8_pack(ctypes.byref(shape()), 256, 256, 64, 256, 65, 256, 1 << 60, 256, None) == ham.HAM_EINVAL
+
+
+@pytest.mark.parametrize("at,value,code", [
+    (0, None, "EINVAL"), (1, None, "EINVAL"), (1, 300, "EINVAL"), (2, 7, "ENOMEM"), (3, None, "EINVAL"), (4, None, "EINVAL"), (5, -1, "EINVAL"),
+    (5, 4097, "EINVAL"), (6, 0, "EINVAL"), (6, 129, "EINVAL"), (7, -1, "EINVAL"), (7, 4, "EINVAL"), (8, -1, "EINVAL"), (8, 3, "EINVAL"),
+    (8, 2147483647, "EINVAL"), (9, None, "EINVAL"), (10, None, "EINVAL"), (11, None, "EINVAL"), (12, None, "EINVAL"), (13, 64, "ENOMEM")])
+def test_select_refusals(lib, at, value, code):
+    args = [256, 256, 1 << 60, 256, 256, 4000, 4, 2, 2, 256, 256, 256, 256, 1 << 60]
+    args[at] = value
+    assert lib.ham_op_kv8_select(ctypes.byref(shape()), *args, None) == getattr(ham, "HAM_" + code)
+
+
+@pytest.mark.parametrize("at,value,code", [
+    (0, None, "EINVAL"), (0, 24, "EINVAL"), (1, None, "EINVAL"), (2, 7, "ENOMEM"), (3, None, "EINVAL"), (4, None, "EINVAL"), (5, -1, "EINVAL"),
+    (5, 4097, "EINVAL"), (6, None, "EINVAL"), (7, None, "EINVAL"), (8, 0, "EINVAL"), (8, 129, "EINVAL"), (9, None, "EINVAL"), (9, 8, "EINVAL"),
+    (10, None, "EINVAL"), (11, None, "EINVAL"), (12, 64, "ENOMEM")])
+def test_attention_refusals(lib, at, value, code):
+    args = [256, 256, 1 << 60, 256, 256, 4000, 256, 256, 4, 256, 256, 256, 1 << 60]
+    args[at] = value
+    assert lib.ham_op_kv8_attention(ctypes.byref(shape()), *args, None) == getattr(ham, "HAM_" + code)
+
+
+def test_binding_refuses_tensors_that_are_too_small_or_strided(lib):
+    s = ham.kv8_shape(BF16, 2, 4, 2, 64, 64)
+    i32 = torch.zeros(2, dtype=torch.int32)
+    cache = torch.zeros(ham.ham_op_kv8_cache_bytes(s), dtype=torch.uint8)
+    ws = torch.zeros(ham.ham_op_kv8_workspace_bytes(s), dtype=torch.uint8)
+    q = torch.zeros(2, 512, dtype=torch.bfloat16)
+    qkv, cs = torch.zeros(2, 1, 512), torch.zeros(2, 1, 32)
+
+    def attend(**kw):
+        a = dict(q=q, cache=cache, kv_len=i32, enable=i32, kv_max=64, blocks=None, count=None, out=q, err=i32, workspace=ws, stream=0)
+        ham.ham_op_kv8_attention(s, *dict(a, **kw).values())
+    blocks = torch.zeros(2, 2, 1, dtype=torch.int32)
+    for bad in (dict(q=q[:, :500]), dict(q=q[:1]), dict(kv_len=i32[:1]), dict(enable=torch.zeros(4, dtype=torch.int32)[::2]),
+                dict(out=q[:1]), dict(err=i32[:1]), dict(blocks=blocks, count=blocks[0, :, 0]), dict(blocks=blocks),
+                dict(count=blocks), dict(cache=cache[:-256]), dict(workspace=ws[:16])):
+        with pytest.raises(ham.HamError):
+            attend(**bad)
+    for bad in (dict(cos=cs[:1]), dict(sin=cs[:, :, ::2]), dict(start=i32[:1]), dict(q=q[:1]), dict(qkv=qkv[:1])):
+        a = dict(qkv=qkv, cos=cs, sin=cs, start=i32, count=i32, cache=cache, q=q, err=i32, stream=0)
+        with pytest.raises(ham.HamError):
+            ham.ham_op_kv8_append(s, *dict(a, **bad).values())
+
+
+@pytest.fixture(scope="module")
+def splits():
+    """kv8_attn_splits of csrc/launch_rules.h, compiled on its own."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_20438_amd", "csrc")
+    with tempfile.TemporaryDirectory() as d:
+        src, out = os.path.join(d, "r.cpp"), os.path.join(d, "r.so")
+        with open(src, "w") as f:
+            f.write('#include "launch_rules.h"\nextern "C" int splits(int R, int Hk, int blocks) '
+                    '{ return ham::kv8_attn_splits(R, Hk, blocks); }\n')
+        subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc, src, "-o", out], check=True)
+        yield ctypes.CDLL(out).splits
+
+
+def test_split_limits(splits):
+    for rows in (1, 2, 3, 7, 16, 33, 64, 500, 4096):
+        for hk in (1, 2, 3, 8, 64, 1024):
+            last = 0
+            for blocks in (0, 1, 7, 8, 9, 15, 16, 17, 64, 80, 100, 1000, 1 << 19):
+                n = splits(rows, hk, blocks)
+                assert 1 <= n <= 64 and n >= last, (rows, hk, blocks)      # the workspace holds the records of the most blocks
+                last = n
+
+
+def test_workspace_holds_the_records_of_every_length(lib, splits):
+    for rows, H, hk, hd, slots in ((1, 32, 8, 128, 33344), (4, 32, 8, 128, 33344), (32, 32, 8, 64, 2560), (1, 16, 1, 128, 1 << 20)):
+        s = ham.kv8_shape(BF16, rows, H, hk, hd, slots)
+        for blocks in range(0, slots // 32 + 1, 7):
+            n = splits(rows, hk, blocks)
+            assert n == 1 or ham.ham_op_kv8_workspace_bytes(s) >= rows * H * n * (hd + 2) * 4
