@@ -286,46 +286,47 @@ def ham_op_kv8_info(shape: HamKv8Shape) -> dict:
     return {k: x.value for k, x in zip(("codes", "scales", "bounds", "open"), v)}
 
 
-def _nbytes(t) -> int:
-    return t.numel() * t.element_size()
+def _fits(*tensors) -> bool:
+    """Whether device tensors hold what a call reads and writes of them: (tensor, bytes) pairs, packed and large enough."""
+    for t, need in tensors:
+        if t.nbytes < need or not t.is_contiguous():
+            return False
+    return True
 
 
-def _holds(shape: HamKv8Shape, **tensors) -> None:
-    """Device tensors against what the call reads and writes of them: name=(tensor, bytes); packed, at least that large."""
+def _refuse(**tensors) -> None:
     for name, (t, need) in tensors.items():
         if not t.is_contiguous():
             raise HamError(HAM_EINVAL, f"{name} must be contiguous")
-        if _nbytes(t) < need:
-            raise HamError(HAM_EINVAL, f"{name} holds {_nbytes(t)} bytes, the call needs {need}")
-
-
-def _act_bytes(shape: HamKv8Shape, rows: int) -> int:
-    return rows * shape.n_heads * shape.head_dim * 4   # fp32, or a bf16 hi/lo pair
+        if t.nbytes < need:
+            raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
 
 
 def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int) -> None:
     """RoPE and append of ``count[r]`` slots per row (include/ham_ops.h): qkv fp32 [rows][n_tokens][...], q act rows of
     the same tokens or None."""
-    n = qkv.numel() // max(1, shape.rows * (shape.n_heads + 2 * shape.n_kv_heads) * shape.head_dim)
-    rope = shape.rows * n * shape.head_dim * 2
-    need = dict(qkv=(qkv, shape.rows * n * (shape.n_heads + 2 * shape.n_kv_heads) * shape.head_dim * 4), cos=(cos, rope),
-                sin=(sin, rope), start=(start, 4 * shape.rows), count=(count, 4 * shape.rows), err=(err, 4 * shape.rows),
-                cache=(cache, 0))
-    if q is not None:
-        need["q"] = (q, _act_bytes(shape, shape.rows * n))
-    _holds(shape, **need)
+    rows, hd, H = shape.rows, shape.head_dim, shape.n_heads
+    width = (H + 2 * shape.n_kv_heads) * hd
+    n = qkv.numel() // (rows * width or 1)
+    rope, act, i4 = rows * n * hd * 2, rows * n * H * hd * 4, 4 * rows   # act rows: fp32, or a bf16 hi/lo pair
+    if not (_fits((qkv, rows * n * width * 4), (cos, rope), (sin, rope), (start, i4), (count, i4), (cache, 0), (err, i4))
+            and (q is None or _fits((q, act)))):
+        _refuse(qkv=(qkv, rows * n * width * 4), cos=(cos, rope), sin=(sin, rope), start=(start, i4), count=(count, i4),
+                cache=(cache, 0), err=(err, i4), q=(err if q is None else q, 0 if q is None else act))
     _check(load_library().ham_op_kv8_append(
         ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), start.data_ptr(), count.data_ptr(),
-        cache.data_ptr(), _nbytes(cache), _ptr(q), err.data_ptr(), stream))
+        cache.data_ptr(), cache.nbytes, None if q is None else q.data_ptr(), err.data_ptr(), stream))
 
 
 def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, stream: int) -> None:
     """A filled cache of the storage type, k [rows][n_kv_heads][slots][head_dim] and vt its V tiles, into 8 bits."""
-    slots = k.numel() // max(1, shape.rows * shape.n_kv_heads * shape.head_dim)
-    need = shape.rows * shape.n_kv_heads * slots * shape.head_dim * (2 if shape.dtype == HAM_BF16 else 4)
-    _holds(shape, k=(k, need), vt=(vt, need), kv_len=(kv_len, 4 * shape.rows), err=(err, 4 * shape.rows), cache=(cache, 0))
+    rows, pairs = shape.rows, shape.rows * shape.n_kv_heads
+    slots = k.numel() // (pairs * shape.head_dim or 1)
+    need, i4 = pairs * slots * shape.head_dim * (2 if shape.dtype == HAM_BF16 else 4), 4 * rows
+    if not _fits((k, need), (vt, need), (kv_len, i4), (cache, 0), (err, i4)):
+        _refuse(k=(k, need), vt=(vt, need), kv_len=(kv_len, i4), cache=(cache, 0), err=(err, i4))
     _check(load_library().ham_op_kv8_pack(
-        ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), _nbytes(cache),
+        ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), cache.nbytes,
         err.data_ptr(), stream))
 
 
@@ -333,32 +334,32 @@ def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int,
                       keep_last: int, blocks, count, err, workspace, stream: int) -> None:
     """The ``n_blocks`` closed blocks of each (row, kv head) with the greatest bounds of q . k, ascending, into ``blocks``
     int32 [rows][n_kv_heads][n_blocks]; how many into ``count`` int32 [rows][n_kv_heads]."""
-    r = 4 * shape.rows
-    _holds(shape, q=(q, _act_bytes(shape, shape.rows)), cache=(cache, 0), kv_len=(kv_len, r), enable=(enable, r), err=(err, r),
-           blocks=(blocks, r * shape.n_kv_heads * max(0, n_blocks)), count=(count, r * shape.n_kv_heads), workspace=(workspace, 0))
+    i4, act = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4
+    lists, counts = i4 * shape.n_kv_heads * n_blocks, i4 * shape.n_kv_heads
+    if not _fits((q, act), (cache, 0), (kv_len, i4), (enable, i4), (blocks, lists), (count, counts), (err, i4), (workspace, 0)):
+        _refuse(q=(q, act), cache=(cache, 0), kv_len=(kv_len, i4), enable=(enable, i4), blocks=(blocks, lists), count=(count, counts),
+                err=(err, i4), workspace=(workspace, 0))
     _check(load_library().ham_op_kv8_select(
-        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), _nbytes(cache), kv_len.data_ptr(), enable.data_ptr(), kv_max,
+        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         n_blocks, keep_first, keep_last, blocks.data_ptr(), count.data_ptr(), err.data_ptr(), workspace.data_ptr(),
-        _nbytes(workspace), stream))
+        workspace.nbytes, stream))
 
 
 def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int, blocks, count, out, err, workspace,
                          stream: int) -> None:
     """Attention of one act row per sequence over an 8-bit cache: every block, or those of ``blocks`` and ``count``
     (ham_op_kv8_select), and the open one."""
-    r = 4 * shape.rows
-    need = dict(q=(q, _act_bytes(shape, shape.rows)), cache=(cache, 0), kv_len=(kv_len, r), enable=(enable, r), err=(err, r),
-                out=(out, _act_bytes(shape, shape.rows)), workspace=(workspace, 0))
-    most = 0
-    if blocks is not None:
-        most = blocks.numel() // max(1, shape.rows * shape.n_kv_heads)
-        need["blocks"] = (blocks, r * shape.n_kv_heads * most)
-    if count is not None:
-        need["count"] = (count, r * shape.n_kv_heads)
-    _holds(shape, **need)
+    i4, act, pairs = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4, shape.rows * shape.n_kv_heads
+    most = 0 if blocks is None else blocks.numel() // (pairs or 1)
+    if not (_fits((q, act), (cache, 0), (kv_len, i4), (enable, i4), (out, act), (err, i4), (workspace, 0))
+            and (blocks is None or _fits((blocks, 4 * pairs * most))) and (count is None or _fits((count, 4 * pairs)))):
+        _refuse(q=(q, act), cache=(cache, 0), kv_len=(kv_len, i4), enable=(enable, i4), out=(out, act), err=(err, i4),
+                workspace=(workspace, 0), blocks=(err if blocks is None else blocks, 0 if blocks is None else 4 * pairs * most),
+                count=(err if count is None else count, 0 if count is None else 4 * pairs))
     _check(load_library().ham_op_kv8_attention(
-        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), _nbytes(cache), kv_len.data_ptr(), enable.data_ptr(), kv_max,
-        _ptr(blocks), _ptr(count), most, out.data_ptr(), err.data_ptr(), workspace.data_ptr(), _nbytes(workspace), stream))
+        ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
+        None if blocks is None else blocks.data_ptr(), None if count is None else count.data_ptr(), most, out.data_ptr(),
+        err.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream))
 
 
 def ham_steps_done(model: int) -> int:
