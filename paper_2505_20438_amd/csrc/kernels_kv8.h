@@ -61,7 +61,7 @@ struct Kv8SelectArgs {
 };
 struct Kv8AttnArgs {
   Kv8Cache c;
-  int R, H, Hk, kv_max, nsplit;
+  int R, H, Hk, grp, kv_max, nsplit; // grp = H / Hk
   const void* q; void* out;          // act rows
   const int* kv_len; const int* enable;
   const int* blocks; const int* n_blocks; int max_blocks;  // listed blocks, or null: all

@@ -58,6 +58,32 @@ template <typename T> __device__ __forceinline__ f4 get_act4(const void* base, s
   return v;
 }
 
+// N values of the storage type as they lie in memory: a load without a conversion, which would wait for it
+template <typename T, int N>
+struct Raw {
+  static constexpr int W = N * (int)sizeof(T) / 4;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (W % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const u4 v = ld16((const uint32_t*)p + 4 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
+      }
+    } else {
+      static_assert(W == 2, "8 bytes");
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x;
+      w[1] = v.y;
+    }
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+};
+
 // Rotate-half RoPE of the pair (x, y): products and sums are rounded one by one (no fused multiply-add), so that what is
 // rounded to 8 bits next does not depend on how the compiler contracts.
 __device__ __forceinline__ void rotate(f4& x, f4& y, f4 c, f4 s) {
@@ -480,24 +506,58 @@ struct CodeBlock {  // a block in registers: 16 bytes a lane of each 1 KB piece
   u4 k[2][HD / 64], v[HD / 32];
   float ks, vs;
 };
+// Range-checked loads, so that a loop of them has no branches (blk < 0: nothing is read, the block is zeros): the compiler
+// then waits for the block that it needs and not for those behind it.
 template <int HD>
 __device__ __forceinline__ void load_block(CodeBlock<HD>& x, const uint8_t* codes, const float* scales, int blk) {
-  const uint8_t* p = codes + (size_t)blk * (2 * KV8_BLOCK * HD) + (threadIdx.x & 63) * 16;
+  const int at = max(blk, 0);
+  const BufRsrc rs = buf_rsrc(codes + (size_t)at * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
+  const uint32_t p = (threadIdx.x & 63) * 16;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < HD / 64; ++i) x.k[t][i] = ld16_stream(p + (t * (HD / 64) + i) * 1024);
+    for (int i = 0; i < HD / 64; ++i) x.k[t][i] = buf_u4_stream(rs, p + (t * (HD / 64) + i) * 1024);
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) x.v[i] = ld16_stream(p + KV8_BLOCK * HD + i * 1024);
-  x.ks = scales[2 * (size_t)blk];
-  x.vs = scales[2 * (size_t)blk + 1];
+  for (int i = 0; i < HD / 32; ++i) x.v[i] = buf_u4_stream(rs, p + KV8_BLOCK * HD + i * 1024);
+  x.ks = scales[2 * (size_t)at];
+  x.vs = scales[2 * (size_t)at + 1];
+  __builtin_amdgcn_sched_barrier(0);  // a block's loads stay together: the wait for one must not cover the next
+}
+
+// the greater of v in the four lane groups, in every lane (lanes 16 and 32 apart swapped on the vector units)
+__device__ __forceinline__ float group_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float group_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// the sum and the maximum over the 16 lanes of a row, in each of them
+template <int ROR> __device__ __forceinline__ float row_ror(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + ROR, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += row_ror<8>(v);
+  v += row_ror<4>(v);
+  v += row_ror<2>(v);
+  return v + row_ror<1>(v);
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, row_ror<8>(v));
+  v = fmaxf(v, row_ror<4>(v));
+  v = fmaxf(v, row_ror<2>(v));
+  return fmaxf(v, row_ror<1>(v));
 }
 
 // Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
-// and P V.  `scale` is log2(e) / sqrt(hd).
+// and P V.  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this lane's slots alone.
 template <int HD, int N>
 __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*q)[N], float scale, float& m, float& l, f4* o) {
-  const int g = (threadIdx.x & 63) >> 4;
   float sc[8];
   const float c = x.ks * scale;
 #pragma unroll
@@ -517,21 +577,11 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
   float top = sc[0];
 #pragma unroll
   for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
-  top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-  top = fmaxf(top, __shfl_xor(top, 32, WAVE));
-  const float mnew = fmaxf(m, top), mz = mnew == -INFINITY ? 0.f : mnew;  // scores of -inf alone: all weights 0
-  float p[8], ps = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(sc[e] - mz);
-    ps += p[e];
-    p[e] *= x.vs;
-  }
-  ps += __shfl_xor(ps, 16, WAVE);
-  ps += __shfl_xor(ps, 32, WAVE);
-  if (__any(mnew != m)) {  // a maximum rarely moves once a row has seen many keys
-    const float alpha = __builtin_amdgcn_exp2f(m - mz);
+  if (__any(top > m)) {  // rarely, once a row has seen many keys
+    const float mnew = fmaxf(m, group_max(top));
+    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
     l *= alpha;
+    const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float ai = __shfl(alpha, 4 * g + i, WAVE);
@@ -540,7 +590,14 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
     }
     m = mnew;
   }
-  l += ps;
+  const float mz = m == -INFINITY ? 0.f : m;  // scores of -inf alone: all weights 0
+  float p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(sc[e] - mz);
+    l += p[e];
+    p[e] *= x.vs;
+  }
   u4 pp[N];
   to_planes<N>(p, pp);
 #pragma unroll
@@ -553,111 +610,200 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
     }
 }
 
-constexpr int ATT_NW = 8;
+constexpr int ATT_NW = 8, ATT_THREADS = 64 * ATT_NW;
+template <int HD> struct AttDepth { static constexpr int NB = HD == 64 ? 4 : 3; };  // blocks of a wave under way
 template <int HD, int GR>
 struct AttLds {
   float o[ATT_NW][GR][HD];
   float m[ATT_NW][16], l[ATT_NW][16];
-  float q[GR][HD];                 // the open block's part
-  float v[KV8_BLOCK][HD];
-  float p[GR][KV8_BLOCK];
-  float tm[GR], tl[GR];
+  float q[GR][HD], v[KV8_BLOCK][HD], p[GR][KV8_BLOCK];  // queries, values and weights of the open block
+  float tm[GR], tl[GR];                                 // its maxima and sums
 };
 
-// One workgroup per (split, kv head, row); its waves take every eighth block of the split's share.  Split 0 attends over
-// the open block too, in fp32 on the vector units (at most 31 slots).
-template <typename T, int HD, int GR>
-__global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
+// One workgroup per (split, kv head, row).  Wave w of split s takes the blocks (or list entries) 8 s + w, 8 (s + nsplit) +
+// w, ...: which block is first depends on nothing in memory, so its loads are under way before the row's length is known
+// (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split 0 attends over
+// the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
+template <typename T, int HD, int GR, bool LIST>
+__global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, CPL = HD / 16;  // channels a lane of the open block
+  constexpr int NB = AttDepth<HD>::NB, PL = Act<T>::PL;
+  constexpr int OUT = (GR * HD + ATT_THREADS - 1) / ATT_THREADS;                              // outputs of a thread
   __shared__ AttLds<HD, GR> sh;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r16 = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.grp;
   const size_t pair = (size_t)r * a.Hk + kvh;
-  int n = a.kv_len[r];
+  const int first = split * ATT_NW + w, stride = a.nsplit * ATT_NW;
+  const uint8_t* codes = a.c.codes + pair * a.c.NB * (2 * B * HD);
+  const float* scales = a.c.scales + pair * a.c.NB * 2;
+  const int* list = LIST ? a.blocks + pair * a.max_blocks : nullptr;
+  int blk = -1, before = -1;  // this lane's list entry and the one before it
+  if constexpr (LIST) {
+    const int e = first + lane * stride;
+    if (e < a.max_blocks) {
+      blk = list[e];
+      if (e > 0) before = list[e - 1];
+    }
+  }
+  int n = a.kv_len[r], cnt = LIST ? a.n_blocks[pair] : 0;
+  const int on = a.enable[r];
+  // this thread's share of the open block: slot ts, channels tc ..
+  const int ts = tid / 16, tc = tid % 16 * CPL;
+  static_assert(GR * HD / 4 <= ATT_THREADS, "four query channels a thread");
+  Raw<T, CPL> tk, tv;
+  Raw<T, 4> tq[PL];
+  const T* qrow = (const T*)a.q + (size_t)r * PL * a.H * HD + kvh * grp * HD;  // hi plane of the kv head's q-heads
+  if (split == 0) {
+    const T* op = (const T*)a.c.open + pair * 2 * B * HD + ts * HD + tc;
+    tk.load(op);
+    tv.load(op + B * HD);
+    if (tid * 4 < grp * HD) {
+#pragma unroll
+      for (int i = 0; i < PL; ++i) tq[i].load(qrow + i * a.H * HD + tid * 4);
+    }
+  }
+  // query fragments, channels in the order of the K codes: fragment 2 i + h holds 64 i + 16 g + 8 h ..; rows past the q-heads
+  // of the kv head are out of the buffer's range, which loads zeros
+  constexpr int QW = (int)sizeof(T) / 2;  // 16-byte loads of 8 channels
+  const BufRsrc qs = buf_rsrc(qrow, ((PL - 1) * a.H + grp) * HD * (int)sizeof(T));
+  const uint32_t qo = r16 < grp ? (r16 * HD + 16 * g) * (uint32_t)sizeof(T) : BUF_FAR;
+  u4 raw[NF][PL * QW];
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+#pragma unroll
+      for (int j = 0; j < QW; ++j)
+        raw[f][i * QW + j] = buf_u4(qs, qo + (uint32_t)(i * a.H * HD + 64 * (f / 2) + 8 * (f % 2)) * (uint32_t)sizeof(T) + 16 * j);
+  CodeBlock<HD> x[NB];
+  if constexpr (!LIST) {
+    const int bound = a.kv_max / B;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, first + b * stride < bound ? first + b * stride : -1);
+  }
   if (n < 0 || n > a.kv_max) {
     if (split == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
     n = 0;
   }
-  if (!a.enable[r]) n = 0;
-  const int closed = n / B, rest = n % B;
-  int cnt = closed;
-  const int* list = nullptr;
-  if (a.blocks && n > 0) {
-    list = a.blocks + pair * a.max_blocks;
-    cnt = a.n_blocks[pair];
-    if (cnt < 0 || cnt > a.max_blocks) {
-      if (split == 0 && tid == 0) atomicOr(a.err + r, 16);
-      cnt = 0;
-    }
+  if (!on) n = 0;
+  const int closed = n / B, rest = split == 0 ? n % B : 0;
+  if (!LIST || n == 0) {
+    cnt = closed;
+  } else if (cnt < 0 || cnt > a.max_blocks) {
+    if (split == 0 && tid == 0) atomicOr(a.err + r, 16);
+    cnt = 0;
   }
-  const int per = (cnt + a.nsplit - 1) / a.nsplit, e0 = min(cnt, split * per), e1 = min(cnt, e0 + per);
-  const bool tail = split == 0 && rest > 0;
-  // this thread's share of the open block: slot ts, channels tc ..
-  const int ts = tid / 16, tc = tid % 16 * CPL;
-  f4 tk[CPL / 4], tv[CPL / 4];
-  if (tail && ts < rest) {
-    const T* op = (const T*)a.c.open + pair * 2 * B * HD + ts * HD + tc;
+  int mine = 0;  // list entries among the wave's next 64
+  const auto check_entries = [&](int e0) {  // an entry that is not ascending or out of range is left out
+    const bool there = e0 + lane * stride < cnt;
+    mine = __popcll(__ballot(there));
+    if (there && (blk < 0 || blk <= before || blk >= closed)) {
+      atomicOr(a.err + r, 16);
+      blk = -1;
+    }
+  };
+  if constexpr (LIST) {
+    check_entries(first);
 #pragma unroll
-    for (int i = 0; i < CPL / 4; ++i) {
-      tk[i] = ld4<T>(op + 4 * i);
-      tv[i] = ld4<T>(op + B * HD + 4 * i);
+    for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, b < mine ? __builtin_amdgcn_readlane(blk, b) : -1);
+  }
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  float tx[OUT];  // the open block's part of this thread's outputs
+  if (rest > 0) {
+    if (tid * 4 < grp * HD) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) (&sh.q[0][0])[tid * 4 + e] = PL == 1 ? tq[0].at(e) : tq[0].at(e) + tq[PL - 1].at(e);
+    }
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) sh.v[ts][tc + e] = ts < rest ? tv.at(e) : 0.f;  // what lies past the row's end may be NaN
+    lds_barrier();
+    for (int j = 0; j < grp; ++j) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) s += sh.q[j][tc + e] * tk.at(e);
+      s = row_sum(s);
+      if (tid % 16 == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
+    }
+    lds_barrier();
+    for (int j = w; j < grp; j += ATT_NW) {  // weights, 32 slots twice in a wave
+      const float s = sh.p[j][lane % B];
+      const float top = group_max(row_max(s)), mz = top == -INFINITY ? 0.f : top;
+      const float p = __builtin_amdgcn_exp2f(s - mz);
+      const float sum = group_sum(row_sum(p)) * 0.5f;
+      if (lane < B) sh.p[j][lane] = p;
+      if (lane == 0) {
+        sh.tm[j] = top;
+        sh.tl[j] = sum;
+      }
+    }
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < OUT; ++k) {
+      const int t = tid + k * ATT_THREADS, j = t / HD, d = t % HD;
+      tx[k] = 0.f;
+      if (j >= grp) break;
+#pragma unroll 4
+      for (int i = 0; i < B; i += 4) {
+        const f4 p = *reinterpret_cast<const f4*>(&sh.p[j][i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tx[k] += p[e] * sh.v[i + e][d];
+      }
     }
   }
-  if (tail)
-    for (int i = tid * 4; i < grp * HD; i += 64 * ATT_NW * 4)
-      *reinterpret_cast<f4*>(&sh.q[i / HD][i % HD]) = get_act4<T>(a.q, r, a.H * HD, kvh * grp * HD + i);
-  // query fragments, channels in the order of the K codes: fragment 2 i + h holds 64 i + 16 g + 8 h ..
   u4 q[NF][N];
 #pragma unroll
   for (int f = 0; f < NF; ++f) {
-    const int d = 64 * (f / 2) + 16 * g + 8 * (f % 2);
-    if (r16 < grp) {
-      const T* p = (const T*)a.q + (size_t)r * Act<T>::PL * a.H * HD + (size_t)(kvh * grp + r16) * HD + d;
-      if constexpr (Act<T>::SPLIT) {
-        q[f][0] = ld16(p);
-        q[f][1] = ld16(p + a.H * HD);
-      } else {
-        float v[8];
+    if constexpr (Act<T>::SPLIT) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = p[e];
-        to_planes<N>(v, q[f]);
-      }
+      for (int i = 0; i < N; ++i) q[f][i] = raw[f][i];
     } else {
+      float v[8];
 #pragma unroll
-      for (int i = 0; i < N; ++i) q[f][i] = zero16();
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(raw[f][e / 4][e % 4]);
+      to_planes<N>(v, q[f]);
     }
+    // waited for here and not, with every block under way, in the loop
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(q[f][i]));
   }
-  const float scale = 1.4426950408889634f / sqrtf((float)HD);
   f4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  const uint8_t* codes = a.c.codes + pair * a.c.NB * (2 * B * HD);
-  const float* scales = a.c.scales + pair * a.c.NB * 2;
-  for (int c0 = e0 + w; c0 < e1; c0 += ATT_NW * 64) {  // 64 of the wave's blocks at a time
-    const int mine = min(64, (e1 - c0 + ATT_NW - 1) / ATT_NW);
-    int blk = c0 + lane * ATT_NW;
-    if (list && lane < mine) {
-      const int e = blk, before = e > 0 ? list[e - 1] : -1;
-      blk = list[e];
-      if (blk < 0 || blk <= before || blk >= closed) {  // not ascending or out of range: left out
-        atomicOr(a.err + r, 16);
-        blk = -1;
+  if constexpr (!LIST) {
+    for (int e = first; e < cnt; e += NB * stride) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (e + b * stride < cnt) attend_block<HD, N>(x[b], q, scale, m, l, o);
+        const int next = e + (b + NB) * stride;
+        load_block<HD>(x[b], codes, scales, next < cnt ? next : -1);
       }
     }
-    CodeBlock<HD> x0, x1;
-    int i0 = __builtin_amdgcn_readlane(blk, 0), i1 = -1;
-    if (i0 >= 0) load_block<HD>(x0, codes, scales, i0);
-    for (int j = 0; j < mine; j += 2) {
-      i1 = j + 1 < mine ? __builtin_amdgcn_readlane(blk, j + 1) : -1;
-      if (i1 >= 0) load_block<HD>(x1, codes, scales, i1);
-      if (i0 >= 0) attend_block<HD, N>(x0, q, scale, m, l, o);
-      i0 = j + 2 < mine ? __builtin_amdgcn_readlane(blk, j + 2) : -1;
-      if (i0 >= 0) load_block<HD>(x0, codes, scales, i0);
-      if (i1 >= 0) attend_block<HD, N>(x1, q, scale, m, l, o);
+  } else {
+    for (int e0 = first; e0 < cnt; e0 += 64 * stride) {  // 64 of the wave's entries at a time: one a lane
+      const auto index = [&](int j) { return j < mine ? __builtin_amdgcn_readlane(blk, j) : -1; };
+      if (e0 > first) {
+        const int e = e0 + lane * stride;
+        blk = -1;
+        if (e < cnt) {
+          blk = list[e];
+          before = list[e - 1];
+        }
+        check_entries(e0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, index(b));
+      }
+      for (int j = 0; j < mine; j += NB) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if (index(j + b) >= 0) attend_block<HD, N>(x[b], q, scale, m, l, o);
+          load_block<HD>(x[b], codes, scales, index(j + b + NB));
+        }
+      }
     }
   }
   // per wave: maximum, sum and unnormalised outputs
+  l = group_sum(l);
   if (g == 0) {
     sh.m[w][r16] = m;
     sh.l[w][r16] = l;
@@ -670,43 +816,12 @@ __global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
       for (int d = 0; d < ND; ++d) sh.o[w][j][d * 16 + r16] = o[d][i];
     }
   }
-  __syncthreads();
-  if (tail) {
-    if (ts < rest) {
+  lds_barrier();
 #pragma unroll
-      for (int i = 0; i < CPL / 4; ++i) *reinterpret_cast<f4*>(&sh.v[ts][tc + 4 * i]) = tv[i];
-    }
-    for (int j = 0; j < grp; ++j) {
-      float s = 0.f;
-      if (ts < rest) {
-#pragma unroll
-        for (int i = 0; i < CPL / 4; ++i) {
-          const f4 qv = *reinterpret_cast<const f4*>(&sh.q[j][tc + 4 * i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s += qv[e] * tk[i][e];
-        }
-      }
-#pragma unroll
-      for (int b = 1; b < 16; b <<= 1) s += __shfl_xor(s, b, WAVE);
-      if (tid % 16 == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
-    }
-    __syncthreads();
-    for (int j = w; j < grp; j += ATT_NW) {
-      const float s = lane < B ? sh.p[j][lane] : -INFINITY;
-      const float top = wave_max(s), mz = top == -INFINITY ? 0.f : top;
-      const float p = lane < rest ? __builtin_amdgcn_exp2f(s - mz) : 0.f;
-      const float sum = wave_sum(p);
-      if (lane < B) sh.p[j][lane] = p;
-      if (lane == 0) {
-        sh.tm[j] = top;
-        sh.tl[j] = sum;
-      }
-    }
-    __syncthreads();
-  }
-  for (int t = tid; t < grp * HD; t += 64 * ATT_NW) {
-    const int j = t / HD, d = t % HD;
-    float M = tail ? sh.tm[j] : -INFINITY;
+  for (int k = 0; k < OUT; ++k) {
+    const int t = tid + k * ATT_THREADS, j = t / HD, d = t % HD;
+    if (j >= grp) break;
+    float M = rest > 0 ? sh.tm[j] : -INFINITY;
 #pragma unroll
     for (int i = 0; i < ATT_NW; ++i) M = fmaxf(M, sh.m[i][j]);
     const float mz = M == -INFINITY ? 0.f : M;
@@ -718,12 +833,10 @@ __global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
       L += e * sh.l[i][j];
       O += e * sh.o[i][j][d];
     }
-    if (tail) {
+    if (rest > 0) {
       const float e = __builtin_amdgcn_exp2f(sh.tm[j] - mz);
-      float x = 0.f;
-      for (int s = 0; s < rest; ++s) x += sh.p[j][s] * sh.v[s][d];
       L += e * sh.tl[j];
-      O += e * x;
+      O += e * tx[k];
     }
     if (a.nsplit == 1) {
       Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L == 0.f ? 0.f : O / L);
@@ -731,7 +844,7 @@ __global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
       const size_t rec = (pair * a.nsplit + split) * grp + j;
       a.part[rec * HD + d] = O;
       if (d == 0) {
-        float* ml = a.part + (size_t)a.R * a.Hk * a.nsplit * grp * HD + 2 * rec;
+        float* ml = a.part + (size_t)a.R * a.H * a.nsplit * HD + 2 * rec;
         ml[0] = M;
         ml[1] = L;
       }
@@ -739,39 +852,48 @@ __global__ __launch_bounds__(64 * ATT_NW) void k_kv8_attn(Kv8AttnArgs a) {
   }
 }
 
-// Log-sum-exp combine of the splits of one (row, q-head), in split order.
+// Log-sum-exp combine of the splits of one (row, q-head), in split order.  The outputs are on their way while the weights
+// are formed: one round trip to memory, which with the launch is most of its time.
 constexpr int COMB_THREADS = 256;
 template <typename T, int HD>
 __global__ __launch_bounds__(COMB_THREADS) void k_kv8_combine(Kv8AttnArgs a) {
-  constexpr int G = COMB_THREADS / HD;
+  constexpr int G = COMB_THREADS / HD, UN = 8;
   __shared__ float wts[64];
   __shared__ float acc[COMB_THREADS];
-  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, ns = a.nsplit;
-  const int grp = a.H / a.Hk, kvh = h / grp, j = h % grp;
+  const int j = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, tid = threadIdx.x, lane = tid & 63, ns = a.nsplit, grp = a.grp;
   const size_t rec0 = ((size_t)r * a.Hk + kvh) * ns * grp + j;  // record of split s: rec0 + s * grp
+  const int d = tid % HD, sg = tid / HD;
+  float v[UN];
+#pragma unroll
+  for (int u = 0; u < UN; ++u) {
+    const int s = sg + u * G;
+    v[u] = s < ns ? a.part[(rec0 + (size_t)s * grp) * HD + d] : 0.f;
+  }
   if (tid < 64) {
     float ms = -INFINITY, ls = 0.f;
     if (lane < ns) {
-      const float* ml = a.part + (size_t)a.R * a.Hk * ns * grp * HD + 2 * (rec0 + (size_t)lane * grp);
+      const float* ml = a.part + (size_t)a.R * a.H * ns * HD + 2 * (rec0 + (size_t)lane * grp);
       ms = ml[0];
       ls = ml[1];
     }
-    const float M = wave_max(ms), mz = M == -INFINITY ? 0.f : M;
+    const float M = group_max(row_max(ms)), mz = M == -INFINITY ? 0.f : M;
     const float e = __builtin_amdgcn_exp2f(ms - mz);
-    const float L = wave_sum(e * ls);
+    const float L = group_sum(row_sum(e * ls));
     wts[lane] = L == 0.f ? 0.f : e / L;
   }
-  __syncthreads();
-  const int d = tid % HD, sg = tid / HD;
+  lds_barrier();
   float o = 0.f;
-  for (int s = sg; s < ns; s += G) o += wts[s] * a.part[(rec0 + (size_t)s * grp) * HD + d];
+#pragma unroll
+  for (int u = 0; u < UN; ++u)
+    if (sg + u * G < ns) o += wts[sg + u * G] * v[u];
+  for (int s = sg + UN * G; s < ns; s += G) o += wts[s] * a.part[(rec0 + (size_t)s * grp) * HD + d];
   acc[tid] = o;
-  __syncthreads();
+  lds_barrier();
   if (tid < HD) {
     float x = acc[tid];
 #pragma unroll
     for (int i = 1; i < G; ++i) x += acc[i * HD + tid];
-    Act<T>::put(a.out, r, a.H * HD, h * HD + tid, x);
+    Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + tid, x);
   }
 }
 
@@ -796,10 +918,11 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
 }
 template <typename T, int HD>
 int attention_t(const Kv8AttnArgs& a, Stream s) {
-  const dim3 grid(a.nsplit, a.Hk, a.R), block(64 * ATT_NW);
-  if (a.H / a.Hk <= 4) launch_k((k_kv8_attn<T, HD, 4>), grid, block, 0, s, a);
-  else launch_k((k_kv8_attn<T, HD, 16>), grid, block, 0, s, a);
-  if (a.nsplit > 1) launch_k((k_kv8_combine<T, HD>), dim3(a.R, a.H), dim3(COMB_THREADS), 0, s, a);
+  const dim3 grid(a.nsplit, a.Hk, a.R), block(ATT_THREADS);
+  const bool few = a.grp <= 4;
+  if (a.blocks) launch_k(few ? k_kv8_attn<T, HD, 4, true> : k_kv8_attn<T, HD, 16, true>, grid, block, 0, s, a);
+  else launch_k(few ? k_kv8_attn<T, HD, 4, false> : k_kv8_attn<T, HD, 16, false>, grid, block, 0, s, a);
+  if (a.nsplit > 1) launch_k((k_kv8_combine<T, HD>), dim3(a.grp, a.Hk, a.R), dim3(COMB_THREADS), 0, s, a);
   return 0;
 }
 

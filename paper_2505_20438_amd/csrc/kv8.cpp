@@ -167,7 +167,7 @@ int ham_op_kv8_attention(const ham_kv8_shape* p, const void* d_q, const void* d_
   if (workspace_bytes < need) return fail(HAM_ENOMEM, "the workspace needs %zu bytes", need);
   Kv8AttnArgs a{};
   a.c = cache_of(p, d_cache);
-  a.R = p->rows; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.kv_max = kv_max;
+  a.R = p->rows; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.grp = p->n_heads / p->n_kv_heads; a.kv_max = kv_max;
   a.q = d_q; a.out = d_out; a.kv_len = d_kv_len; a.enable = d_enable;
   a.blocks = d_blocks; a.n_blocks = d_n_blocks; a.max_blocks = d_blocks ? max_blocks : 0; a.err = d_err;
   a.part = (float*)d_workspace;
