@@ -71,8 +71,10 @@ struct Raw {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
       }
+    } else if constexpr (W == 1) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-      static_assert(W == 2, "8 bytes");
+      static_assert(W == 2, "4, 8 or a multiple of 16 bytes");
       const uint2 v = *reinterpret_cast<const uint2*>(p);
       w[0] = v.x;
       w[1] = v.y;
@@ -501,28 +503,31 @@ __device__ __forceinline__ u4 codes_bf16(uint32_t a, uint32_t b) {
             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true))};
 }
 
+// A block in registers: 16 bytes a lane of each 1 KB piece.  Range-checked loads, so that a loop of them has no branches
+// (blk < 0: nothing is read, the block is zeros): the compiler then waits for the half that it needs and not for what is
+// behind it.  The next block's K is loaded as soon as this one's is used up, its V likewise: half a block is always on its
+// way, with one set of registers and one copy of the code (a call's first pass fetches every instruction from memory).
 template <int HD>
-struct CodeBlock {  // a block in registers: 16 bytes a lane of each 1 KB piece
+struct CodeBlock {
   u4 k[2][HD / 64], v[HD / 32];
   float ks, vs;
+  __device__ __forceinline__ void load_k(const uint8_t* codes, const float* scales, int blk) {
+    const BufRsrc rs = buf_rsrc(codes + (size_t)max(blk, 0) * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
+    ks = scales[2 * (size_t)max(blk, 0)];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < HD / 64; ++i) k[t][i] = buf_u4_stream(rs, (threadIdx.x & 63) * 16 + (t * (HD / 64) + i) * 1024);
+    __builtin_amdgcn_sched_barrier(0);  // the loads stay in this order: the wait for K must not cover V
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* codes, const float* scales, int blk) {
+    const BufRsrc rs = buf_rsrc(codes + (size_t)max(blk, 0) * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
+    vs = scales[2 * (size_t)max(blk, 0) + 1];
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) v[i] = buf_u4_stream(rs, (threadIdx.x & 63) * 16 + KV8_BLOCK * HD + i * 1024);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 };
-// Range-checked loads, so that a loop of them has no branches (blk < 0: nothing is read, the block is zeros): the compiler
-// then waits for the block that it needs and not for those behind it.
-template <int HD>
-__device__ __forceinline__ void load_block(CodeBlock<HD>& x, const uint8_t* codes, const float* scales, int blk) {
-  const int at = max(blk, 0);
-  const BufRsrc rs = buf_rsrc(codes + (size_t)at * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
-  const uint32_t p = (threadIdx.x & 63) * 16;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < HD / 64; ++i) x.k[t][i] = buf_u4_stream(rs, p + (t * (HD / 64) + i) * 1024);
-#pragma unroll
-  for (int i = 0; i < HD / 32; ++i) x.v[i] = buf_u4_stream(rs, p + KV8_BLOCK * HD + i * 1024);
-  x.ks = scales[2 * (size_t)at];
-  x.vs = scales[2 * (size_t)at + 1];
-  __builtin_amdgcn_sched_barrier(0);  // a block's loads stay together: the wait for one must not cover the next
-}
 
 // the greater of v in the four lane groups, in every lane (lanes 16 and 32 apart swapped on the vector units)
 __device__ __forceinline__ float group_max(float v) {
@@ -555,11 +560,13 @@ __device__ __forceinline__ float row_max(float v) {
 }
 
 // Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
-// and P V.  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this lane's slots alone.
-template <int HD, int N>
-__device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*q)[N], float scale, float& m, float& l, f4* o) {
+// and P V; then x holds block `next`.  q: fragments in LDS (registers would not do for four waves a SIMD).  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this
+// lane's slots alone.  LIST: a block that is not `there` (zeros) counts for nothing.
+template <int HD, int N, bool LIST>
+__device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64], float scale, float& m, float& l, f4* o,
+                                             const uint8_t* codes, const float* scales, int next, bool there) {
   float sc[8];
-  const float c = x.ks * scale;
+  const float c = LIST && !there ? 0.f : x.ks * scale, none = LIST && !there ? -INFINITY : 0.f;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     f4 s = f4{0.f, 0.f, 0.f, 0.f};
@@ -569,11 +576,12 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
       for (int h = 0; h < 2; ++h) {
         const u4 k = codes_bf16(x.k[t][i][2 * h], x.k[t][i][2 * h + 1]);
 #pragma unroll
-        for (int n = 0; n < N; ++n) Frag<bf16>::mma(s, k, q[2 * i + h][n]);
+        for (int n = 0; n < N; ++n) Frag<bf16>::mma(s, k, q[(2 * i + h) * N + n][threadIdx.x & 63]);
       }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sc[4 * t + e] = s[e] * c;
+    for (int e = 0; e < 4; ++e) sc[4 * t + e] = LIST ? s[e] * c + none : s[e] * c;
   }
+  x.load_k(codes, scales, next);
   float top = sc[0];
 #pragma unroll
   for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
@@ -592,11 +600,12 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
   }
   const float mz = m == -INFINITY ? 0.f : m;  // scores of -inf alone: all weights 0
   float p[8];
+  const float vs = LIST && !there ? 0.f : x.vs;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     p[e] = __builtin_amdgcn_exp2f(sc[e] - mz);
     l += p[e];
-    p[e] *= x.vs;
+    p[e] *= vs;
   }
   u4 pp[N];
   to_planes<N>(p, pp);
@@ -608,32 +617,38 @@ __device__ __forceinline__ void attend_block(const CodeBlock<HD>& x, const u4 (*
 #pragma unroll
       for (int n = 0; n < N; ++n) Frag<bf16>::mma(o[2 * i + h], pp[n], v);
     }
+  x.load_v(codes, scales, next);
 }
 
-constexpr int ATT_NW = 8, ATT_THREADS = 64 * ATT_NW;
-template <int HD> struct AttDepth { static constexpr int NB = HD == 64 ? 4 : 3; };  // blocks of a wave under way
-template <int HD, int GR>
+// Waves of a workgroup: four a SIMD with 128 registers each; the fp32 models' three planes take more, so two.
+template <typename T> constexpr int ATT_WAVES = Act<T>::SPLIT ? 16 : 8;
+template <int HD, int GR, int N, int NW>
 struct AttLds {
-  float o[ATT_NW][GR][HD];
-  float m[ATT_NW][16], l[ATT_NW][16];
-  float q[GR][HD], v[KV8_BLOCK][HD], p[GR][KV8_BLOCK];  // queries, values and weights of the open block
-  float tm[GR], tl[GR];                                 // its maxima and sums
+  static constexpr int PUB = GR == 16 ? 8 : NW;  // waves that publish their outputs at a time (64 KB)
+  u4 qf[HD / 32 * N][64];                      // query fragments, channels in the order of the K codes
+  union {
+    float o[PUB][GR][HD];
+    float q[GR][HD];                           // queries for the open block, done with before the main loop ends
+  };
+  float m[NW][16], l[NW][16];
+  float v[KV8_BLOCK][HD], p[GR][KV8_BLOCK];    // values and weights of the open block
+  float tm[GR], tl[GR];                        // its maxima and sums
 };
 
-// One workgroup per (split, kv head, row).  Wave w of split s takes the blocks (or list entries) 8 s + w, 8 (s + nsplit) +
-// w, ...: which block is first depends on nothing in memory, so its loads are under way before the row's length is known
+// One workgroup per (split, kv head, row).  Wave w of NW of split s takes the blocks (or list entries) NW s + w, NW
+// (s + nsplit) + w, ...: which block is first depends on nothing in memory, so its loads are under way before the row's length is known
 // (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split 0 attends over
 // the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
 template <typename T, int HD, int GR, bool LIST>
-__global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
-  constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, CPL = HD / 16;  // channels a lane of the open block
-  constexpr int NB = AttDepth<HD>::NB, PL = Act<T>::PL;
-  constexpr int OUT = (GR * HD + ATT_THREADS - 1) / ATT_THREADS;                              // outputs of a thread
-  __shared__ AttLds<HD, GR> sh;
+__global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
+  constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, PL = Act<T>::PL;
+  constexpr int NW = ATT_WAVES<T>, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;            // open block: lanes of a slot, channels a lane
+  constexpr int OUT = (GR * HD + THREADS - 1) / THREADS;  // outputs of a thread
+  __shared__ AttLds<HD, GR, N, NW> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
   const int split = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.grp;
   const size_t pair = (size_t)r * a.Hk + kvh;
-  const int first = split * ATT_NW + w, stride = a.nsplit * ATT_NW;
+  const int first = split * NW + w, stride = a.nsplit * NW;
   const uint8_t* codes = a.c.codes + pair * a.c.NB * (2 * B * HD);
   const float* scales = a.c.scales + pair * a.c.NB * 2;
   const int* list = LIST ? a.blocks + pair * a.max_blocks : nullptr;
@@ -648,8 +663,8 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
   int n = a.kv_len[r], cnt = LIST ? a.n_blocks[pair] : 0;
   const int on = a.enable[r];
   // this thread's share of the open block: slot ts, channels tc ..
-  const int ts = tid / 16, tc = tid % 16 * CPL;
-  static_assert(GR * HD / 4 <= ATT_THREADS, "four query channels a thread");
+  const int ts = tid / LPS, tc = tid % LPS * CPL;
+  static_assert(GR * HD / 4 <= THREADS, "four query channels a thread");
   Raw<T, CPL> tk, tv;
   Raw<T, 4> tq[PL];
   const T* qrow = (const T*)a.q + (size_t)r * PL * a.H * HD + kvh * grp * HD;  // hi plane of the kv head's q-heads
@@ -662,24 +677,24 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
       for (int i = 0; i < PL; ++i) tq[i].load(qrow + i * a.H * HD + tid * 4);
     }
   }
-  // query fragments, channels in the order of the K codes: fragment 2 i + h holds 64 i + 16 g + 8 h ..; rows past the q-heads
-  // of the kv head are out of the buffer's range, which loads zeros
-  constexpr int QW = (int)sizeof(T) / 2;  // 16-byte loads of 8 channels
-  const BufRsrc qs = buf_rsrc(qrow, ((PL - 1) * a.H + grp) * HD * (int)sizeof(T));
-  const uint32_t qo = r16 < grp ? (r16 * HD + 16 * g) * (uint32_t)sizeof(T) : BUF_FAR;
-  u4 raw[NF][PL * QW];
+  // query fragments: fragment f = 2 i + h holds channels 64 i + 16 g + 8 h ..; one or more a wave.  Rows past the q-heads of
+  // the kv head are out of the buffer's range, which loads zeros.
+  constexpr int QL = (int)sizeof(T) / 2;  // 16-byte loads of 8 channels
+  constexpr int FRAGS = Act<T>::SPLIT ? NF * PL : NF;
+  static_assert(FRAGS <= NW, "a fragment a wave");
+  const int qf = Act<T>::SPLIT ? w / PL : w, plane = Act<T>::SPLIT ? w % PL : 0;
+  u4 raw[QL];
+  if (w < FRAGS) {
+    const BufRsrc qs = buf_rsrc(qrow + (size_t)plane * a.H * HD, grp * HD * (int)sizeof(T));
+    const uint32_t qo = (r16 * HD + 64 * (qf / 2) + 16 * g + 8 * (qf % 2)) * (uint32_t)sizeof(T);
 #pragma unroll
-  for (int f = 0; f < NF; ++f)
-#pragma unroll
-    for (int i = 0; i < PL; ++i)
-#pragma unroll
-      for (int j = 0; j < QW; ++j)
-        raw[f][i * QW + j] = buf_u4(qs, qo + (uint32_t)(i * a.H * HD + 64 * (f / 2) + 8 * (f % 2)) * (uint32_t)sizeof(T) + 16 * j);
-  CodeBlock<HD> x[NB];
+    for (int j = 0; j < QL; ++j) raw[j] = buf_u4(qs, qo + 16 * j);
+  }
+  CodeBlock<HD> x;
   if constexpr (!LIST) {
-    const int bound = a.kv_max / B;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, first + b * stride < bound ? first + b * stride : -1);
+    const int b0 = first < a.kv_max / B ? first : -1;
+    x.load_k(codes, scales, b0);
+    x.load_v(codes, scales, b0);
   }
   if (n < 0 || n > a.kv_max) {
     if (split == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
@@ -704,11 +719,25 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
   };
   if constexpr (LIST) {
     check_entries(first);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, b < mine ? __builtin_amdgcn_readlane(blk, b) : -1);
+    asm volatile("" : "+v"(blk));
+    const int b0 = mine > 0 ? __builtin_amdgcn_readlane(blk, 0) : -1;
+    x.load_k(codes, scales, b0);
+    x.load_v(codes, scales, b0);
   }
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
-  float tx[OUT];  // the open block's part of this thread's outputs
+  if (w < FRAGS) {
+    if constexpr (Act<T>::SPLIT) {
+      sh.qf[w][lane] = raw[0];
+    } else {
+      float v[8];
+      u4 pl[N];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(raw[e / 4][e % 4]);
+      to_planes<N>(v, pl);
+#pragma unroll
+      for (int i = 0; i < N; ++i) sh.qf[w * N + i][lane] = pl[i];
+    }
+  }
   if (rest > 0) {
     if (tid * 4 < grp * HD) {
 #pragma unroll
@@ -716,16 +745,20 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < CPL; ++e) sh.v[ts][tc + e] = ts < rest ? tv.at(e) : 0.f;  // what lies past the row's end may be NaN
-    lds_barrier();
+  }
+  lds_barrier();
+  float tx[OUT];  // the open block's part of this thread's outputs
+  if (rest > 0) {
     for (int j = 0; j < grp; ++j) {
       float s = 0.f;
 #pragma unroll
       for (int e = 0; e < CPL; ++e) s += sh.q[j][tc + e] * tk.at(e);
       s = row_sum(s);
-      if (tid % 16 == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
+      if constexpr (LPS == 32) s += __shfl_xor(s, 16, WAVE);
+      if (tid % LPS == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
     }
     lds_barrier();
-    for (int j = w; j < grp; j += ATT_NW) {  // weights, 32 slots twice in a wave
+    for (int j = w; j < grp; j += NW) {  // weights, 32 slots twice in a wave
       const float s = sh.p[j][lane % B];
       const float top = group_max(row_max(s)), mz = top == -INFINITY ? 0.f : top;
       const float p = __builtin_amdgcn_exp2f(s - mz);
@@ -739,7 +772,7 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
     lds_barrier();
 #pragma unroll
     for (int k = 0; k < OUT; ++k) {
-      const int t = tid + k * ATT_THREADS, j = t / HD, d = t % HD;
+      const int t = tid + k * THREADS, j = t / HD, d = t % HD;
       tx[k] = 0.f;
       if (j >= grp) break;
 #pragma unroll 4
@@ -750,38 +783,15 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
       }
     }
   }
-  u4 q[NF][N];
-#pragma unroll
-  for (int f = 0; f < NF; ++f) {
-    if constexpr (Act<T>::SPLIT) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) q[f][i] = raw[f][i];
-    } else {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(raw[f][e / 4][e % 4]);
-      to_planes<N>(v, q[f]);
-    }
-    // waited for here and not, with every block under way, in the loop
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(q[f][i]));
-  }
   f4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   if constexpr (!LIST) {
-    for (int e = first; e < cnt; e += NB * stride) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if (e + b * stride < cnt) attend_block<HD, N>(x[b], q, scale, m, l, o);
-        const int next = e + (b + NB) * stride;
-        load_block<HD>(x[b], codes, scales, next < cnt ? next : -1);
-      }
-    }
+    for (int e = first; e < cnt; e += stride)
+      attend_block<HD, N, false>(x, sh.qf, scale, m, l, o, codes, scales, e + stride < cnt ? e + stride : -1, true);
   } else {
     for (int e0 = first; e0 < cnt; e0 += 64 * stride) {  // 64 of the wave's entries at a time: one a lane
-      const auto index = [&](int j) { return j < mine ? __builtin_amdgcn_readlane(blk, j) : -1; };
       if (e0 > first) {
         const int e = e0 + lane * stride;
         blk = -1;
@@ -790,63 +800,77 @@ __global__ __launch_bounds__(ATT_THREADS) void k_kv8_attn(Kv8AttnArgs a) {
           before = list[e - 1];
         }
         check_entries(e0);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) load_block<HD>(x[b], codes, scales, index(b));
+        asm volatile("" : "+v"(blk));  // waited for here, not with blocks under way
+        const int b0 = __builtin_amdgcn_readlane(blk, 0);
+        x.load_k(codes, scales, b0);
+        x.load_v(codes, scales, b0);
       }
-      for (int j = 0; j < mine; j += NB) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          if (index(j + b) >= 0) attend_block<HD, N>(x[b], q, scale, m, l, o);
-          load_block<HD>(x[b], codes, scales, index(j + b + NB));
-        }
+      for (int j = 0; j < mine; ++j) {
+        const int next = j + 1 < mine ? __builtin_amdgcn_readlane(blk, j + 1) : -1;
+        attend_block<HD, N, true>(x, sh.qf, scale, m, l, o, codes, scales, next, __builtin_amdgcn_readlane(blk, j) >= 0);
       }
     }
   }
-  // per wave: maximum, sum and unnormalised outputs
+  // per wave: maximum, sum and unnormalised outputs, PUB waves at a time
+  constexpr int PUB = AttLds<HD, GR, N, NW>::PUB;
   l = group_sum(l);
   if (g == 0) {
     sh.m[w][r16] = m;
     sh.l[w][r16] = l;
   }
+  float M[OUT], L[OUT], O[OUT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = 4 * g + i;
-    if (j < grp) {
+  for (int w0 = 0; w0 < NW; w0 += PUB) {
+    if (w0 > 0) lds_barrier();  // the outputs before have been read
+    if (w >= w0 && w < w0 + PUB) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d) sh.o[w][j][d * 16 + r16] = o[d][i];
+      for (int i = 0; i < 4; ++i) {
+        const int j = 4 * g + i;
+        if (j < grp) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) sh.o[w - w0][j][d * 16 + r16] = o[d][i];
+        }
+      }
+    }
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < OUT; ++k) {
+      const int t = tid + k * THREADS, j = t / HD, d = t % HD;
+      if (j >= grp) break;
+      if (w0 == 0) {
+        M[k] = rest > 0 ? sh.tm[j] : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) M[k] = fmaxf(M[k], sh.m[i][j]);
+        L[k] = O[k] = 0.f;
+      }
+      const float mz = M[k] == -INFINITY ? 0.f : M[k];
+#pragma unroll
+      for (int i = 0; i < PUB; ++i) {
+        const float e = __builtin_amdgcn_exp2f(sh.m[w0 + i][j] - mz);  // 0 for a wave without slots
+        // a wave whose scores are all NaN has maximum -inf and sum NaN, which e = 0 keeps
+        L[k] += e * sh.l[w0 + i][j];
+        O[k] += e * sh.o[i][j][d];
+      }
     }
   }
-  lds_barrier();
 #pragma unroll
   for (int k = 0; k < OUT; ++k) {
-    const int t = tid + k * ATT_THREADS, j = t / HD, d = t % HD;
+    const int t = tid + k * THREADS, j = t / HD, d = t % HD;
     if (j >= grp) break;
-    float M = rest > 0 ? sh.tm[j] : -INFINITY;
-#pragma unroll
-    for (int i = 0; i < ATT_NW; ++i) M = fmaxf(M, sh.m[i][j]);
-    const float mz = M == -INFINITY ? 0.f : M;
-    float L = 0.f, O = 0.f;
-#pragma unroll
-    for (int i = 0; i < ATT_NW; ++i) {
-      const float e = __builtin_amdgcn_exp2f(sh.m[i][j] - mz);  // 0 for a wave without slots
-      // a wave whose scores are all NaN has maximum -inf and sum NaN, which e = 0 keeps
-      L += e * sh.l[i][j];
-      O += e * sh.o[i][j][d];
-    }
     if (rest > 0) {
-      const float e = __builtin_amdgcn_exp2f(sh.tm[j] - mz);
-      L += e * sh.tl[j];
-      O += e * tx[k];
+      const float e = __builtin_amdgcn_exp2f(sh.tm[j] - (M[k] == -INFINITY ? 0.f : M[k]));
+      L[k] += e * sh.tl[j];
+      O[k] += e * tx[k];
     }
     if (a.nsplit == 1) {
-      Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L == 0.f ? 0.f : O / L);
+      Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L[k] == 0.f ? 0.f : O[k] / L[k]);
     } else {
       const size_t rec = (pair * a.nsplit + split) * grp + j;
-      a.part[rec * HD + d] = O;
+      a.part[rec * HD + d] = O[k];
       if (d == 0) {
         float* ml = a.part + (size_t)a.R * a.H * a.nsplit * HD + 2 * rec;
-        ml[0] = M;
-        ml[1] = L;
+        ml[0] = M[k];
+        ml[1] = L[k];
       }
     }
   }
@@ -918,7 +942,7 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
 }
 template <typename T, int HD>
 int attention_t(const Kv8AttnArgs& a, Stream s) {
-  const dim3 grid(a.nsplit, a.Hk, a.R), block(ATT_THREADS);
+  const dim3 grid(a.nsplit, a.Hk, a.R), block(64 * ATT_WAVES<T>);
   const bool few = a.grp <= 4;
   if (a.blocks) launch_k(few ? k_kv8_attn<T, HD, 4, true> : k_kv8_attn<T, HD, 16, true>, grid, block, 0, s, a);
   else launch_k(few ? k_kv8_attn<T, HD, 4, false> : k_kv8_attn<T, HD, 16, false>, grid, block, 0, s, a);
