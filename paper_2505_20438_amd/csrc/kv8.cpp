@@ -52,9 +52,10 @@ Kv8Cache cache_of(const ham_kv8_shape* p, const void* d_cache) {
                   p->slots_cap / KV8_BLOCK};
 }
 
-// records of a split launch; a split launch has at most 256 + pairs workgroups
-size_t attn_record_bytes(const ham_kv8_shape* p, int nsplit) {
-  return nsplit > 1 ? (size_t)p->rows * p->n_heads * nsplit * (p->head_dim + 2) * 4 : 0;
+// records of the split launch with the most workgroups (kv8_attn_splits)
+size_t attn_record_bytes(const ham_kv8_shape* p) {
+  const size_t pairs = (size_t)p->rows * p->n_kv_heads;
+  return std::min(std::max<size_t>(KV8_MOST_WGS, 4 * pairs), KV8_MAX_SPLIT * pairs) * (p->n_heads / p->n_kv_heads) * (p->head_dim + 2) * 4;
 }
 
 // what every call checks: the shape, the cache buffer, alignment of the 16-byte accesses
@@ -87,8 +88,7 @@ size_t ham_op_kv8_cache_bytes(const ham_kv8_shape* p) { return check_shape(p) ? 
 size_t ham_op_kv8_workspace_bytes(const ham_kv8_shape* p) {
   if (check_shape(p)) return 0;
   const size_t pairs = (size_t)p->rows * p->n_kv_heads, blocks = p->slots_cap / KV8_BLOCK;
-  const int most = kv8_attn_splits(p->rows, p->n_kv_heads, (int)blocks);  // does not fall with the blocks
-  return al(std::max(attn_record_bytes(p, most), pairs * blocks * 4));
+  return al(std::max(attn_record_bytes(p), pairs * blocks * 4));
 }
 
 int ham_op_kv8_info(const ham_kv8_shape* p, size_t* codes, size_t* scales, size_t* bounds, size_t* open) {
@@ -172,7 +172,7 @@ int ham_op_kv8_attention(const ham_kv8_shape* p, const void* d_q, const void* d_
   a.blocks = d_blocks; a.n_blocks = d_n_blocks; a.max_blocks = d_blocks ? max_blocks : 0; a.err = d_err;
   a.part = (float*)d_workspace;
   const int blocks = d_blocks ? std::min(max_blocks, kv_max / KV8_BLOCK) : kv_max / KV8_BLOCK;
-  a.nsplit = kv8_attn_splits(p->rows, p->n_kv_heads, blocks);
+  a.nsplit = kv8_attn_splits(p->rows, p->n_kv_heads, p->head_dim, blocks);
   return launched(launch_kv8_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
 }
 

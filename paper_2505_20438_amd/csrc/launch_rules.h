@@ -73,11 +73,36 @@ inline PromptAttnGrid prompt_attn_grid(int R, int s0, int T, int H, int Hkv) {
 }
 
 // Splits of the attention over the 8-bit cache for R rows of Hk kv heads of which the longest reads `blocks` blocks of 32
-// slots: workgroups until every CU has one, eight blocks (one a wave) or more each.
-inline int kv8_attn_splits(int R, int Hk, int blocks) {
+// slots.  One workgroup of 16 waves runs per CU.  Its 16 blocks (one a wave) take 2.3 us at head dim 128 and 1.45 at 64
+// alone and half as much again with all 256 CUs at work, but no less than its share of memory: a block of every CU's takes
+// 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk * splits workgroups take ceil(... / 256) rounds, the first 5.4 us and the
+// others 2 beside that, and a split launch 2.5 us more for the combine.  The count with the least estimate, the lowest of
+// equal ones.  8 kv heads of 128, us at the splits here / at 256 / (R * Hk) rounded up: 4 rows x 33,300 slots 45.5 / 47.2,
+// 5 x 33,300 55 / 73, 12 x 4,096 21 / 26, 20 x 4,096 31 / 38, 40 x 4,096 61 / 63 (and 1 x 1,000 10.2 unsplit / 10.7).
+// A row's blocks are shared by its own splits alone, so a long row among short ones is a serial chain (1,040 blocks 155 us
+// unsplit, 47 in four): from 512 blocks on a row gets one split for every 256, up to four; where all rows are long that
+// costs up to a twentieth (32 x 33,300 317 -> 329).
+constexpr int KV8_MOST_WGS = 1024;  // workgroups of a split launch, unless four splits of every pair are more
+inline int kv8_attn_splits(int R, int Hk, int hd, int blocks) {
   const long long pairs = (long long)R * Hk;
-  const long long width = (256 + pairs - 1) / pairs;
-  return (int)std::max(1ll, std::min({width, (long long)(blocks + 7) / 8, (long long)MAX_ATTN_SPLIT}));
+  const int least = std::max(1, std::min(4, blocks / 256));
+  const int most = (int)std::max<long long>(least, std::min<long long>({(blocks + 15) / 16, KV8_MOST_WGS / pairs, MAX_ATTN_SPLIT}));
+  const double wave = hd == 128 ? 2.3 : 1.45, share = hd == 128 ? 0.30 : 0.15;
+  int best = least;
+  double best_t = 1e30;
+  for (int s = least; s <= most; ++s) {
+    const int u = (blocks + s - 1) / s;
+    const double rounds = (double)((pairs * s + 255) / 256), last = (double)(pairs * s) / 256 - (rounds - 1);
+    const auto time = [&](double fill) {
+      return std::max(wave * (1 + 0.55 * fill) * ((u + 15) / 16), share * (0.85 + 0.15 * fill) * u * fill);
+    };
+    const double t = 5.4 + (rounds - 1) * (2 + time(1)) + time(last) + (s > 1 ? 2.5 : 0);
+    if (t < best_t - 1e-9) {
+      best_t = t;
+      best = s;
+    }
+  }
+  return best;
 }
 
 }  // namespace ham

@@ -150,25 +150,32 @@ def splits():
     with tempfile.TemporaryDirectory() as d:
         src, out = os.path.join(d, "r.cpp"), os.path.join(d, "r.so")
         with open(src, "w") as f:
-            f.write('#include "launch_rules.h"\nextern "C" int splits(int R, int Hk, int blocks) '
-                    '{ return ham::kv8_attn_splits(R, Hk, blocks); }\n')
+            f.write('#include "launch_rules.h"\nextern "C" int splits(int R, int Hk, int hd, int blocks) '
+                    '{ return ham::kv8_attn_splits(R, Hk, hd, blocks); }\n')
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc, src, "-o", out], check=True)
         yield ctypes.CDLL(out).splits
 
 
 def test_split_limits(splits):
-    for rows in (1, 2, 3, 7, 16, 33, 64, 500, 4096):
-        for hk in (1, 2, 3, 8, 64, 1024):
-            last = 0
-            for blocks in (0, 1, 7, 8, 9, 15, 16, 17, 64, 80, 100, 1000, 1 << 19):
-                n = splits(rows, hk, blocks)
-                assert 1 <= n <= 64 and n >= last, (rows, hk, blocks)      # the workspace holds the records of the most blocks
-                last = n
+    for hd in (64, 128):
+        for rows in (1, 2, 3, 7, 16, 33, 64, 500, 4096):
+            for hk in (1, 2, 3, 8, 64, 1024):
+                for blocks in (0, 1, 7, 8, 16, 17, 33, 64, 80, 100, 512, 1000, 1 << 19):
+                    n = splits(rows, hk, hd, blocks)
+                    assert 1 <= n <= 64, (rows, hk, blocks)
+                    assert n == 1 or n <= 4 or n * 16 < blocks + 16   # a block for every wave
+                    assert n >= min(4, blocks // 256)               # a long row among short ones
 
 
 def test_workspace_holds_the_records_of_every_length(lib, splits):
-    for rows, H, hk, hd, slots in ((1, 32, 8, 128, 33344), (4, 32, 8, 128, 33344), (32, 32, 8, 64, 2560), (1, 16, 1, 128, 1 << 20)):
+    for rows, H, hk, hd, slots in ((1, 32, 8, 128, 33344), (4, 32, 8, 128, 33344), (32, 32, 8, 64, 2560), (1, 16, 1, 128, 1 << 20),
+                                   (64, 8, 8, 64, 1 << 15), (300, 9, 3, 128, 1 << 16), (4096, 8, 8, 64, 1 << 16)):
         s = ham.kv8_shape(BF16, rows, H, hk, hd, slots)
         for blocks in range(0, slots // 32 + 1, 7):
-            n = splits(rows, hk, blocks)
+            n = splits(rows, hk, hd, blocks)
             assert n == 1 or ham.ham_op_kv8_workspace_bytes(s) >= rows * H * n * (hd + 2) * 4
+
+
+@pytest.mark.parametrize("rows,blocks,n", [(1, 10, 1), (1, 31, 1), (1, 128, 8), (12, 128, 2), (20, 128, 1), (32, 80, 1), (4, 1040, 6), (5, 1040, 5)])
+def test_splits_at_eight_heads_of_128(splits, rows, blocks, n):
+    assert splits(rows, 8, 128, blocks) == n
