@@ -52,7 +52,7 @@ struct Kv8PackArgs {
 };
 struct Kv8SelectArgs {
   Kv8Cache c;
-  int R, H, Hk, kv_max, n, first, last;
+  int R, H, Hk, grp, kv_max, n, first, last;  // grp = H / Hk
   const void* q;                     // act rows
   const int* kv_len; const int* enable;
   int* blocks; int* n_blocks;

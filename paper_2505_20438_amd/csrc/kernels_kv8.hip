@@ -307,95 +307,237 @@ __global__ __launch_bounds__(CODE_THREADS) void k_kv8_pack(Kv8PackArgs a) {
 //   sum_d max(q_d lo_d, q_d hi_d) = sum_d (q_d (lo_d + hi_d) + |q_d| (hi_d - lo_d)) / 2,
 // the greatest over the kv head's q-heads, times the block's scale.  Products of q (24 bits) and codes (4 bits) and their
 // sums are taken in fp64: blocks are compared by these values, and fp32 sums of another order would order near ones
-// differently.  HD / 8 lanes to a block, 8 channels each.
-constexpr int SCORE_THREADS = 256, SCORE_BLOCKS = 64;  // blocks of a workgroup
+// differently.  HD / 8 lanes to a block, 8 channels each; four heads at a time.
+template <int CTRL> __device__ __forceinline__ double dpp64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+constexpr int XOR1 = 0xB1, XOR2 = 0x4E, QUAD_REV = 0x1B, HALF_MIRROR = 0x141, ROR8 = 0x128;  // lanes of a row
+__device__ __forceinline__ double max_nan(double a, double b) { return (b > a || b != b) ? b : a; }  // NaN stays
+
 template <typename T, int HD>
-__global__ __launch_bounds__(SCORE_THREADS) void k_kv8_scores(Kv8SelectArgs a, int nb_max) {
-  constexpr int LPB = HD / 8, BPP = SCORE_THREADS / LPB;  // lanes of a block, blocks of a pass
-  __shared__ double sq[KV8_MAX_GROUP][HD];
-  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk, n = a.kv_len[r];
-  const int b0 = blockIdx.x * SCORE_BLOCKS;
-  if (n < 0 || n > a.kv_max || !a.enable[r]) return;
-  const int closed = n / KV8_BLOCK;
-  if (closed <= a.n || b0 >= closed) return;  // every block is taken
-  for (int i = tid * 4; i < grp * HD; i += SCORE_THREADS * 4) {
-    const f4 x = get_act4<T>(a.q, r, a.H * HD, kvh * grp * HD + i);
+struct BlockScore {
+  double q[4][8];
+  int heads;  // of the four
+  // heads h0 .. of kv head kvh, this lane's channels
+  __device__ __forceinline__ void load(const Kv8SelectArgs& a, int r, int kvh, int h0) {
+    constexpr int PL = Act<T>::PL;
+    heads = min(4, a.grp - h0);
+    Raw<T, 8> raw[4][PL];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sq[i / HD][i % HD + e] = (double)x[e];
+    for (int j = 0; j < 4; ++j) {
+      const T* p = (const T*)a.q + (size_t)r * PL * a.H * HD + (kvh * a.grp + h0 + min(j, heads - 1)) * HD + threadIdx.x % (HD / 8) * 8;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) raw[j][i].load(p + i * a.H * HD);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[j][e] = (double)(PL == 1 ? raw[j][0].at(e) : raw[j][0].at(e) + raw[j][PL - 1].at(e));
   }
-  __syncthreads();
-  const size_t pair = (size_t)r * a.Hk + kvh;
-  const int c = tid % LPB;
-  for (int b = b0 + tid / LPB; b < min(closed, b0 + SCORE_BLOCKS); b += BPP) {
-    const size_t blk = pair * a.c.NB + b;
-    const u4 w = ld16(a.c.bounds + blk * (2 * HD) + c * 16);
-    double sum[8], dif[8];
+  // twice the greatest bound of the heads, w: the lane's 8 least and 8 greatest codes; the same in every lane of the block
+  __device__ __forceinline__ double operator()(u4 w) const {
+    double s[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       const auto lo = p % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[p / 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[p / 2], false);
       const auto hi = p % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[2 + p / 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[2 + p / 2], false);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        sum[2 * p + e] = (double)lo[e] + (double)hi[e];
-        dif[2 * p + e] = (double)hi[e] - (double)lo[e];
+        const double sum = (double)(lo[e] + hi[e]), dif = (double)(hi[e] - lo[e]);  // of two codes, exact in fp32
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[j] = fma(q[j][2 * p + e], sum, s[j]);
+          s[j] = fma(fabs(q[j][2 * p + e]), dif, s[j]);
+        }
       }
     }
-    double best = -INFINITY;
-    for (int j = 0; j < grp; ++j) {
-      double s = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double q = sq[j][c * 8 + e];
-        s = fma(q, sum[e], s);
-        s = fma(fabs(q), dif[e], s);
-      }
-#pragma unroll
-      for (int o = 1; o < LPB; o <<= 1) s += __shfl_xor(s, o, WAVE);
-      best = (s > best || s != s) ? s : best;  // NaN stays
-    }
-    if (c == 0) a.scores[pair * nb_max + b] = (float)(0.5 * best * (double)a.c.scales[2 * blk]) + 0.0f;
+    // sums over the block's lanes: each lane of four gives three heads away and keeps one
+    const bool odd = threadIdx.x & 1, two = threadIdx.x & 2;
+    double a = (odd ? s[2] : s[0]) + dpp64<XOR1>(odd ? s[0] : s[2]);
+    double b = (odd ? s[3] : s[1]) + dpp64<XOR1>(odd ? s[1] : s[3]);
+    a = (two ? b : a) + dpp64<XOR2>(two ? a : b);
+    a += dpp64<QUAD_REV>(dpp64<HALF_MIRROR>(a));  // the lane 4 away
+    if constexpr (HD == 128) a += dpp64<ROR8>(a);
+    if ((odd ? 2 : 0) + (two ? 1 : 0) >= heads) a = -INFINITY;
+    a = max_nan(a, dpp64<XOR1>(a));
+    return max_nan(a, dpp64<XOR2>(a));
   }
+};
+// Bounds of the blocks [b0, b1) of a (row, kv head) for all heads: put(b, twice the bound, first four heads) by one lane of
+// each.  A wave takes 64 / LPB blocks at a time, NW of them in turn; the loop is not unrolled (a call fetches its code from
+// memory), the next blocks' codes are on their way.
+template <typename T, int HD, int NW, typename Put>
+__device__ __forceinline__ void score_blocks(const Kv8SelectArgs& a, int r, int kvh, size_t pair, int b0, int b1, Put put) {
+  constexpr int LPB = HD / 8, BPW = 64 / LPB;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sub = lane / LPB, c = lane % LPB;
+  const uint8_t* bounds = a.c.bounds + pair * a.c.NB * (2 * HD) + c * 16;
+  BlockScore<T, HD> score;
+  for (int h0 = 0; h0 < a.grp; h0 += 4) {
+    u4 next = zero16();
+    if (b0 + w * BPW < b1) next = ld16(bounds + (size_t)min(b0 + w * BPW + sub, b1 - 1) * (2 * HD));
+    score.load(a, r, kvh, h0);
+#pragma unroll 1
+    for (int b = b0 + w * BPW; b < b1; b += NW * BPW) {
+      const u4 code = next;
+      next = ld16(bounds + (size_t)min(b + NW * BPW + sub, b1 - 1) * (2 * HD));
+      const double v = score(code);
+      if (c == 0 && b + sub < b1) put(b + sub, v, h0 == 0);
+    }
+  }
+}
+__device__ __forceinline__ float block_score(double twice, float scale) { return (float)(0.5 * twice * (double)scale) + 0.0f; }
+
+// Scores of `per` (at most SCORE_BLOCKS) blocks of a (row, kv head) a workgroup, up to kv_max (blocks that are there, whatever
+// the length).  Bound by fp64 instructions: ~250 of a wave for 512 / hd blocks, ~150 before its first.
+constexpr int SCORE_NW = 4, SCORE_BLOCKS = 64;
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, int nb_max, int per) {
+  __shared__ double best[SCORE_BLOCKS];
+  const int kvh = blockIdx.y, r = blockIdx.z, b0 = blockIdx.x * per, b1 = min(nb_max, b0 + per);
+  const size_t pair = (size_t)r * a.Hk + kvh;
+  const int i = threadIdx.x;
+  const float scale = i < b1 - b0 ? a.c.scales[2 * (pair * a.c.NB + b0 + i)] : 0.f;
+  score_blocks<T, HD, SCORE_NW>(a, r, kvh, pair, b0, b1, [&](int b, double v, bool first) {
+    best[b - b0] = first ? v : max_nan(best[b - b0], v);
+  });
+  lds_barrier();
+  if (i < b1 - b0) a.scores[pair * nb_max + b0 + i] = block_score(best[i], scale);
 }
 
 // The n best blocks of a (row, kv head), in the order of their indices.  Equal scores: the lower index.  A NaN (a block
-// with an infinity or NaN) counts as greatest, so that it is read and seen.  Threshold by histograms of 2,048 bins over the
-// range that is left, at most three times; then one pass in the order of the blocks writes what lies above it.
-constexpr int PICK_THREADS = 1024, PICK_BINS = 2048, PICK_LDS_KEYS = 8192;
+// with an infinity or NaN) counts as greatest, so that it is read and seen.  Blocks [f, l) are chosen by score, those before
+// and after are always taken.
 __device__ __forceinline__ uint32_t score_key(float s) {
   const uint32_t u = __float_as_uint(s);
   return s != s ? 0xFFFFFFFFu : (u & 0x80000000u ? ~u : u | 0x80000000u);
 }
-__global__ __launch_bounds__(PICK_THREADS) void k_kv8_pick(Kv8SelectArgs a, int nb_max) {
-  constexpr int NW = PICK_THREADS / 64;
-  __shared__ uint32_t keys[PICK_LDS_KEYS];
-  __shared__ int hist[PICK_BINS];
-  __shared__ uint32_t wlo[NW], whi[NW];
-  __shared__ int wsum[NW], wsum2[NW];
-  __shared__ uint32_t s_lo, s_hi;
-  __shared__ int s_need;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r];
+struct Choice {
+  int closed, take, f, l, need;
+  __device__ __forceinline__ Choice(const Kv8SelectArgs& a, int n, int on, int r, int kvh, size_t pair) {
+    const bool bad = n < 0 || n > a.kv_max;
+    if (bad && kvh == 0 && threadIdx.x == 0) atomicOr(a.err + r, 8);
+    closed = bad || !on ? 0 : n / KV8_BLOCK;
+    take = min(a.n, closed);
+    f = a.first;
+    l = closed - a.last;
+    need = take - a.first - a.last;  // not negative where closed > a.n
+    if (threadIdx.x == 0) a.n_blocks[pair] = take;
+  }
+};
+
+// Rows of up to PICK_FEW blocks: one launch.  A workgroup scores the blocks of its (row, kv head), and thread b counts the
+// blocks that go before block b.
+constexpr int PICK_FEW = 128, FEW_NW = 8;
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * FEW_NW) void k_kv8_pick_few(Kv8SelectArgs a, int nb_max) {
+  __shared__ double best[PICK_FEW];
+  __shared__ __align__(16) uint32_t keys[PICK_FEW];
+  __shared__ int wsum[PICK_FEW / 64];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r], on = a.enable[r];
   const size_t pair = (size_t)r * a.Hk + kvh;
+  const float scale = tid < nb_max ? a.c.scales[2 * (pair * a.c.NB + tid)] : 0.f;
+  score_blocks<T, HD, FEW_NW>(a, r, kvh, pair, 0, nb_max, [&](int b, double v, bool first) {
+    best[b] = first ? v : max_nan(best[b], v);
+  });
+  const Choice ch(a, n, on, r, kvh, pair);
   int* out = a.blocks + pair * a.n;
-  const bool bad = n < 0 || n > a.kv_max;
-  if (bad && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
-  const int closed = bad || !a.enable[r] ? 0 : n / KV8_BLOCK, take = min(a.n, closed);
-  if (tid == 0) a.n_blocks[pair] = take;
-  for (int i = tid; i < a.n; i += PICK_THREADS)
-    if (i >= take) out[i] = -1;
-    else if (closed <= a.n) out[i] = i;
-  if (closed <= a.n) return;
-  // blocks [f, l) are chosen by score; the first f and those from l on are always taken
-  const int f = a.first, l = closed - a.last;
-  int need = take - a.first - a.last;  // f + last <= n < closed
+  for (int i = ch.take + tid; i < a.n; i += 64 * FEW_NW) out[i] = -1;
+  lds_barrier();
+  if (tid >= PICK_FEW) return;  // the barriers below count the waves that are left
+  // blocks that are not chosen by score have key 0, which no score has
+  const uint32_t k = tid >= ch.f && tid < ch.l ? score_key(block_score(best[tid], scale)) : 0u;
+  keys[tid] = k;
+  lds_barrier();
+  int before = 0;
+#pragma unroll 4
+  for (int i = ch.f & ~3; i < ch.l; i += 4) {
+    const u4 v = *reinterpret_cast<const u4*>(&keys[i]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) before += v[e] > k || (v[e] == k && i + e < tid);
+  }
+  const bool taken = tid < ch.closed && (ch.closed <= a.n || tid < ch.f || tid >= ch.l || before < ch.need);
+  const unsigned long long m = __ballot(taken);
+  if (lane == 0) wsum[w] = __popcll(m);
+  lds_barrier();
+  if (taken) {
+    int at = __popcll(m & ((1ull << lane) - 1));
+    for (int i = 0; i < w; ++i) at += wsum[i];
+    out[at] = tid;
+  }
+}
+
+// Longer rows: scores by k_kv8_scores, then one workgroup per (row, kv head) finds the key of the last block to be taken:
+// the keys' range in 1,024 bins, the bin in which the count from above reaches the number wanted, and so on within it until
+// it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.  A
+// last pass in the order of the blocks writes those above the key and the first of those equal to it.  NW waves: all of a
+// step's waves wait for each other, so short rows have few.
+constexpr int PICK_BINS = 1024, PICK_CAND = 256, PICK_LDS_KEYS = 14 * 1024;  // keys in LDS: below 64 KB with the rest
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 of rows 0 and 2 to the rows after them
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to the upper half
+  return v;
+}
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void k_kv8_pick(Kv8SelectArgs a, int nb_max) {
+  constexpr int NT = 64 * NW, UN = 8;
+  extern __shared__ uint32_t keys[];
+  __shared__ int hist[PICK_BINS];
+  __shared__ uint32_t cand[PICK_CAND], wlo[NW], whi[NW];
+  __shared__ int sums[2][NW], s_m, s_need, s_want, s_cand;
+  __shared__ uint32_t s_lo, s_hi;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r], on = a.enable[r];
+  const size_t pair = (size_t)r * a.Hk + kvh;
   const float* sc = a.scores + pair * nb_max;
-  const bool in_lds = l - f <= PICK_LDS_KEYS;
-  const auto key_at = [&](int b) { return in_lds ? keys[b - f] : score_key(sc[b]); };
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  for (int b = f + tid; b < l; b += PICK_THREADS) {
-    const uint32_t k = score_key(sc[b]);
-    if (in_lds) keys[b - f] = k;
-    lo = min(lo, k);
-    hi = max(hi, k);
+  float early[UN];  // the first scores, before the row's length is known (they are there up to kv_max)
+#pragma unroll
+  for (int u = 0; u < UN; ++u) early[u] = sc[min(a.first + tid + u * NT, max(nb_max, 1) - 1)];
+  const Choice ch(a, n, on, r, kvh, pair);
+  const int f = ch.f, l = ch.l;
+  int need = ch.need;
+  int* out = a.blocks + pair * a.n;
+  for (int i = tid; i < a.n; i += NT)
+    if (i >= ch.take) out[i] = -1;
+    else if (ch.closed <= a.n) out[i] = i;
+  if (ch.closed <= a.n) return;
+  const bool in_lds = nb_max <= PICK_LDS_KEYS;
+  // keys of the blocks b, b + NT, .. (UN of them), 0 (which no score has) where a block is not chosen by score
+  const auto keys_at = [&](int b, uint32_t* k, bool lds) {
+    float v[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int i = b + u * NT, at = min(max(i, f), l - 1);
+      if (lds) k[u] = keys[at];
+      else v[u] = sc[at];
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int i = b + u * NT;
+      if (!lds) k[u] = score_key(v[u]);
+      if (i < f || i >= l) k[u] = 0;
+    }
+  };
+  uint32_t lo = 0xFFFFFFFFu, hi = 0, k[UN];
+  for (int b = f + tid; b - tid < l; b += UN * NT) {
+    if (b < UN * NT + f) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u) k[u] = b + u * NT < l ? score_key(early[u]) : 0;
+    } else {
+      keys_at(b, k, false);
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      if (in_lds && b + u * NT < l) keys[b + u * NT] = k[u];
+      lo = min(lo, k[u] - 1);  // 0 goes last
+      hi = max(hi, k[u]);
+    }
   }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
@@ -406,70 +548,111 @@ __global__ __launch_bounds__(PICK_THREADS) void k_kv8_pick(Kv8SelectArgs a, int 
     wlo[w] = lo;
     whi[w] = hi;
   }
-  __syncthreads();
+  for (int i = tid; i < PICK_BINS; i += NT) hist[i] = 0;
+  if (tid == 0) s_cand = 0;
+  lds_barrier();
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
     lo = min(lo, wlo[i]);
     hi = max(hi, whi[i]);
   }
-  // invariant: every key above hi is taken, `need` of those in [lo, hi] are, none below lo
-  while (need > 0 && lo < hi) {
-    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
-    for (int i = tid; i < PICK_BINS; i += PICK_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int b = f + tid; b < l; b += PICK_THREADS) {
-      const uint32_t k = key_at(b);
-      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
-    }
-    __syncthreads();
-    // keys in the bins above: thread t holds bins 2047 - 2t and 2046 - 2t
-    const int j = PICK_BINS - 1 - 2 * tid, h0 = hist[j], h1 = hist[j - 1];
-    int inc = h0 + h1;
+  lo += 1;
+  // `need` of the keys in [lo, hi] are taken, all above and none below
+  int m = PICK_CAND + 1;
+  while (need > 0 && lo < hi && m > PICK_CAND) {
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
+    for (int b = f + tid; b - tid < l; b += UN * NT) {
+      keys_at(b, k, in_lds);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(inc, o, WAVE);
-      if (lane >= o) inc += v;
+      for (int u = 0; u < UN; ++u)
+        if (k[u] >= lo && k[u] <= hi) atomicAdd(&hist[(k[u] - lo) >> shift], 1);
     }
-    if (lane == 63) wsum[w] = inc;
-    __syncthreads();
-    int above = inc - h0 - h1;
-    for (int i = 0; i < w; ++i) above += wsum[i];
-    if (above < need && need <= above + h0 + h1) {  // one thread
-      const bool first = need <= above + h0;
-      const uint32_t bin = first ? j : j - 1, b_lo = lo + (bin << shift);
-      s_need = need - above - (first ? 0 : h0);
-      s_lo = b_lo;
-      s_hi = min(hi - b_lo, (1u << shift) - 1) + b_lo;
+    lds_barrier();
+    // thread t holds PB bins, from the top
+    constexpr int PB = PICK_BINS / NT > 0 ? PICK_BINS / NT : 1;
+    const int top = PICK_BINS - 1 - tid * PB;
+    int h[PB], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      h[i] = hist[top - i];
+      sum += h[i];
     }
-    __syncthreads();
+    int above = wave_scan(sum);
+    if (lane == 63) sums[0][w] = above;
+    lds_barrier();
+    above -= sum;
+    for (int i = 0; i < w; ++i) above += sums[0][i];
+    if (above < need && need <= above + sum) {  // one thread
+      int i = 0;
+      while (need > above + h[i]) above += h[i++];
+      s_m = h[i];
+      s_need = need - above;
+      s_lo = lo + ((uint32_t)(top - i) << shift);
+      s_hi = s_lo + min(hi - s_lo, (1u << shift) - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) hist[top - i] = 0;
+    lds_barrier();
     lo = s_lo;
     hi = s_hi;
     need = s_need;
+    m = s_m;
   }
-  // keys above hi, and the first `need` of those equal to it (need is 0 only where nothing is chosen by score)
-  int base = 0, base_eq = 0;
-  for (int b0 = 0; b0 < closed; b0 += PICK_THREADS) {
-    const int b = b0 + tid;
-    const bool in = b >= f && b < l;
-    const uint32_t k = in ? key_at(b) : 0;
-    const bool gt = b < closed && (in ? need > 0 && k > hi : true), eq = in && need > 0 && k == hi;
-    const unsigned long long mg = __ballot(gt), me = __ballot(eq), below = (1ull << lane) - 1;
-    __syncthreads();  // the sums of the pass before have been read
-    if (lane == 0) {
-      wsum[w] = __popcll(mg);
-      wsum2[w] = __popcll(me);
+  if (need > 0 && lo < hi) {  // at most PICK_CAND keys: each counts what lies above it
+    for (int b = f + tid; b - tid < l; b += UN * NT) {
+      keys_at(b, k, in_lds);
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+        if (k[u] >= lo && k[u] <= hi) cand[atomicAdd(&s_cand, 1)] = k[u];
     }
-    __syncthreads();
-    int ng = base + __popcll(mg & below), ne = base_eq + __popcll(me & below);
-    for (int i = 0; i < NW; ++i) {
-      if (i < w) {
-        ng += wsum[i];
-        ne += wsum2[i];
+    lds_barrier();
+    if (tid < m) {
+      const uint32_t c = cand[tid];
+      int gt = 0, ge = 0;
+      for (int i = 0; i < m; ++i) {
+        const uint32_t v = cand[i];
+        gt += v > c;
+        ge += v >= c;
       }
-      base += wsum[i];
-      base_eq += wsum2[i];
+      if (gt < need && need <= ge) {  // equal keys write the same
+        s_lo = c;
+        s_want = need - gt;
+      }
     }
-    if (gt || (eq && ne < need)) out[ng + min(ne, need)] = b;
+    lds_barrier();
+    lo = s_lo;
+    need = s_want;
+  }
+  // keys above lo, and the first `need` of those equal to it (none by score where need is 0), and the blocks outside [f, l)
+  const bool some = need > 0;
+  const int K = ((ch.closed + NT - 1) / NT) | 1, t0 = tid * K, t1 = min(ch.closed, t0 + K);  // odd: LDS banks
+  int ng = 0, ne = 0;
+  const auto key_of = [&](int b) { return b < f || b >= l ? 0xFFFFFFFFu : in_lds ? keys[b] : score_key(sc[b]); };
+  for (int b = t0; b < t1; ++b) {
+    const uint32_t v = key_of(b);
+    const bool in = b >= f && b < l;
+    ng += !in || (some && v > lo);
+    ne += in && some && v == lo;
+  }
+  int pg = wave_scan(ng), pe = wave_scan(ne);
+  lds_barrier();  // sums of the loop above have been read
+  if (lane == 63) {
+    sums[0][w] = pg;
+    sums[1][w] = pe;
+  }
+  lds_barrier();
+  for (int i = 0; i < w; ++i) {
+    pg += sums[0][i];
+    pe += sums[1][i];
+  }
+  pg -= ng;
+  pe -= ne;
+  for (int b = t0; b < t1; ++b) {
+    const uint32_t v = key_of(b);
+    const bool in = b >= f && b < l, gt = !in || (some && v > lo), eq = in && some && v == lo;
+    if (gt || (eq && pe < need)) out[pg + min(pe, need)] = b;
+    pg += gt;
+    pe += eq;
   }
 }
 
@@ -935,9 +1118,17 @@ int pack_t(const Kv8PackArgs& a, Stream s) {
 template <typename T, int HD>
 int select_t(const Kv8SelectArgs& a, Stream s) {
   const int nb = a.kv_max / KV8_BLOCK;
-  if (nb > a.n)
-    launch_k((k_kv8_scores<T, HD>), dim3((nb + SCORE_BLOCKS - 1) / SCORE_BLOCKS, a.Hk, a.R), dim3(SCORE_THREADS), 0, s, a, nb);
-  launch_k(k_kv8_pick, dim3(a.Hk, a.R), dim3(PICK_THREADS), 0, s, a, nb);
+  if (nb <= PICK_FEW && nb > 0) {
+    launch_k((k_kv8_pick_few<T, HD>), dim3(a.Hk, a.R), dim3(64 * FEW_NW), 0, s, a, nb);
+    return 0;
+  }
+  if (nb > a.n) {
+    // one block a lane group while that leaves a SIMD no more than two waves
+    const int per = (long long)nb * a.Hk * a.R <= 512 * SCORE_NW * (512 / HD) ? SCORE_NW * (512 / HD) : SCORE_BLOCKS;
+    launch_k((k_kv8_scores<T, HD>), dim3((nb + per - 1) / per, a.Hk, a.R), dim3(64 * SCORE_NW), 0, s, a, nb, per);
+  }
+  const bool wide = nb > 4096;
+  launch_k(wide ? k_kv8_pick<16> : k_kv8_pick<4>, dim3(a.Hk, a.R), dim3(wide ? 1024 : 256), nb <= PICK_LDS_KEYS ? nb * 4 : 0, s, a, nb);
   return 0;
 }
 template <typename T, int HD>

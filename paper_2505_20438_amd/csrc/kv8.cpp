@@ -146,7 +146,7 @@ int ham_op_kv8_select(const ham_kv8_shape* p, const void* d_q, const void* d_cac
   if (workspace_bytes < need) return fail(HAM_ENOMEM, "the workspace needs %zu bytes", need);
   Kv8SelectArgs a{};
   a.c = cache_of(p, d_cache);
-  a.R = p->rows; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.kv_max = kv_max; a.n = n_blocks; a.first = keep_first;
+  a.R = p->rows; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.grp = p->n_heads / p->n_kv_heads; a.kv_max = kv_max; a.n = n_blocks; a.first = keep_first;
   a.last = keep_last; a.q = d_q; a.kv_len = d_kv_len; a.enable = d_enable; a.blocks = d_blocks; a.n_blocks = d_n_blocks;
   a.err = d_err; a.scores = (float*)d_workspace;
   return launched(launch_kv8_select(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));

@@ -363,7 +363,8 @@ def choose(ham, s, q, cache, lens, kv_max, n, first=0, last=0, enable=None):
 SELECTS = [
     (BF16, 32, 8, 128, [3300, 0, 31, 32, 1000], 16, 0, 0), (BF16, 32, 8, 64, [2560, 2049], 16, 1, 2), (F32, 4, 2, 64, [5000], 7, 3, 4),
     (F32, 16, 1, 128, [700, 40000], 20, 0, 20), (BF16, 9, 3, 64, [1000, 65], 1, 0, 0), (BF16, 5, 1, 128, [1000, 320, 352], 10, 1, 1),
-    (BF16, 2, 2, 64, [70000], 1000, 4, 8), (BF16, 5, 1, 64, [300000], 33, 0, 0)]
+    (BF16, 2, 2, 64, [70000], 1000, 4, 8), (BF16, 5, 1, 64, [300000], 33, 0, 0), (BF16, 4, 1, 64, [4127, 4128, 4160, 4095], 9, 0, 1),
+    (BF16, 4, 1, 64, [131071, 131103], 40, 2, 0), (F32, 2, 1, 64, [500000, 4000], 25, 5, 3)]
 
 
 @pytest.mark.parametrize("dtype,H,Hk,hd,lens,n,first,last", SELECTS)
@@ -418,6 +419,18 @@ def test_no_key_of_a_block_left_out_beats_the_least_chosen_score(ham):
             left = torch.ones(n // B, dtype=torch.bool)
             left[chosen] = False
             assert torch.all(best[left] <= score[chosen].min() * (1 + 2.0 ** -23)) and torch.all(best <= score + score.abs() * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("kv_max", [0, 31, 32])
+def test_no_closed_block_or_one(ham, kv_max):
+    lens = [kv_max, 0]
+    s, ref, cache, q, qd = filled(ham, BF16, 8, 2, 64, lens, cap=128)
+    blocks, count, err = choose(ham, s, q, cache, lens, kv_max, 3, 1, 1)
+    nb = kv_max // B
+    assert blocks.tolist() == [[[0] * nb + [-1] * (3 - nb)] * 2, [[-1] * 3] * 2] and count.tolist() == [[nb] * 2, [0] * 2] and err == [0, 0]
+    got, err = attend(ham, s, q, cache, lens, kv_max, blocks, count)
+    near(got, ref.attention(qd, lens), BF16)
+    assert err == [0, 0]
 
 
 def test_rows_without_a_choice(ham):
