@@ -36,7 +36,7 @@ __host__ __device__ __forceinline__ int kv8_v_index(int s, int d) {
 
 struct Kv8AppendArgs {
   Kv8Cache c;
-  int R, T, H, Hk;
+  int R, T, H, Hk, grp;              // grp = H / Hk
   long long slots;                   // capacity of a row
   const float* qkv; const float* cos; const float* sin;
   const int* start; const int* count;

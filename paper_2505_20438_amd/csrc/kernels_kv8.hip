@@ -40,22 +40,26 @@ template <typename T> __device__ __forceinline__ f4 stored4(f4 v) {  // rounded 
   for (int e = 0; e < 4; ++e) v[e] = to_f<T>(from_f<T>(v[e]));
   return v;
 }
-// four values of an activation row of width W
-template <typename T> __device__ __forceinline__ void put_act4(void* base, size_t row, int W, int i, f4 v) {
+// eight values of an activation row of width W
+template <typename T> __device__ __forceinline__ void put_act8(void* base, size_t row, int W, int i, const f4* v) {
   if constexpr (Act<T>::SPLIT) {
     T* p = (T*)base + row * 2 * W + i;
-    const f4 hi = stored4<T>(v);
-    st4<T>(p, hi);
-    st4<T>(p + W, v - hi);
+    u4 hi, lo;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f4 h = stored4<T>(v[u]), d = v[u] - h;
+      hi[2 * u] = f2bf2(h[0], h[1]);
+      hi[2 * u + 1] = f2bf2(h[2], h[3]);
+      lo[2 * u] = f2bf2(d[0], d[1]);
+      lo[2 * u + 1] = f2bf2(d[2], d[3]);
+    }
+    *reinterpret_cast<u4*>(p) = hi;
+    *reinterpret_cast<u4*>(p + W) = lo;
   } else {
-    st4<T>((T*)base + row * W + i, v);
+    T* p = (T*)base + row * W + i;
+    st4<T>(p, v[0]);
+    st4<T>(p + 4, v[1]);
   }
-}
-template <typename T> __device__ __forceinline__ f4 get_act4(const void* base, size_t row, int W, int i) {
-  const T* p = (const T*)base + row * Act<T>::PL * W + i;
-  f4 v = ld4<T>(p);
-  if constexpr (Act<T>::SPLIT) v += ld4<T>(p + W);
-  return v;
 }
 
 // N values of the storage type as they lie in memory: a load without a conversion, which would wait for it
@@ -86,6 +90,23 @@ struct Raw {
   }
 };
 
+// the sum and the maximum over the 16 lanes of a row, in each of them
+template <int ROR> __device__ __forceinline__ float row_ror(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + ROR, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += row_ror<8>(v);
+  v += row_ror<4>(v);
+  v += row_ror<2>(v);
+  return v + row_ror<1>(v);
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, row_ror<8>(v));
+  v = fmaxf(v, row_ror<4>(v));
+  v = fmaxf(v, row_ror<2>(v));
+  return fmaxf(v, row_ror<1>(v));
+}
+
 // Rotate-half RoPE of the pair (x, y): products and sums are rounded one by one (no fused multiply-add), so that what is
 // rounded to 8 bits next does not depend on how the compiler contracts.
 __device__ __forceinline__ void rotate(f4& x, f4& y, f4 c, f4 s) {
@@ -100,95 +121,99 @@ __device__ __forceinline__ void block_scale(uint32_t top, float& scale, float& i
   scale = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top) / KV8_MAX;
   inv = scale >= 1.17549435e-38f ? 1.0f / scale : 0.0f;
 }
-__device__ __forceinline__ float to_range(float x, float inv) { return fminf(fmaxf(x * inv, -KV8_MAX), KV8_MAX); }
+// |x inv| is at most 448 and two roundings; the conversion takes what is below 464 to 448
 __device__ __forceinline__ uint32_t code4(const float* x, float inv) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_range(x[0], inv), to_range(x[1], inv), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_range(x[2], inv), to_range(x[3], inv), w, true);
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
 }
-__device__ __forceinline__ uint32_t top4(uint32_t top, f4 v) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-  return top;
-}
+__device__ __forceinline__ uint32_t magnitude(uint32_t top, float v) { return max(top, __float_as_uint(v) & 0x7FFFFFFFu); }
 
-// A full block in LDS (fp32 values of the storage type), coded and written.
-constexpr int CODE_THREADS = 256;
+// A full block is coded by 2 HD threads from their registers.  The first HD hold K: thread (t, g, r) of slot 8 (r / 4) + 4 t
+// + r % 4 the 16 channels from 16 g on and those HD / 2 after them (the other half of their RoPE pairs), which are two
+// 16-byte pieces of the codes.  The others hold V, and find the least and greatest value of K in each channel from a copy
+// in LDS.
 template <int HD>
-struct BlockLds {
-  float k[KV8_BLOCK][HD + 4], v[KV8_BLOCK][HD + 4];
-  uint32_t top[2][CODE_THREADS / 64];
+struct CodeLds {
+  uint32_t top[2 * HD / 64];
+  float k[KV8_BLOCK][HD + 4];
 };
-
-// `tk`, `tv`: bits of the greatest magnitude of K and V that this thread wrote.  Every thread of the workgroup calls it.
+template <int HD> struct KeyThread {  // of thread tid < HD
+  int t, g, r, slot, d0;
+  __device__ __forceinline__ explicit KeyThread(int tid) {
+    constexpr int G = HD / 32;  // channel groups of 16 in half a head
+    t = tid / (16 * G);
+    g = tid / 16 % G;
+    r = tid % 16;
+    slot = 8 * (r / 4) + 4 * t + r % 4;
+    d0 = 16 * g;
+  }
+};
 template <int HD>
-__device__ __forceinline__ void code_block(BlockLds<HD>& sh, uint32_t tk, uint32_t tv, const Kv8Cache& c, size_t blk) {
-  const int tid = threadIdx.x, lane = tid & 63;
+__device__ __forceinline__ void share_keys(CodeLds<HD>& sh, const KeyThread<HD>& kt, const float* k0, const float* k1) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    tk = max(tk, (uint32_t)__shfl_xor((int)tk, o, WAVE));
-    tv = max(tv, (uint32_t)__shfl_xor((int)tv, o, WAVE));
+  for (int e = 0; e < 16; e += 4) {
+    *reinterpret_cast<f4*>(&sh.k[kt.slot][kt.d0 + e]) = f4{k0[e], k0[e + 1], k0[e + 2], k0[e + 3]};
+    *reinterpret_cast<f4*>(&sh.k[kt.slot][kt.d0 + HD / 2 + e]) = f4{k1[e], k1[e + 1], k1[e + 2], k1[e + 3]};
   }
-  if (lane == 0) {
-    sh.top[0][tid >> 6] = tk;
-    sh.top[1][tid >> 6] = tv;
+}
+__device__ __forceinline__ void wave_top(uint32_t* tops, uint32_t top) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, WAVE));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+}
+// after a barrier: the scales of the block, written by one thread
+template <int HD>
+__device__ __forceinline__ void block_scales(const CodeLds<HD>& sh, const Kv8Cache& c, size_t blk, float& ki, float& vi) {
+  float ks, vs;
+  uint32_t k = sh.top[0], v = sh.top[HD / 64];
+  if constexpr (HD == 128) {
+    k = max(k, sh.top[1]);
+    v = max(v, sh.top[3]);
   }
-  __syncthreads();
-  float ks, ki, vs, vi;
-  block_scale(max(max(sh.top[0][0], sh.top[0][1]), max(sh.top[0][2], sh.top[0][3])), ks, ki);
-  block_scale(max(max(sh.top[1][0], sh.top[1][1]), max(sh.top[1][2], sh.top[1][3])), vs, vi);
-  if (tid == 0) {
+  block_scale(k, ks, ki);
+  block_scale(v, vs, vi);
+  if (threadIdx.x == 0) {
     c.scales[2 * blk] = ks;
     c.scales[2 * blk + 1] = vs;
   }
+}
+template <int HD>
+__device__ __forceinline__ void write_keys(const KeyThread<HD>& kt, const float* k0, const float* k1, float ki, const Kv8Cache& c,
+                                           size_t blk) {
   uint8_t* out = c.codes + blk * (2 * KV8_BLOCK * HD);
-  constexpr int CHUNKS = KV8_BLOCK * HD / 16;
-  for (int q = tid; q < CHUNKS; q += CODE_THREADS) {
-    const int r = q % 16, g = q / 16 % 4, p = q / 64;
-    {  // K: piece (t, i)
-      const int t = p / (HD / 64), i = p % (HD / 64);
-      const float* x = &sh.k[8 * (r / 4) + 4 * t + r % 4][64 * i + 16 * g];
-      u4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = code4(x + 4 * e, ki);
-      *reinterpret_cast<u4*>(out + q * 16) = w;
-    }
-    {  // V: piece p
-      u4 w;
+  for (int h = 0; h < 2; ++h) {
+    u4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x[4];
-#pragma unroll
-        for (int f = 0; f < 4; ++f) x[f] = sh.v[8 * g + (4 * e + f) % 8][32 * p + 16 * (e / 2) + r];
-        w[e] = code4(x, vi);
-      }
-      *reinterpret_cast<u4*>(out + KV8_BLOCK * HD + q * 16) = w;
-    }
+    for (int e = 0; e < 4; ++e) w[e] = code4((h ? k1 : k0) + 4 * e, ki);
+    *reinterpret_cast<u4*>(out + kv8_k_index(kt.slot, kt.d0 + h * (HD / 2), HD)) = w;
   }
-  // coding keeps the order, so the least code is that of the least value
-  if (tid < HD) {
-    float lo = sh.k[0][tid], hi = lo;
+}
+// bounds of channel d; coding keeps the order, so the least code is that of the least value
+template <int HD>
+__device__ __forceinline__ void write_bounds(const CodeLds<HD>& sh, int d, float ki, const Kv8Cache& c, size_t blk) {
+  float lo = sh.k[0][d], hi = lo;
 #pragma unroll
-    for (int s = 1; s < KV8_BLOCK; ++s) {
-      lo = fminf(lo, sh.k[s][tid]);
-      hi = fmaxf(hi, sh.k[s][tid]);
-    }
-    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_range(lo, ki), to_range(hi, ki), 0, false);
-    uint8_t* b = c.bounds + blk * (2 * HD) + tid / 8 * 16 + tid % 8;
-    b[0] = (uint8_t)w;
-    b[8] = (uint8_t)(w >> 8);
+  for (int s = 1; s < KV8_BLOCK; ++s) {
+    lo = fminf(lo, sh.k[s][d]);
+    hi = fmaxf(hi, sh.k[s][d]);
   }
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(lo * ki, hi * ki, 0, false);
+  uint8_t* b = c.bounds + blk * (2 * HD) + d / 8 * 16 + d % 8;
+  b[0] = (uint8_t)w;
+  b[8] = (uint8_t)(w >> 8);
 }
 
 // ---------------------------------------------------------------- append
 // Workgroups x < nb of a (row, kv head): block `first + x` of the row if the new tokens fill it; workgroup 0 also puts the
 // tokens past the last full block into the open one, after it has read what the open block held (so no other workgroup
-// touches it).  The others: q of APPEND_QT tokens each.
+// touches it).  The others: q of APPEND_QT tokens each, 8 pairs a thread.
 constexpr int APPEND_QT = 32;
 template <typename T, int HD>
-__global__ __launch_bounds__(CODE_THREADS) void k_kv8_append(Kv8AppendArgs a, int nb) {
-  constexpr int B = KV8_BLOCK, HALF = HD / 2, QPS = HALF / 4;  // quads of pairs per head
-  __shared__ BlockLds<HD> sh;
-  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.H / a.Hk;
+__global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) {
+  constexpr int B = KV8_BLOCK, HALF = HD / 2, QPS = HALF / 4, THREADS = 2 * HD;  // QPS: quads of pairs per head
+  __shared__ CodeLds<HD> sh;
+  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.grp;
   const int n0 = a.start[r], cnt = a.count[r];
   if (n0 < 0 || cnt < 0 || cnt > a.T || (long long)n0 + cnt > a.slots) {
     if (blockIdx.x == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
@@ -199,15 +224,23 @@ __global__ __launch_bounds__(CODE_THREADS) void k_kv8_append(Kv8AppendArgs a, in
   const float* cs = a.cos + (size_t)r * a.T * HALF;
   const float* sn = a.sin + (size_t)r * a.T * HALF;
   if ((int)blockIdx.x >= nb) {  // q
-    const int t0 = ((int)blockIdx.x - nb) * APPEND_QT, t1 = min(cnt, t0 + APPEND_QT), per = grp * QPS;
-    for (int q = tid; q < (t1 - t0) * per; q += CODE_THREADS) {
-      const int t = t0 + q / per, j = q % per / QPS, i = q % QPS * 4, h = kvh * grp + j;
+    const int t0 = ((int)blockIdx.x - nb) * APPEND_QT, t1 = min(cnt, t0 + APPEND_QT), items = (t1 - t0) * grp * (HALF / 8);
+    for (int q = tid; q < items; q += THREADS) {
+      const int i = q % (HALF / 8) * 8, hq = q / (HALF / 8), t = t0 + hq / grp, h = kvh * grp + hq % grp;
       const float* p = src + (size_t)t * ld + h * HD + i;
-      f4 x = *reinterpret_cast<const f4*>(p), y = *reinterpret_cast<const f4*>(p + HALF);
-      rotate(x, y, *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + i), *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + i));
+      f4 x[2], y[2], c[2], s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        x[u] = *reinterpret_cast<const f4*>(p + 4 * u);
+        y[u] = *reinterpret_cast<const f4*>(p + HALF + 4 * u);
+        c[u] = *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + i + 4 * u);
+        s[u] = *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + i + 4 * u);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) rotate(x[u], y[u], c[u], s[u]);
       const size_t row = (size_t)r * a.T + t;
-      put_act4<T>(a.q, row, a.H * HD, h * HD + i, x);
-      put_act4<T>(a.q, row, a.H * HD, h * HD + i + HALF, y);
+      put_act8<T>(a.q, row, a.H * HD, h * HD + i, x);
+      put_act8<T>(a.q, row, a.H * HD, h * HD + i + HALF, y);
     }
     return;
   }
@@ -223,41 +256,71 @@ __global__ __launch_bounds__(CODE_THREADS) void k_kv8_append(Kv8AppendArgs a, in
     rotate(x, y, *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + i), *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + i));
   };
   if (x0 < last - first) {
-    const int base = (first + x0) * B;
-    uint32_t tk = 0, tv = 0;
-    for (int q = tid; q < B * QPS; q += CODE_THREADS) {
-      const int w = q / QPS, i = q % QPS * 4, t = base + w - n0;
-      f4 x, y;
-      if (t < 0) {
-        x = ld4<T>(open + w * HD + i);
-        y = ld4<T>(open + w * HD + i + HALF);
-      } else {
-        key(t, i, x, y);
-        x = stored4<T>(x);
-        y = stored4<T>(y);
+    const size_t blk = pair * a.c.NB + first + x0;
+    const int base = (first + x0) * B - n0;  // token of the block's slot 0
+    float ki, vi;
+    if (tid < HD) {
+      const KeyThread<HD> kt(tid);
+      float k0[16], k1[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        f4 x, y;
+        if (base + kt.slot < 0) {
+          x = ld4<T>(open + kt.slot * HD + kt.d0 + i);
+          y = ld4<T>(open + kt.slot * HD + kt.d0 + i + HALF);
+        } else {
+          key(base + kt.slot, kt.d0 + i, x, y);
+          x = stored4<T>(x);
+          y = stored4<T>(y);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          top = magnitude(magnitude(top, x[e]), y[e]);
+          k0[i + e] = x[e];
+          k1[i + e] = y[e];
+        }
       }
-      tk = top4(top4(tk, x), y);
-      *reinterpret_cast<f4*>(&sh.k[w][i]) = x;
-      *reinterpret_cast<f4*>(&sh.k[w][i + HALF]) = y;
+      share_keys<HD>(sh, kt, k0, k1);
+      wave_top(sh.top, top);
+      __syncthreads();
+      block_scales<HD>(sh, a.c, blk, ki, vi);
+      write_keys<HD>(kt, k0, k1, ki, a.c, blk);
+    } else {  // V: channels d .. d + 3 of slots 8 g ..
+      const int d = (tid - HD) % (HD / 4) * 4, g = (tid - HD) / (HD / 4);
+      f4 v[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int w = 8 * g + i, t = base + w;
+        v[i] = t < 0 ? ld4<T>(open + (B + w) * HD + d) : stored4<T>(*reinterpret_cast<const f4*>(vsrc + (size_t)t * ld + d));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = magnitude(top, v[i][e]);
+      wave_top(sh.top, top);
+      __syncthreads();
+      block_scales<HD>(sh, a.c, blk, ki, vi);
+      uint8_t* out = a.c.codes + blk * (2 * B * HD) + B * HD;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo[4] = {v[0][e], v[1][e], v[2][e], v[3][e]}, hi[4] = {v[4][e], v[5][e], v[6][e], v[7][e]};
+        *reinterpret_cast<uint2*>(out + kv8_v_index(8 * g, d + e)) = uint2{code4(lo, vi), code4(hi, vi)};
+      }
+      write_bounds<HD>(sh, tid - HD, ki, a.c, blk);
     }
-    for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
-      const int w = q / (HD / 4), i = q % (HD / 4) * 4, t = base + w - n0;
-      const f4 x = t < 0 ? ld4<T>(open + (B + w) * HD + i) : stored4<T>(*reinterpret_cast<const f4*>(vsrc + (size_t)t * ld + i));
-      tv = top4(tv, x);
-      *reinterpret_cast<f4*>(&sh.v[w][i]) = x;
-    }
-    code_block<HD>(sh, tk, tv, a.c, pair * a.c.NB + first + x0);
   }
-  if (x0 == 0) {  // slots of the open block: tokens t of slots max(n0, 32 last) .. end
+  if (x0 == 0) {  // slots of the open block: tokens t of slots max(n0, 32 last) .. end (what it held has been read: a barrier)
     const int s0 = max(n0, last * B), ns = end - s0;
-    for (int q = tid; q < ns * QPS; q += CODE_THREADS) {
+    for (int q = tid; q < ns * QPS; q += THREADS) {
       const int s = s0 + q / QPS, i = q % QPS * 4, w = s - last * B;
       f4 x, y;
       key(s - n0, i, x, y);
       st4<T>(open + w * HD + i, x);
       st4<T>(open + w * HD + i + HALF, y);
     }
-    for (int q = tid; q < ns * (HD / 4); q += CODE_THREADS) {
+    for (int q = tid; q < ns * (HD / 4); q += THREADS) {
       const int s = s0 + q / (HD / 4), i = q % (HD / 4) * 4, w = s - last * B;
       st4<T>(open + (B + w) * HD + i, *reinterpret_cast<const f4*>(vsrc + (size_t)(s - n0) * ld + i));
     }
@@ -267,9 +330,9 @@ __global__ __launch_bounds__(CODE_THREADS) void k_kv8_append(Kv8AppendArgs a, in
 // ---------------------------------------------------------------- pack
 // One workgroup per (block, kv head, row): a full block is coded, the slots past the last full block go to the open one.
 template <typename T, int HD>
-__global__ __launch_bounds__(CODE_THREADS) void k_kv8_pack(Kv8PackArgs a) {
-  constexpr int B = KV8_BLOCK;
-  __shared__ BlockLds<HD> sh;
+__global__ __launch_bounds__(2 * HD) void k_kv8_pack(Kv8PackArgs a) {
+  constexpr int B = KV8_BLOCK, THREADS = 2 * HD;
+  __shared__ CodeLds<HD> sh;
   const int tid = threadIdx.x, b = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, n = a.kv_len[r];
   if (n < 0 || n > a.kv_max) {
     if (b == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
@@ -277,29 +340,68 @@ __global__ __launch_bounds__(CODE_THREADS) void k_kv8_pack(Kv8PackArgs a) {
   }
   const int closed = n / B, ns = min(B, n - b * B);
   if (ns <= 0) return;
-  const size_t pair = (size_t)r * a.Hk + kvh;
+  const size_t pair = (size_t)r * a.Hk + kvh, blk = pair * a.c.NB + b;
   const T* K = (const T*)a.K + (pair * a.S + (size_t)b * B) * HD;
   const T* VT = (const T*)a.VT + (pair * a.S + (size_t)b * B) * HD;  // [hd][32]
-  uint32_t tk = 0, tv = 0;
   if (b == closed) {  // the open block
     T* open = (T*)a.c.open + pair * 2 * B * HD;
-    for (int q = tid; q < ns * (HD / 4); q += CODE_THREADS) st4<T>(open + q * 4, ld4<T>(K + q * 4));
-    for (int q = tid; q < ns * HD; q += CODE_THREADS) open[B * HD + q] = VT[q % HD * B + q / HD];
+    for (int q = tid; q < ns * (HD / 4); q += THREADS) st4<T>(open + q * 4, ld4<T>(K + q * 4));
+    for (int q = tid; q < ns * HD; q += THREADS) open[B * HD + q] = VT[q % HD * B + q / HD];
     return;
   }
-  for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
-    const f4 x = ld4<T>(K + q * 4);
-    tk = top4(tk, x);
-    *reinterpret_cast<f4*>(&sh.k[q / (HD / 4)][q % (HD / 4) * 4]) = x;
-  }
-  for (int q = tid; q < B * HD / 4; q += CODE_THREADS) {
-    const int d = q / (B / 4), s = q % (B / 4) * 4;
-    const f4 x = ld4<T>(VT + q * 4);
-    tv = top4(tv, x);
+  uint32_t top = 0;
+  float ki, vi;
+  if (tid < HD) {
+    const KeyThread<HD> kt(tid);
+    Raw<T, 16> x, y;
+    x.load(K + kt.slot * HD + kt.d0);
+    y.load(K + kt.slot * HD + kt.d0 + HD / 2);
+    float k0[16], k1[16];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sh.v[s + e][d] = x[e];
+    for (int e = 0; e < 16; ++e) {
+      k0[e] = x.at(e);
+      k1[e] = y.at(e);
+      top = magnitude(magnitude(top, k0[e]), k1[e]);
+    }
+    share_keys<HD>(sh, kt, k0, k1);
+    wave_top(sh.top, top);
+    __syncthreads();
+    block_scales<HD>(sh, a.c, blk, ki, vi);
+    write_keys<HD>(kt, k0, k1, ki, a.c, blk);
+  } else {  // V: two 16-byte pieces, each slots 8 g .. of channels 32 p + r and 32 p + 16 + r
+    Raw<T, 8> v[2][2];
+    const int q0 = tid - HD;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int q = q0 + u * HD;
+        v[u][h].load(VT + (q / 64 * 32 + 16 * h + q % 16) * B + q / 16 % 4 * 8);
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = magnitude(top, v[u][h].at(e));
+    wave_top(sh.top, top);
+    __syncthreads();
+    block_scales<HD>(sh, a.c, blk, ki, vi);
+    uint8_t* out = a.c.codes + blk * (2 * B * HD) + B * HD;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      u4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = v[u][e / 2].at((4 * e + i) % 8);
+        w[e] = code4(f, vi);
+      }
+      *reinterpret_cast<u4*>(out + (q0 + u * HD) * 16) = w;
+    }
+    write_bounds<HD>(sh, q0, ki, a.c, blk);
   }
-  code_block<HD>(sh, tk, tv, a.c, pair * a.c.NB + b);
 }
 
 // ---------------------------------------------------------------- select
@@ -725,23 +827,6 @@ __device__ __forceinline__ float group_sum(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-// the sum and the maximum over the 16 lanes of a row, in each of them
-template <int ROR> __device__ __forceinline__ float row_ror(float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + ROR, 0xF, 0xF, true));
-}
-__device__ __forceinline__ float row_sum(float v) {
-  v += row_ror<8>(v);
-  v += row_ror<4>(v);
-  v += row_ror<2>(v);
-  return v + row_ror<1>(v);
-}
-__device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, row_ror<8>(v));
-  v = fmaxf(v, row_ror<4>(v));
-  v = fmaxf(v, row_ror<2>(v));
-  return fmaxf(v, row_ror<1>(v));
-}
-
 // Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
 // and P V; then x holds block `next`.  q: fragments in LDS (registers would not do for four waves a SIMD).  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this
 // lane's slots alone.  LIST: a block that is not `there` (zeros) counts for nothing.
@@ -1107,12 +1192,12 @@ __global__ __launch_bounds__(COMB_THREADS) void k_kv8_combine(Kv8AttnArgs a) {
 template <typename T, int HD>
 int append_t(const Kv8AppendArgs& a, Stream s) {
   const int nb = std::max(1, (a.T + KV8_BLOCK - 1) / KV8_BLOCK), nq = a.q ? (a.T + APPEND_QT - 1) / APPEND_QT : 0;
-  launch_k((k_kv8_append<T, HD>), dim3(nb + nq, a.Hk, a.R), dim3(CODE_THREADS), 0, s, a, nb);
+  launch_k((k_kv8_append<T, HD>), dim3(nb + nq, a.Hk, a.R), dim3(2 * HD), 0, s, a, nb);
   return 0;
 }
 template <typename T, int HD>
 int pack_t(const Kv8PackArgs& a, Stream s) {
-  launch_k((k_kv8_pack<T, HD>), dim3(std::max(1, (a.kv_max + KV8_BLOCK - 1) / KV8_BLOCK), a.Hk, a.R), dim3(CODE_THREADS), 0, s, a);
+  launch_k((k_kv8_pack<T, HD>), dim3(std::max(1, (a.kv_max + KV8_BLOCK - 1) / KV8_BLOCK), a.Hk, a.R), dim3(2 * HD), 0, s, a);
   return 0;
 }
 template <typename T, int HD>

@@ -111,7 +111,7 @@ int ham_op_kv8_append(const ham_kv8_shape* p, int32_t n_tokens, const float* d_q
   if (misaligned({d_qkv, d_cos, d_sin, d_q})) return fail(HAM_EINVAL, "buffers must be 16-byte aligned");
   Kv8AppendArgs a{};
   a.c = cache_of(p, d_cache);
-  a.R = p->rows; a.T = n_tokens; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.slots = p->slots_cap;
+  a.R = p->rows; a.T = n_tokens; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.grp = p->n_heads / p->n_kv_heads; a.slots = p->slots_cap;
   a.qkv = d_qkv; a.cos = d_cos; a.sin = d_sin; a.start = d_start; a.count = d_count; a.q = d_q; a.err = d_err;
   return launched(launch_kv8_append(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
 }
