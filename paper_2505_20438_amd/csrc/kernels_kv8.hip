@@ -12,6 +12,7 @@
 // k_kv8_scores, k_kv8_pick   the blocks whose keys' upper bounds are greatest.
 // k_kv8_attn, k_kv8_combine  attention of one query row per sequence over all or listed blocks and the open one.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kernels_kv8.h"
@@ -821,16 +822,20 @@ __device__ __forceinline__ float group_max(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ float group_sum(float v) {
+__device__ __forceinline__ float pair16_sum(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float pair32_sum(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+__device__ __forceinline__ float group_sum(float v) { return pair32_sum(pair16_sum(v)); }
 // Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
 // and P V; then x holds block `next`.  q: fragments in LDS (registers would not do for four waves a SIMD).  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this
-// lane's slots alone.  LIST: a block that is not `there` (zeros) counts for nothing.
-template <int HD, int N, bool LIST>
+// lane's slots alone.  LIST: a block that is not `there` (zeros) counts for nothing.  SPARE > 0: the operand rows from SPARE on
+// repeat the queries of those before, and take the third plane of their weights in the first product.
+template <int HD, int N, bool LIST, int SPARE>
 __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64], float scale, float& m, float& l, f4* o,
                                              const uint8_t* codes, const float* scales, int next, bool there) {
   float sc[8];
@@ -847,12 +852,13 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
         for (int n = 0; n < N; ++n) Frag<bf16>::mma(s, k, q[(2 * i + h) * N + n][threadIdx.x & 63]);
       }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sc[4 * t + e] = LIST ? s[e] * c + none : s[e] * c;
+    for (int e = 0; e < 4; ++e) sc[4 * t + e] = s[e];
   }
   x.load_k(codes, scales, next);
   float top = sc[0];
 #pragma unroll
   for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
+  top = top * c + none;  // c is not negative
   if (__any(top > m)) {  // rarely, once a row has seen many keys
     const float mnew = fmaxf(m, group_max(top));
     const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
@@ -866,17 +872,25 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
     }
     m = mnew;
   }
-  const float mz = m == -INFINITY ? 0.f : m;  // scores of -inf alone: all weights 0
+  const float mz = none - (m == -INFINITY ? 0.f : m);  // scores of -inf alone: all weights 0
   float p[8];
   const float vs = LIST && !there ? 0.f : x.vs;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(sc[e] - mz);
+    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], c, mz));
     l += p[e];
     p[e] *= vs;
   }
-  u4 pp[N];
-  to_planes<N>(p, pp);
+  u4 pp[SPARE > 0 ? 3 : N];
+  to_planes<(SPARE > 0 ? 3 : N)>(p, pp);
+  if constexpr (SPARE > 0) {
+    const bool third = threadIdx.x & SPARE;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pp[0][i] = third ? pp[2][i] : pp[0][i];
+      pp[1][i] = third ? 0u : pp[1][i];
+    }
+  }
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
@@ -910,6 +924,8 @@ struct AttLds {
 template <typename T, int HD, int GR, bool LIST>
 __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, PL = Act<T>::PL;
+  // a bf16 model's weights have a third plane where the 16 operand rows have room for it: 24 significant bits and not 16
+  constexpr int SPARE = N == 2 && GR < 16 ? GR : 0;
   constexpr int NW = ATT_WAVES<T>, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;            // open block: lanes of a slot, channels a lane
   constexpr int OUT = (GR * HD + THREADS - 1) / THREADS;  // outputs of a thread
   __shared__ AttLds<HD, GR, N, NW> sh;
@@ -954,7 +970,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
   u4 raw[QL];
   if (w < FRAGS) {
     const BufRsrc qs = buf_rsrc(qrow + (size_t)plane * a.H * HD, grp * HD * (int)sizeof(T));
-    const uint32_t qo = (r16 * HD + 64 * (qf / 2) + 16 * g + 8 * (qf % 2)) * (uint32_t)sizeof(T);
+    const uint32_t qo = ((SPARE > 0 && r16 < 2 * SPARE ? r16 % SPARE : r16) * HD + 64 * (qf / 2) + 16 * g + 8 * (qf % 2)) * (uint32_t)sizeof(T);
 #pragma unroll
     for (int j = 0; j < QL; ++j) raw[j] = buf_u4(qs, qo + 16 * j);
   }
@@ -1057,7 +1073,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
   float m = -INFINITY, l = 0.f;
   if constexpr (!LIST) {
     for (int e = first; e < cnt; e += stride)
-      attend_block<HD, N, false>(x, sh.qf, scale, m, l, o, codes, scales, e + stride < cnt ? e + stride : -1, true);
+      attend_block<HD, N, false, SPARE>(x, sh.qf, scale, m, l, o, codes, scales, e + stride < cnt ? e + stride : -1, true);
   } else {
     for (int e0 = first; e0 < cnt; e0 += 64 * stride) {  // 64 of the wave's entries at a time: one a lane
       if (e0 > first) {
@@ -1075,9 +1091,15 @@ __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
       }
       for (int j = 0; j < mine; ++j) {
         const int next = j + 1 < mine ? __builtin_amdgcn_readlane(blk, j + 1) : -1;
-        attend_block<HD, N, true>(x, sh.qf, scale, m, l, o, codes, scales, next, __builtin_amdgcn_readlane(blk, j) >= 0);
+        attend_block<HD, N, true, SPARE>(x, sh.qf, scale, m, l, o, codes, scales, next, __builtin_amdgcn_readlane(blk, j) >= 0);
       }
     }
+  }
+  if constexpr (SPARE > 0) {  // rows r and r + SPARE belong together: lanes 16 apart for 4 rows, 32 for 8
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[d][i] = SPARE == 4 ? pair16_sum(o[d][i]) : pair32_sum(o[d][i]);
   }
   // per wave: maximum, sum and unnormalised outputs, PUB waves at a time
   constexpr int PUB = AttLds<HD, GR, N, NW>::PUB;
@@ -1219,9 +1241,11 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
 template <typename T, int HD>
 int attention_t(const Kv8AttnArgs& a, Stream s) {
   const dim3 grid(a.nsplit, a.Hk, a.R), block(64 * ATT_WAVES<T>);
-  const bool few = a.grp <= 4;
-  if (a.blocks) launch_k(few ? k_kv8_attn<T, HD, 4, true> : k_kv8_attn<T, HD, 16, true>, grid, block, 0, s, a);
-  else launch_k(few ? k_kv8_attn<T, HD, 4, false> : k_kv8_attn<T, HD, 16, false>, grid, block, 0, s, a);
+  const auto kernel = [&](auto list) {
+    constexpr bool LIST = decltype(list)::value;
+    return a.grp <= 4 ? k_kv8_attn<T, HD, 4, LIST> : a.grp <= 8 ? k_kv8_attn<T, HD, 8, LIST> : k_kv8_attn<T, HD, 16, LIST>;
+  };
+  launch_k(a.blocks ? kernel(std::true_type{}) : kernel(std::false_type{}), grid, block, 0, s, a);
   if (a.nsplit > 1) launch_k((k_kv8_combine<T, HD>), dim3(a.grp, a.Hk, a.R), dim3(COMB_THREADS), 0, s, a);
   return 0;
 }
