@@ -662,7 +662,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_pick(Kv8SelectArgs a, int nb_ma
   lo += 1;
   // `need` of the keys in [lo, hi] are taken, all above and none below
   int m = PICK_CAND + 1;
-  while (need > 0 && lo < hi && m > PICK_CAND) {
+  for (int round = 0; round < 4 && need > 0 && lo < hi && m > PICK_CAND; ++round) {  // 32 -> 22 -> 12 -> 2 -> 0 bits
     const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
     for (int b = f + tid; b - tid < l; b += UN * NT) {
       keys_at(b, k, in_lds);
@@ -706,9 +706,10 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_pick(Kv8SelectArgs a, int nb_ma
       keys_at(b, k, in_lds);
 #pragma unroll
       for (int u = 0; u < UN; ++u)
-        if (k[u] >= lo && k[u] <= hi) cand[atomicAdd(&s_cand, 1)] = k[u];
+        if (k[u] >= lo && k[u] <= hi) cand[min(atomicAdd(&s_cand, 1), PICK_CAND - 1)] = k[u];  // there are m
     }
     lds_barrier();
+    m = min(m, PICK_CAND);
     if (tid < m) {
       const uint32_t c = cand[tid];
       int gt = 0, ge = 0;
@@ -753,7 +754,7 @@ __global__ __launch_bounds__(64 * NW) void k_kv8_pick(Kv8SelectArgs a, int nb_ma
   for (int b = t0; b < t1; ++b) {
     const uint32_t v = key_of(b);
     const bool in = b >= f && b < l, gt = !in || (some && v > lo), eq = in && some && v == lo;
-    if (gt || (eq && pe < need)) out[pg + min(pe, need)] = b;
+    if ((gt || (eq && pe < need)) && pg + min(pe, need) < ch.take) out[pg + min(pe, need)] = b;
     pg += gt;
     pe += eq;
   }

@@ -287,19 +287,21 @@ def ham_op_kv8_info(shape: HamKv8Shape) -> dict:
 
 
 def _fits(*tensors) -> bool:
-    """Whether device tensors hold what a call reads and writes of them: (tensor, bytes) pairs, packed and large enough."""
+    """Whether tensors hold what a call reads and writes of them: (tensor, bytes) pairs, on a GPU, packed and large enough."""
     for t, need in tensors:
-        if t.nbytes < need or not t.is_contiguous():
+        if t.nbytes < need or not t.is_cuda or not t.is_contiguous():
             return False
     return True
 
 
 def _refuse(**tensors) -> None:
     for name, (t, need) in tensors.items():
-        if not t.is_contiguous():
-            raise HamError(HAM_EINVAL, f"{name} must be contiguous")
         if t.nbytes < need:
             raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
+        if not t.is_contiguous():
+            raise HamError(HAM_EINVAL, f"{name} must be contiguous")
+        if not t.is_cuda:
+            raise HamError(HAM_EINVAL, f"{name} must be on a GPU")
 
 
 def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int) -> None:

@@ -137,6 +137,8 @@ def test_binding_refuses_tensors_that_are_too_small_or_strided(lib):
                 dict(count=blocks), dict(cache=cache[:-256]), dict(workspace=ws[:16])):
         with pytest.raises(ham.HamError):
             attend(**bad)
+    with pytest.raises(ham.HamError, match="on a GPU"):   # host memory never reaches a kernel
+        attend()
     for bad in (dict(cos=cs[:1]), dict(sin=cs[:, :, ::2]), dict(start=i32[:1]), dict(q=q[:1]), dict(qkv=qkv[:1])):
         a = dict(qkv=qkv, cos=cs, sin=cs, start=i32, count=i32, cache=cache, q=q, err=i32, stream=0)
         with pytest.raises(ham.HamError):
