@@ -206,26 +206,30 @@ __device__ __forceinline__ void write_bounds(const CodeLds<HD>& sh, int d, float
 }
 
 // ---------------------------------------------------------------- append
-// Workgroups x < nb of a (row, kv head): block `first + x` of the row if the new tokens fill it; workgroup 0 also puts the
-// tokens past the last full block into the open one, after it has read what the open block held (so no other workgroup
-// touches it).  The others: q of APPEND_QT tokens each, 8 pairs a thread.
-constexpr int APPEND_QT = 32;
+// Two kinds of workgroup for each of the nb steps of 32 tokens, row and kv head.  One: block `first + x` of the row if the
+// new tokens fill it; that of step 0 also puts the tokens past the last full block into the open one, after it has read
+// what the open block held (so no other workgroup touches it).  The other (if q is wanted): q of 32 tokens, 8 pairs a
+// thread.  All of one step of a row run on one XCD (workgroups go round the eight of them), whose L2 then holds the step's
+// RoPE factors: read by every XCD they were a third of all bytes read.
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) {
   constexpr int B = KV8_BLOCK, HALF = HD / 2, QPS = HALF / 4, THREADS = 2 * HD;  // QPS: quads of pairs per head
   __shared__ CodeLds<HD> sh;
-  const int tid = threadIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.grp;
+  const int tid = threadIdx.x, grp = a.grp, kinds = a.q ? 2 : 1;
+  const uint32_t s8 = blockIdx.x / 8, step = s8 / (uint32_t)(kinds * a.Hk) * 8 + blockIdx.x % 8, head = s8 % (uint32_t)(kinds * a.Hk);
+  const int r = (int)(step / (uint32_t)nb), x0 = (int)(step % (uint32_t)nb), kvh = (int)head % a.Hk;
+  if (r >= a.R) return;
   const int n0 = a.start[r], cnt = a.count[r];
   if (n0 < 0 || cnt < 0 || cnt > a.T || (long long)n0 + cnt > a.slots) {
-    if (blockIdx.x == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+    if (x0 == 0 && head == 0 && tid == 0) atomicOr(a.err + r, 8);
     return;
   }
   const int ld = (a.H + 2 * a.Hk) * HD;
   const float* src = a.qkv + (size_t)r * a.T * ld;
   const float* cs = a.cos + (size_t)r * a.T * HALF;
   const float* sn = a.sin + (size_t)r * a.T * HALF;
-  if ((int)blockIdx.x >= nb) {  // q
-    const int t0 = ((int)blockIdx.x - nb) * APPEND_QT, t1 = min(cnt, t0 + APPEND_QT), items = (t1 - t0) * grp * (HALF / 8);
+  if ((int)head >= a.Hk) {  // q
+    const int t0 = x0 * 32, t1 = min(cnt, t0 + 32), items = (t1 - t0) * grp * (HALF / 8);
     for (int q = tid; q < items; q += THREADS) {
       const int i = q % (HALF / 8) * 8, hq = q / (HALF / 8), t = t0 + hq / grp, h = kvh * grp + hq % grp;
       const float* p = src + (size_t)t * ld + h * HD + i;
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
     }
     return;
   }
-  const int x0 = blockIdx.x, end = n0 + cnt, first = n0 / B, last = end / B;
+  const int end = n0 + cnt, first = n0 / B, last = end / B;
   const size_t pair = (size_t)r * a.Hk + kvh;
   T* open = (T*)a.c.open + pair * 2 * B * HD;  // K, then V
   const float* ksrc = src + (size_t)(a.H + kvh) * HD;
@@ -262,24 +266,33 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
     float ki, vi;
     if (tid < HD) {
       const KeyThread<HD> kt(tid);
+      // every load first (a token for every lane, also where the slot is an old one), then the arithmetic
+      const int t = max(base + kt.slot, 0);
+      const float* p = ksrc + (size_t)t * ld + kt.d0;
+      f4 x[4], y[4], c[4], sv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = *reinterpret_cast<const f4*>(p + 4 * i);
+        y[i] = *reinterpret_cast<const f4*>(p + HALF + 4 * i);
+        c[i] = *reinterpret_cast<const f4*>(cs + (size_t)t * HALF + kt.d0 + 4 * i);
+        sv[i] = *reinterpret_cast<const f4*>(sn + (size_t)t * HALF + kt.d0 + 4 * i);
+      }
       float k0[16], k1[16];
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        f4 x, y;
-        if (base + kt.slot < 0) {
-          x = ld4<T>(open + kt.slot * HD + kt.d0 + i);
-          y = ld4<T>(open + kt.slot * HD + kt.d0 + i + HALF);
-        } else {
-          key(base + kt.slot, kt.d0 + i, x, y);
-          x = stored4<T>(x);
-          y = stored4<T>(y);
+      for (int i = 0; i < 4; ++i) {
+        rotate(x[i], y[i], c[i], sv[i]);
+        x[i] = stored4<T>(x[i]);
+        y[i] = stored4<T>(y[i]);
+        if (base < 0 && base + kt.slot < 0) {  // the row's first block: slots from the open one
+          x[i] = ld4<T>(open + kt.slot * HD + kt.d0 + 4 * i);
+          y[i] = ld4<T>(open + kt.slot * HD + kt.d0 + HALF + 4 * i);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          top = magnitude(magnitude(top, x[e]), y[e]);
-          k0[i + e] = x[e];
-          k1[i + e] = y[e];
+          top = magnitude(magnitude(top, x[i][e]), y[i][e]);
+          k0[4 * i + e] = x[i][e];
+          k1[4 * i + e] = y[i][e];
         }
       }
       share_keys<HD>(sh, kt, k0, k1);
@@ -292,14 +305,14 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
       f4 v[8];
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int w = 8 * g + i, t = base + w;
-        v[i] = t < 0 ? ld4<T>(open + (B + w) * HD + d) : stored4<T>(*reinterpret_cast<const f4*>(vsrc + (size_t)t * ld + d));
-      }
+      for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f4*>(vsrc + (size_t)max(base + 8 * g + i, 0) * ld + d);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i) {
+        v[i] = stored4<T>(v[i]);
+        if (base < 0 && base + 8 * g + i < 0) v[i] = ld4<T>(open + (B + 8 * g + i) * HD + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = magnitude(top, v[i][e]);
+      }
       wave_top(sh.top, top);
       __syncthreads();
       block_scales<HD>(sh, a.c, blk, ki, vi);
@@ -1214,8 +1227,9 @@ __global__ __launch_bounds__(COMB_THREADS) void k_kv8_combine(Kv8AttnArgs a) {
 
 template <typename T, int HD>
 int append_t(const Kv8AppendArgs& a, Stream s) {
-  const int nb = std::max(1, (a.T + KV8_BLOCK - 1) / KV8_BLOCK), nq = a.q ? (a.T + APPEND_QT - 1) / APPEND_QT : 0;
-  launch_k((k_kv8_append<T, HD>), dim3(nb + nq, a.Hk, a.R), dim3(2 * HD), 0, s, a, nb);
+  const int nb = (a.T + 31) / 32;
+  const unsigned steps = (unsigned)((((long long)a.R * nb + 7) / 8) * 8);
+  launch_k((k_kv8_append<T, HD>), dim3(steps * a.Hk * (a.q ? 2 : 1)), dim3(2 * HD), 0, s, a, nb);
   return 0;
 }
 template <typename T, int HD>

@@ -109,6 +109,8 @@ int ham_op_kv8_append(const ham_kv8_shape* p, int32_t n_tokens, const float* d_q
   if (n_tokens < 1 || n_tokens > (1 << 24)) return fail(HAM_EINVAL, "n_tokens must be in 1..2^24");
   if (!d_qkv || !d_cos || !d_sin || !d_start || !d_count || !d_err) return fail(HAM_EINVAL, "null pointer");
   if (misaligned({d_qkv, d_cos, d_sin, d_q})) return fail(HAM_EINVAL, "buffers must be 16-byte aligned");
+  if (((long long)p->rows * ((n_tokens + 31) / 32) + 8) * p->n_kv_heads * 4 * p->head_dim > UINT32_MAX)
+    return fail(HAM_EINVAL, "rows * n_tokens * n_kv_heads * head_dim too large for one call");
   Kv8AppendArgs a{};
   a.c = cache_of(p, d_cache);
   a.R = p->rows; a.T = n_tokens; a.H = p->n_heads; a.Hk = p->n_kv_heads; a.grp = p->n_heads / p->n_kv_heads; a.slots = p->slots_cap;
