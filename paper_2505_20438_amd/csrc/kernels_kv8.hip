@@ -544,36 +544,42 @@ struct Choice {
   }
 };
 
-// Rows of up to PICK_FEW blocks: one launch.  A workgroup scores the blocks of its (row, kv head), and thread b counts the
-// blocks that go before block b.
-constexpr int PICK_FEW = 128, FEW_NW = 8;
-template <typename T, int HD>
-__global__ __launch_bounds__(64 * FEW_NW) void k_kv8_pick_few(Kv8SelectArgs a, int nb_max) {
-  __shared__ double best[PICK_FEW];
-  __shared__ __align__(16) uint32_t keys[PICK_FEW];
-  __shared__ int wsum[PICK_FEW / 64];
+// Rows of up to PICK_FEW blocks: one launch.  A workgroup scores the blocks of its (row, kv head); for block b thread b and
+// three more count the blocks that go before it, a quarter of them each.
+constexpr int PICK_FEW = 192;
+template <typename T, int HD, int MOST>
+__global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int nb_max) {
+  constexpr int PARTS = 4;
+  __shared__ double best[MOST];
+  __shared__ __align__(16) uint32_t keys[MOST];
+  __shared__ int wsum[MOST / 64], parts[PARTS][MOST];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r], on = a.enable[r];
   const size_t pair = (size_t)r * a.Hk + kvh;
   const float scale = tid < nb_max ? a.c.scales[2 * (pair * a.c.NB + tid)] : 0.f;
-  score_blocks<T, HD, FEW_NW>(a, r, kvh, pair, 0, nb_max, [&](int b, double v, bool first) {
+  score_blocks<T, HD, MOST / 16>(a, r, kvh, pair, 0, nb_max, [&](int b, double v, bool first) {
     best[b] = first ? v : max_nan(best[b], v);
   });
   const Choice ch(a, n, on, r, kvh, pair);
   int* out = a.blocks + pair * a.n;
-  for (int i = ch.take + tid; i < a.n; i += 64 * FEW_NW) out[i] = -1;
+  for (int i = ch.take + tid; i < a.n; i += 4 * MOST) out[i] = -1;
   lds_barrier();
-  if (tid >= PICK_FEW) return;  // the barriers below count the waves that are left
   // blocks that are not chosen by score have key 0, which no score has
-  const uint32_t k = tid >= ch.f && tid < ch.l ? score_key(block_score(best[tid], scale)) : 0u;
-  keys[tid] = k;
+  if (tid < MOST) keys[tid] = tid >= ch.f && tid < ch.l ? score_key(block_score(best[tid], scale)) : 0u;
   lds_barrier();
+  const int b = tid % MOST, part = tid / MOST;
+  const uint32_t k = keys[b];
   int before = 0;
-#pragma unroll 4
-  for (int i = ch.f & ~3; i < ch.l; i += 4) {
+#pragma unroll 2
+  for (int i = (ch.f & ~3) + 4 * part; i < ch.l; i += 4 * PARTS) {
     const u4 v = *reinterpret_cast<const u4*>(&keys[i]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) before += v[e] > k || (v[e] == k && i + e < tid);
+    for (int e = 0; e < 4; ++e) before += v[e] > k || (v[e] == k && i + e < b);
   }
+  parts[part][b] = before;
+  lds_barrier();
+  if (tid >= MOST) return;  // the barrier below counts the waves that are left
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) before += parts[i][b];
   const bool taken = tid < ch.closed && (ch.closed <= a.n || tid < ch.f || tid >= ch.l || before < ch.need);
   const unsigned long long m = __ballot(taken);
   if (lane == 0) wsum[w] = __popcll(m);
@@ -1241,7 +1247,7 @@ template <typename T, int HD>
 int select_t(const Kv8SelectArgs& a, Stream s) {
   const int nb = a.kv_max / KV8_BLOCK;
   if (nb <= PICK_FEW && nb > 0) {
-    launch_k((k_kv8_pick_few<T, HD>), dim3(a.Hk, a.R), dim3(64 * FEW_NW), 0, s, a, nb);
+    launch_k(nb <= 128 ? k_kv8_pick_few<T, HD, 128> : k_kv8_pick_few<T, HD, PICK_FEW>, dim3(a.Hk, a.R), dim3(nb <= 128 ? 512 : 768), 0, s, a, nb);
     return 0;
   }
   if (nb > a.n) {
@@ -1249,7 +1255,7 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
     const int per = (long long)nb * a.Hk * a.R <= 512 * SCORE_NW * (512 / HD) ? SCORE_NW * (512 / HD) : SCORE_BLOCKS;
     launch_k((k_kv8_scores<T, HD>), dim3((nb + per - 1) / per, a.Hk, a.R), dim3(64 * SCORE_NW), 0, s, a, nb, per);
   }
-  const bool wide = nb > 4096;
+  const bool wide = nb > 2048;
   launch_k(wide ? k_kv8_pick<16> : k_kv8_pick<4>, dim3(a.Hk, a.R), dim3(wide ? 1024 : 256), nb <= PICK_LDS_KEYS ? nb * 4 : 0, s, a, nb);
   return 0;
 }

@@ -75,13 +75,14 @@ inline PromptAttnGrid prompt_attn_grid(int R, int s0, int T, int H, int Hkv) {
 // Splits of the attention over the 8-bit cache for R rows of Hk kv heads of which the longest reads `blocks` blocks of 32
 // slots.  One workgroup of 16 waves runs per CU.  Its 16 blocks (one a wave) take 2.3 us at head dim 128 and 1.45 at 64
 // alone and half as much again with all 256 CUs at work, but no less than its share of memory: a block of every CU's takes
-// 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk * splits workgroups take ceil(... / 256) rounds, the first 5.4 us and the
-// others 2 beside that, and a split launch 2.5 us more for the combine.  The count with the least estimate, the lowest of
-// equal ones.  8 kv heads of 128, us at the splits here / at 256 / (R * Hk) rounded up: 4 rows x 33,300 slots 45.5 / 47.2,
-// 5 x 33,300 55 / 73, 12 x 4,096 21 / 26, 20 x 4,096 31 / 38, 40 x 4,096 61 / 63 (and 1 x 1,000 10.2 unsplit / 10.7).
+// 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk * splits workgroups take ceil(... / 256)
+// rounds, the first 5.4 us and the others 2 beside that, and a split launch 2.5 us more for the combine.  The count with the
+// least estimate, the lowest of equal ones.  8 kv heads of 128, us at the splits here / at 256 / (R * Hk) rounded up:
+// 4 rows x 33,300 slots 45.9 / 48.1, 5 x 33,300 55 / 74, 12 x 4,096 21 / 27, 20 x 4,096 29 / 40, 40 x 4,096 62 / 65 (and
+// 1 x 1,000 11.4 unsplit / 11.5).  The best of 1 .. 48 splits was at most 4% below it at 13 of 15 shapes tried, 7% at two.
 // A row's blocks are shared by its own splits alone, so a long row among short ones is a serial chain (1,040 blocks 155 us
-// unsplit, 47 in four): from 512 blocks on a row gets one split for every 256, up to four; where all rows are long that
-// costs up to a twentieth (32 x 33,300 317 -> 329).
+// unsplit, 48 in four): from 512 blocks on a row gets one split for every 256, up to four; where all rows are long that
+// costs up to a twentieth (32 x 33,300 319 -> 333).
 constexpr int KV8_MOST_WGS = 1024;  // workgroups of a split launch, unless four splits of every pair are more
 inline int kv8_attn_splits(int R, int Hk, int hd, int blocks) {
   const long long pairs = (long long)R * Hk;
