@@ -108,6 +108,21 @@ __device__ __forceinline__ float row_max(float v) {
   return fmaxf(v, row_ror<1>(v));
 }
 
+// the greatest over a row of 16 lanes and over a wave, in each lane (lanes 16 and 32 apart are swapped on the vector units)
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, true));  // row_ror 8, 4, 2, 1
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, true));
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = row_max(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
 // Rotate-half RoPE of the pair (x, y): products and sums are rounded one by one (no fused multiply-add), so that what is
 // rounded to 8 bits next does not depend on how the compiler contracts.
 __device__ __forceinline__ void rotate(f4& x, f4& y, f4 c, f4 s) {
@@ -158,8 +173,7 @@ __device__ __forceinline__ void share_keys(CodeLds<HD>& sh, const KeyThread<HD>&
   }
 }
 __device__ __forceinline__ void wave_top(uint32_t* tops, uint32_t top) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, WAVE));
+  top = wave_max(top);
   if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
 }
 // after a barrier: the scales of the block, written by one thread
@@ -593,189 +607,195 @@ __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int 
 
 // Longer rows: scores by k_kv8_scores, then one workgroup per (row, kv head) finds the key of the last block to be taken:
 // the keys' range in 1,024 bins, the bin in which the count from above reaches the number wanted, and so on within it until
-// it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.  A
-// last pass in the order of the blocks writes those above the key and the first of those equal to it.  NW waves: all of a
-// step's waves wait for each other, so short rows have few.
-constexpr int PICK_BINS = 1024, PICK_CAND = 256, PICK_LDS_KEYS = 14 * 1024;  // keys in LDS: below 64 KB with the rest
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int v) {
+// it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.
+// Those above the key and the first of those equal to it are then written in the order of the blocks.  The keys stay in
+// registers, UN a thread; rows with more are read again for each step.  Every step is a few dependent instructions and a
+// barrier, which a lone wave issues at one in eight to ten cycles: sixteen waves, not four (1,040 blocks 17 -> 13 us).
+constexpr int PICK_BINS = 1024, PICK_CAND = 128;  // counting 256 keys takes as long as three rounds of bins
+// inclusive sum over the lanes up to this one, of a row of 16 and of the wave
+__device__ __forceinline__ int row_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1, 2, 4, 8
   v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
   v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v = row_scan(v);
   v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 of rows 0 and 2 to the rows after them
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to the upper half
   return v;
 }
-template <int NW>
-__global__ __launch_bounds__(64 * NW) void k_kv8_pick(Kv8SelectArgs a, int nb_max) {
-  constexpr int NT = 64 * NW, UN = 8;
-  extern __shared__ uint32_t keys[];
-  __shared__ int hist[PICK_BINS];
-  __shared__ uint32_t cand[PICK_CAND], wlo[NW], whi[NW];
-  __shared__ int sums[2][NW], s_m, s_need, s_want, s_cand;
-  __shared__ uint32_t s_lo, s_hi;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r], on = a.enable[r];
+template <int UN>
+__global__ __launch_bounds__(1024) void k_kv8_pick(Kv8SelectArgs a, int nb_max) {
+  constexpr int NW = 16, NT = 64 * NW, STEP = UN * NT, PER = UN * NW > 64 ? UN * NW / 64 : 1;
+  __shared__ int hist[PICK_BINS], counts[UN * NW], sums[NW], s_m, s_need, s_want, s_cand;
+  __shared__ __align__(16) uint32_t cand[PICK_CAND];
+  __shared__ int above[PICK_CAND], upto[PICK_CAND];
+  __shared__ uint32_t wlo[NW], whi[NW], s_lo, s_hi;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), kvh = blockIdx.x, r = blockIdx.y;
+  const int n = a.kv_len[r], on = a.enable[r];
   const size_t pair = (size_t)r * a.Hk + kvh;
   const float* sc = a.scores + pair * nb_max;
-  float early[UN];  // the first scores, before the row's length is known (they are there up to kv_max)
+  float v[UN];  // the first scores, before the row's length is known (they are there up to kv_max)
 #pragma unroll
-  for (int u = 0; u < UN; ++u) early[u] = sc[min(a.first + tid + u * NT, max(nb_max, 1) - 1)];
+  for (int u = 0; u < UN; ++u) v[u] = sc[min(a.first + tid + u * NT, max(nb_max, 1) - 1)];
+  static_assert(PICK_BINS == NT, "a bin a thread");
+  hist[tid] = 0;
+  if (tid < PICK_CAND) {
+    cand[tid] = 0;
+    above[tid] = 0;
+    upto[tid] = 0;
+  }
+  if (tid == 0) s_cand = 0;
   const Choice ch(a, n, on, r, kvh, pair);
   const int f = ch.f, l = ch.l;
   int need = ch.need;
   int* out = a.blocks + pair * a.n;
+  const bool all = ch.closed <= a.n;
   for (int i = tid; i < a.n; i += NT)
     if (i >= ch.take) out[i] = -1;
-    else if (ch.closed <= a.n) out[i] = i;
-  if (ch.closed <= a.n) return;
-  const bool in_lds = nb_max <= PICK_LDS_KEYS;
-  // keys of the blocks b, b + NT, .. (UN of them), 0 (which no score has) where a block is not chosen by score
-  const auto keys_at = [&](int b, uint32_t* k, bool lds) {
-    float v[UN];
+    else if (all || i < f) out[i] = i;
+    else if (i >= ch.take - a.last) out[i] = ch.closed - (ch.take - i);
+  if (all || need <= 0) return;
+  const bool many = l - f > STEP;
+  uint32_t k[UN];  // keys of the blocks c + tid, c + tid + NT, ..: 0 (which no score has) past the last
+  const auto keys_of = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int i = b + u * NT, at = min(max(i, f), l - 1);
-      if (lds) k[u] = keys[at];
-      else v[u] = sc[at];
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int i = b + u * NT;
-      if (!lds) k[u] = score_key(v[u]);
-      if (i < f || i >= l) k[u] = 0;
-    }
+    for (int u = 0; u < UN; ++u) k[u] = c + tid + u * NT < l ? score_key(v[u]) : 0;
   };
-  uint32_t lo = 0xFFFFFFFFu, hi = 0, k[UN];
-  for (int b = f + tid; b - tid < l; b += UN * NT) {
-    if (b < UN * NT + f) {
+  const auto fetch = [&](int c) {
 #pragma unroll
-      for (int u = 0; u < UN; ++u) k[u] = b + u * NT < l ? score_key(early[u]) : 0;
-    } else {
-      keys_at(b, k, false);
-    }
+    for (int u = 0; u < UN; ++u) v[u] = sc[min(c + tid + u * NT, l - 1)];
+    keys_of(c);
+  };
+  keys_of(f);
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int c = f; c < l; c += STEP) {
+    if (c > f) fetch(c);
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      if (in_lds && b + u * NT < l) keys[b + u * NT] = k[u];
       lo = min(lo, k[u] - 1);  // 0 goes last
       hi = max(hi, k[u]);
     }
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, WAVE));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, WAVE));
-  }
+  lo = ~wave_max(~lo);
+  hi = wave_max(hi);
   if (lane == 0) {
     wlo[w] = lo;
     whi[w] = hi;
   }
-  for (int i = tid; i < PICK_BINS; i += NT) hist[i] = 0;
-  if (tid == 0) s_cand = 0;
   lds_barrier();
-#pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    lo = min(lo, wlo[i]);
-    hi = max(hi, whi[i]);
-  }
-  lo += 1;
+  lo = ~row_max(~wlo[lane % NW]) + 1;
+  hi = row_max(whi[lane % NW]);
   // `need` of the keys in [lo, hi] are taken, all above and none below
-  int m = PICK_CAND + 1;
-  for (int round = 0; round < 4 && need > 0 && lo < hi && m > PICK_CAND; ++round) {  // 32 -> 22 -> 12 -> 2 -> 0 bits
+  int m = min(l - f, PICK_CAND + 1);
+  for (int round = 0; round < 4 && lo < hi && m > PICK_CAND; ++round) {  // 32 -> 22 -> 12 -> 2 -> 0 bits
     const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
-    for (int b = f + tid; b - tid < l; b += UN * NT) {
-      keys_at(b, k, in_lds);
+    for (int c = f; c < l; c += STEP) {
+      if (many) fetch(c);
 #pragma unroll
       for (int u = 0; u < UN; ++u)
         if (k[u] >= lo && k[u] <= hi) atomicAdd(&hist[(k[u] - lo) >> shift], 1);
     }
     lds_barrier();
-    // thread t holds PB bins, from the top
-    constexpr int PB = PICK_BINS / NT > 0 ? PICK_BINS / NT : 1;
-    const int top = PICK_BINS - 1 - tid * PB;
-    int h[PB], sum = 0;
-#pragma unroll
-    for (int i = 0; i < PB; ++i) {
-      h[i] = hist[top - i];
-      sum += h[i];
-    }
-    int above = wave_scan(sum);
-    if (lane == 63) sums[0][w] = above;
+    const int bin = PICK_BINS - 1 - tid, here = hist[bin];  // thread t holds bin t from the top
+    int before = wave_scan(here);
+    if (lane == 63) sums[w] = before;
     lds_barrier();
-    above -= sum;
-    for (int i = 0; i < w; ++i) above += sums[0][i];
-    if (above < need && need <= above + sum) {  // one thread
-      int i = 0;
-      while (need > above + h[i]) above += h[i++];
-      s_m = h[i];
-      s_need = need - above;
-      s_lo = lo + ((uint32_t)(top - i) << shift);
+    before -= here;
+    const int waves = row_scan(sums[lane % NW]);
+    if (w > 0) before += __builtin_amdgcn_readlane(waves, w - 1);
+    if (before < need && need <= before + here) {  // one thread
+      s_m = here;
+      s_need = need - before;
+      s_lo = lo + ((uint32_t)bin << shift);
       s_hi = s_lo + min(hi - s_lo, (1u << shift) - 1);
     }
-#pragma unroll
-    for (int i = 0; i < PB; ++i) hist[top - i] = 0;
+    hist[bin] = 0;
     lds_barrier();
     lo = s_lo;
     hi = s_hi;
     need = s_need;
     m = s_m;
   }
-  if (need > 0 && lo < hi) {  // at most PICK_CAND keys: each counts what lies above it
-    for (int b = f + tid; b - tid < l; b += UN * NT) {
-      keys_at(b, k, in_lds);
+  const unsigned long long lower = (1ull << lane) - 1;
+  if (lo < hi) {  // m (at most PICK_CAND) keys: each counts what lies above it
+    for (int c = f; c < l; c += STEP) {
+      if (many) fetch(c);
+      int hits = 0, at = 0;
 #pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (k[u] >= lo && k[u] <= hi) cand[min(atomicAdd(&s_cand, 1), PICK_CAND - 1)] = k[u];  // there are m
+      for (int u = 0; u < UN; ++u) hits += __popcll(__ballot(k[u] >= lo && k[u] <= hi));
+      if (hits == 0) continue;
+      if (lane == 0) at = atomicAdd(&s_cand, hits);
+      at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const bool in = k[u] >= lo && k[u] <= hi;
+        const unsigned long long mask = __ballot(in);
+        if (in) cand[min(at + (int)__popcll(mask & lower), PICK_CAND - 1)] = k[u];
+        at += __popcll(mask);
+      }
     }
     lds_barrier();
     m = min(m, PICK_CAND);
-    if (tid < m) {
-      const uint32_t c = cand[tid];
-      int gt = 0, ge = 0;
-      for (int i = 0; i < m; ++i) {
-        const uint32_t v = cand[i];
-        gt += v > c;
-        ge += v >= c;
+    // 64 keys a group, the waves of a group share what they are compared with
+    const int gs = m <= 64 ? 0 : 1, group = w & ((1 << gs) - 1), part = w >> gs, parts = NW >> gs;
+    static_assert(PICK_CAND == 128, "at most two groups");
+    const uint32_t c = cand[group * 64 + lane];
+    int gt = 0, ge = 0;
+#pragma unroll 2
+    for (int i = 4 * part; i < m; i += 4 * parts) {
+      const u4 x = *reinterpret_cast<const u4*>(&cand[i]);  // 0 past the last: above no key
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        gt += x[e] > c;
+        ge += x[e] >= c;
       }
-      if (gt < need && need <= ge) {  // equal keys write the same
-        s_lo = c;
-        s_want = need - gt;
-      }
+    }
+    atomicAdd(&above[group * 64 + lane], gt);
+    atomicAdd(&upto[group * 64 + lane], ge);
+    lds_barrier();
+    if (tid < m && above[tid] < need && need <= upto[tid]) {  // equal keys write the same
+      s_lo = cand[tid];
+      s_want = need - above[tid];
     }
     lds_barrier();
     lo = s_lo;
     need = s_want;
   }
-  // keys above lo, and the first `need` of those equal to it (none by score where need is 0), and the blocks outside [f, l)
-  const bool some = need > 0;
-  const int K = ((ch.closed + NT - 1) / NT) | 1, t0 = tid * K, t1 = min(ch.closed, t0 + K);  // odd: LDS banks
-  int ng = 0, ne = 0;
-  const auto key_of = [&](int b) { return b < f || b >= l ? 0xFFFFFFFFu : in_lds ? keys[b] : score_key(sc[b]); };
-  for (int b = t0; b < t1; ++b) {
-    const uint32_t v = key_of(b);
-    const bool in = b >= f && b < l;
-    ng += !in || (some && v > lo);
-    ne += in && some && v == lo;
-  }
-  int pg = wave_scan(ng), pe = wave_scan(ne);
-  lds_barrier();  // sums of the loop above have been read
-  if (lane == 63) {
-    sums[0][w] = pg;
-    sums[1][w] = pe;
-  }
-  lds_barrier();
-  for (int i = 0; i < w; ++i) {
-    pg += sums[0][i];
-    pe += sums[1][i];
-  }
-  pg -= ng;
-  pe -= ne;
-  for (int b = t0; b < t1; ++b) {
-    const uint32_t v = key_of(b);
-    const bool in = b >= f && b < l, gt = !in || (some && v > lo), eq = in && some && v == lo;
-    if ((gt || (eq && pe < need)) && pg + min(pe, need) < ch.take) out[pg + min(pe, need)] = b;
-    pg += gt;
-    pe += eq;
+  // keys above lo, and the first `need` of those equal to it: counted for 64 blocks, their places by the sums over those before
+  int pg = 0, pe = 0;
+  for (int c = f; c < l; c += STEP) {
+    if (many) fetch(c);
+    int mine = 0;  // lane u: the numbers of u, 16 bits each
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int g = __popcll(__ballot(k[u] > lo)), e = __popcll(__ballot(k[u] == lo));
+      if (lane == u) mine = g | e << 16;
+    }
+    if (c > f) lds_barrier();  // the counts before have been read
+    if (lane < UN) counts[lane * NW + w] = mine;
+    lds_barrier();
+    int x[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      x[i] = lane * PER + i < UN * NW ? counts[lane * PER + i] : 0;
+      sum += x[i];
+    }
+    const int incl = wave_scan(sum);
+    int start = incl - sum;  // of this wave's count among a lane's
+#pragma unroll
+    for (int i = 0; i + 1 < PER; ++i) start += i < w % PER ? x[i] : 0;
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int s0 = __builtin_amdgcn_readlane(start, (u * NW + w) / PER);
+      const unsigned long long gt = __ballot(k[u] > lo), eq = __ballot(k[u] == lo);
+      const int g = pg + (s0 & 0xFFFF) + (int)__popcll(gt & lower), e = pe + (s0 >> 16) + (int)__popcll(eq & lower), at = f + g + min(e, need);
+      if ((k[u] > lo || (k[u] == lo && e < need)) && at < ch.take) out[at] = c + tid + u * NT;
+    }
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    pg += total & 0xFFFF;
+    pe += total >> 16;
   }
 }
 
@@ -990,7 +1010,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
   u4 raw[QL];
   if (w < FRAGS) {
     const BufRsrc qs = buf_rsrc(qrow + (size_t)plane * a.H * HD, grp * HD * (int)sizeof(T));
-    const uint32_t qo = ((SPARE > 0 && r16 < 2 * SPARE ? r16 % SPARE : r16) * HD + 64 * (qf / 2) + 16 * g + 8 * (qf % 2)) * (uint32_t)sizeof(T);
+    const uint32_t qo = ((SPARE > 0 && r16 < 2 * SPARE ? r16 % (SPARE > 0 ? SPARE : 1) : r16) * HD + 64 * (qf / 2) + 16 * g + 8 * (qf % 2)) * (uint32_t)sizeof(T);
 #pragma unroll
     for (int j = 0; j < QL; ++j) raw[j] = buf_u4(qs, qo + 16 * j);
   }
@@ -1255,8 +1275,7 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
     const int per = (long long)nb * a.Hk * a.R <= 512 * SCORE_NW * (512 / HD) ? SCORE_NW * (512 / HD) : SCORE_BLOCKS;
     launch_k((k_kv8_scores<T, HD>), dim3((nb + per - 1) / per, a.Hk, a.R), dim3(64 * SCORE_NW), 0, s, a, nb, per);
   }
-  const bool wide = nb > 2048;
-  launch_k(wide ? k_kv8_pick<16> : k_kv8_pick<4>, dim3(a.Hk, a.R), dim3(wide ? 1024 : 256), nb <= PICK_LDS_KEYS ? nb * 4 : 0, s, a, nb);
+  launch_k(nb <= 2048 ? k_kv8_pick<2> : k_kv8_pick<16>, dim3(a.Hk, a.R), dim3(1024), 0, s, a, nb);
   return 0;
 }
 template <typename T, int HD>

@@ -395,6 +395,35 @@ def test_equal_scores_take_the_lower_block(ham):
             assert blocks[r, h].tolist() == ref.select(qd, r, h, lens[r], 30, 2, 3), (r, h)
 
 
+# lengths around those at which another kernel, more waves or another pass over the keys takes over
+EDGES = [([6143, 6144, 4127, 1], 6144, 9, 1, 1), ([6175, 6176, 4128, 5000], 6176, 9, 1, 1), ([65567, 65536, 8223, 8256], 65567, 300, 0, 2),
+         ([65568, 65599, 2080, 2111], 65599, 33, 3, 0), ([B * 16384, B * 16387, B * 300], B * 16387, 5, 0, 3),
+         ([B * 33000, B * 16390], B * 33000, 260, 2, 1)]
+
+
+@pytest.mark.parametrize("lens,kv_max,n,first,last", EDGES)
+def test_choice_at_the_edges_of_its_rules(ham, lens, kv_max, n, first, last):
+    s, ref, cache, q, qd = filled(ham, BF16, 2, 1, 64, lens)
+    blocks, count, err = choose(ham, s, q, cache, lens, kv_max, n, first, last)
+    assert err == [0] * len(lens)
+    for r, k in enumerate(lens):
+        want = ref.select(qd, r, 0, k, n, first, last)
+        assert blocks[r, 0].tolist() == want + [-1] * (n - len(want)) and int(count[r, 0]) == len(want)
+
+
+@pytest.mark.parametrize("blocks", [150, 400, 5000, 17000, 40000])
+def test_few_distinct_scores(ham, blocks):
+    lens = [B * blocks]
+    s, ref, cache, q, qd = filled(ham, F32, 1, 1, 64, lens)
+    ref.bounds[:, :, :] = ref.bounds[:, :, :1].clone()
+    g = torch.Generator().manual_seed(3)
+    ref.scales[0, 0, :blocks, 0] = 1.0 + torch.randint(0, 3, (blocks,), generator=g).float()
+    cache.copy_(ref.buf)
+    for n, first, last in ((1, 0, 0), (blocks // 2, 3, 1), (blocks - 1, 0, 0), (blocks // 3, 0, blocks // 3)):
+        got = choose(ham, s, q, cache, lens, lens[0], n, first, last)[0][0, 0].tolist()
+        assert got == ref.select(qd, 0, 0, lens[0], n, first, last)
+
+
 def test_negative_and_nan_scores(ham):
     lens = [B * 1500]
     s, ref, cache, q, qd = filled(ham, F32, 2, 1, 128, lens)
