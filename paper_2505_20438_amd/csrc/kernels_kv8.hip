@@ -224,7 +224,9 @@ __device__ __forceinline__ void write_bounds(const CodeLds<HD>& sh, int d, float
 // new tokens fill it; that of step 0 also puts the tokens past the last full block into the open one, after it has read
 // what the open block held (so no other workgroup touches it).  The other (if q is wanted): q of 32 tokens, 8 pairs a
 // thread.  All of one step of a row run on one XCD (workgroups go round the eight of them), whose L2 then holds the step's
-// RoPE factors: read by every XCD they were a third of all bytes read.
+// RoPE factors: with a row's heads on every XCD 22% more bytes were read.  Bound by memory: 8 kv heads of 128, 4 q-heads each,
+// bf16, 4 rows x 4,001 tokens 133 us (645 MB, 4.9 TB/s; K and V alone 43 us); 32 rows x 1 token 2.8 us, 6.6 where all 256
+// blocks fill up (a chain of loads, maximum, barrier and stores, once).
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) {
   constexpr int B = KV8_BLOCK, HALF = HD / 2, QPS = HALF / 4, THREADS = 2 * HD;  // QPS: quads of pairs per head
@@ -357,6 +359,8 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
 
 // ---------------------------------------------------------------- pack
 // One workgroup per (block, kv head, row): a full block is coded, the slots past the last full block go to the open one.
+// Every value is read once, into registers, and coded from there.  Bound by memory: 4 rows x 8,190 slots, 8 kv heads of 128,
+// bf16, 36 us (134 MB read, 71 written, 5.7 TB/s).
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_kv8_pack(Kv8PackArgs a) {
   constexpr int B = KV8_BLOCK, THREADS = 2 * HD;
@@ -521,7 +525,8 @@ __device__ __forceinline__ void score_blocks(const Kv8SelectArgs& a, int r, int 
 __device__ __forceinline__ float block_score(double twice, float scale) { return (float)(0.5 * twice * (double)scale) + 0.0f; }
 
 // Scores of `per` (at most SCORE_BLOCKS) blocks of a (row, kv head) a workgroup, up to kv_max (blocks that are there, whatever
-// the length).  Bound by fp64 instructions: ~250 of a wave for 512 / hd blocks, ~150 before its first.
+// the length).  Bound by fp64 instructions: ~250 of a wave for 512 / hd blocks, ~150 before its first.  4 rows x 1,040 blocks,
+// 8 kv heads of 128: 7 us (8.5 MB).
 constexpr int SCORE_NW = 4, SCORE_BLOCKS = 64;
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, int nb_max, int per) {
@@ -559,7 +564,9 @@ struct Choice {
 };
 
 // Rows of up to PICK_FEW blocks: one launch.  A workgroup scores the blocks of its (row, kv head); for block b thread b and
-// three more count the blocks that go before it, a quarter of them each.
+// three more count the blocks that go before it, a quarter of them each.  32 rows x 80 blocks, 8 kv heads of 128: 6.1 us,
+// latency.  PICK_FEW, us here / as two launches at 128, 160 and 192 blocks of 128: 1 row 6.7 / 7.0, 7.8 / 7.2, 8.8 / 7.1;
+// 4 rows 7.1 / 7.6, 8.3 / 8.1, 9.2 / 8.4; 32 rows 7.3 / 10.0, 8.5 / 10.8, 9.4 / 11.2; head dim 64 faster here at all of them.
 constexpr int PICK_FEW = 192;
 template <typename T, int HD, int MOST>
 __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int nb_max) {
@@ -609,8 +616,9 @@ __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int 
 // the keys' range in 1,024 bins, the bin in which the count from above reaches the number wanted, and so on within it until
 // it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.
 // Those above the key and the first of those equal to it are then written in the order of the blocks.  The keys stay in
-// registers, UN a thread; rows with more are read again for each step.  Every step is a few dependent instructions and a
-// barrier, which a lone wave issues at one in eight to ten cycles: sixteen waves, not four (1,040 blocks 17 -> 13 us).
+// registers, UN a thread; rows of more than 16 a thread are read again for each step.  Every step is a few dependent instructions and a
+// barrier, and a lone wave issues one instruction in eight to ten cycles: sixteen waves, not four (4 x 1,040 blocks 17 -> 13
+// us with the scores, 12 with the counts shared by the waves).
 constexpr int PICK_BINS = 1024, PICK_CAND = 128;  // counting 256 keys takes as long as three rounds of bins
 // inclusive sum over the lanes up to this one, of a row of 16 and of the wave
 __device__ __forceinline__ int row_scan(int v) {
@@ -1271,11 +1279,13 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
     return 0;
   }
   if (nb > a.n) {
-    // one block a lane group while that leaves a SIMD no more than two waves
+    // one block a lane group while that leaves a SIMD no more than two waves: 1 row x 256 blocks 7.5 us, 8.2 with 64 a workgroup;
+    // 8 rows x 1,040 17.7, 14.5 with 64
     const int per = (long long)nb * a.Hk * a.R <= 512 * SCORE_NW * (512 / HD) ? SCORE_NW * (512 / HD) : SCORE_BLOCKS;
     launch_k((k_kv8_scores<T, HD>), dim3((nb + per - 1) / per, a.Hk, a.R), dim3(64 * SCORE_NW), 0, s, a, nb, per);
   }
-  launch_k(nb <= 2048 ? k_kv8_pick<2> : k_kv8_pick<16>, dim3(a.Hk, a.R), dim3(1024), 0, s, a, nb);
+  // the least that holds the row: 1,040 blocks in 2 keys a thread 11.7 us, in 16 18.8; 4 x 4,096 in 4 20.6, in 8 21.8, in 16 27.0
+  launch_k(nb <= 2048 ? k_kv8_pick<2> : nb <= 4096 ? k_kv8_pick<4> : nb <= 8192 ? k_kv8_pick<8> : k_kv8_pick<16>, dim3(a.Hk, a.R), dim3(1024), 0, s, a, nb);
   return 0;
 }
 template <typename T, int HD>

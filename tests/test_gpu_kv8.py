@@ -398,7 +398,8 @@ def test_equal_scores_take_the_lower_block(ham):
 # lengths around those at which another kernel, more waves or another pass over the keys takes over
 EDGES = [([6143, 6144, 4127, 1], 6144, 9, 1, 1), ([6175, 6176, 4128, 5000], 6176, 9, 1, 1), ([65567, 65536, 8223, 8256], 65567, 300, 0, 2),
          ([65568, 65599, 2080, 2111], 65599, 33, 3, 0), ([B * 16384, B * 16387, B * 300], B * 16387, 5, 0, 3),
-         ([B * 33000, B * 16390], B * 33000, 260, 2, 1)]
+         ([B * 33000, B * 16390], B * 33000, 260, 2, 1), ([B * 4096, B * 4095], B * 4096, 70, 1, 1),
+         ([B * 4097, B * 4096], B * 4097, 70, 1, 1), ([B * 8192, B * 300], B * 8192, 70, 1, 1), ([B * 8193, B * 8192], B * 8193, 70, 1, 1)]
 
 
 @pytest.mark.parametrize("lens,kv_max,n,first,last", EDGES)
