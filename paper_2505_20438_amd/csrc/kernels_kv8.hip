@@ -844,10 +844,10 @@ __device__ __forceinline__ u4 codes_bf16(uint32_t a, uint32_t b) {
 template <int HD>
 struct CodeBlock {
   u4 k[2][HD / 64], v[HD / 32];
-  float ks, vs;
+  float ks, vs;  // by vector loads: a scalar load on its way would be waited for with every read of LDS
   __device__ __forceinline__ void load_k(const uint8_t* codes, const float* scales, int blk) {
     const BufRsrc rs = buf_rsrc(codes + (size_t)max(blk, 0) * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
-    ks = scales[2 * (size_t)max(blk, 0)];
+    ks = buf_f1(buf_rsrc(scales + 2 * (size_t)max(blk, 0), blk < 0 ? 0 : 8), 0);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -856,7 +856,7 @@ struct CodeBlock {
   }
   __device__ __forceinline__ void load_v(const uint8_t* codes, const float* scales, int blk) {
     const BufRsrc rs = buf_rsrc(codes + (size_t)max(blk, 0) * (2 * KV8_BLOCK * HD), blk < 0 ? 0 : 2 * KV8_BLOCK * HD);
-    vs = scales[2 * (size_t)max(blk, 0) + 1];
+    vs = buf_f1(buf_rsrc(scales + 2 * (size_t)max(blk, 0), blk < 0 ? 0 : 8), 4);
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) v[i] = buf_u4_stream(rs, (threadIdx.x & 63) * 16 + KV8_BLOCK * HD + i * 1024);
     __builtin_amdgcn_sched_barrier(0);
@@ -950,19 +950,22 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
   x.load_v(codes, scales, next);
 }
 
-// Waves of a workgroup: four a SIMD with 128 registers each; the fp32 models' three planes take more, so two.
-template <typename T> constexpr int ATT_WAVES = Act<T>::SPLIT ? 16 : 8;
-template <int HD, int GR, int N, int NW>
+// Waves of a workgroup: two a SIMD, and two workgroups a CU (four waves of 128 registers) for a bf16 model.  A SIMD takes its
+// waves' blocks one after the other, the oldest wave first (0.6 us a block at head dim 128), so a few blocks want many CUs:
+// 4 rows x 64 listed blocks 12.9 us with 16 waves, 10.4 with 8, 1 x 4,096 slots 10.5 and 8.4, 4 x 33,300 45.8 and 45.3.
+constexpr int ATT_WAVES = 8;
+template <int HD, int GR, int N>
 struct AttLds {
-  static constexpr int PUB = GR == 16 ? 8 : NW;  // waves that publish their outputs at a time (64 KB)
+  static constexpr int NW = ATT_WAVES;
   u4 qf[HD / 32 * N][64];                      // query fragments, channels in the order of the K codes
   union {
-    float o[PUB][GR][HD];
+    float o[NW][GR][HD];
     float q[GR][HD];                           // queries for the open block, done with before the main loop ends
   };
   float m[NW][16], l[NW][16];
   float v[KV8_BLOCK][HD], p[GR][KV8_BLOCK];    // values and weights of the open block
-  float tm[GR], tl[GR];                        // its maxima and sums
+  float tm[GR], tl[GR];                        // its maxima and sums; in the end its factors, and the sums of all
+  float top[GR];
 };
 
 // One workgroup per (split, kv head, row).  Wave w of NW of split s takes the blocks (or list entries) NW s + w, NW
@@ -970,13 +973,13 @@ struct AttLds {
 // (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split 0 attends over
 // the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
 template <typename T, int HD, int GR, bool LIST>
-__global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
+__global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, PL = Act<T>::PL;
   // a bf16 model's weights have a third plane where the 16 operand rows have room for it: 24 significant bits and not 16
   constexpr int SPARE = N == 2 && GR < 16 ? GR : 0;
-  constexpr int NW = ATT_WAVES<T>, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;            // open block: lanes of a slot, channels a lane
+  constexpr int NW = ATT_WAVES, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;            // open block: lanes of a slot, channels a lane
   constexpr int OUT = (GR * HD + THREADS - 1) / THREADS;  // outputs of a thread
-  __shared__ AttLds<HD, GR, N, NW> sh;
+  __shared__ AttLds<HD, GR, N> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
   const int split = blockIdx.x, kvh = blockIdx.y, r = blockIdx.z, grp = a.grp;
   const size_t pair = (size_t)r * a.Hk + kvh;
@@ -1149,66 +1152,54 @@ __global__ __launch_bounds__(64 * ATT_WAVES<T>) void k_kv8_attn(Kv8AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[d][i] = SPARE == 4 ? pair16_sum(o[d][i]) : pair32_sum(o[d][i]);
   }
-  // per wave: maximum, sum and unnormalised outputs, PUB waves at a time
-  constexpr int PUB = AttLds<HD, GR, N, NW>::PUB;
+  // per wave: maximum, sum and unnormalised outputs
   l = group_sum(l);
   if (g == 0) {
     sh.m[w][r16] = m;
     sh.l[w][r16] = l;
   }
-  float M[OUT], L[OUT], O[OUT];
 #pragma unroll
-  for (int w0 = 0; w0 < NW; w0 += PUB) {
-    if (w0 > 0) lds_barrier();  // the outputs before have been read
-    if (w >= w0 && w < w0 + PUB) {
+  for (int i = 0; i < 4; ++i) {
+    const int j = 4 * g + i;
+    if (j < grp) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = 4 * g + i;
-        if (j < grp) {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) sh.o[w - w0][j][d * 16 + r16] = o[d][i];
-        }
-      }
-    }
-    lds_barrier();
-#pragma unroll
-    for (int k = 0; k < OUT; ++k) {
-      const int t = tid + k * THREADS, j = t / HD, d = t % HD;
-      if (j >= grp) break;
-      if (w0 == 0) {
-        M[k] = rest > 0 ? sh.tm[j] : -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) M[k] = fmaxf(M[k], sh.m[i][j]);
-        L[k] = O[k] = 0.f;
-      }
-      const float mz = M[k] == -INFINITY ? 0.f : M[k];
-#pragma unroll
-      for (int i = 0; i < PUB; ++i) {
-        const float e = __builtin_amdgcn_exp2f(sh.m[w0 + i][j] - mz);  // 0 for a wave without slots
-        // a wave whose scores are all NaN has maximum -inf and sum NaN, which e = 0 keeps
-        L[k] += e * sh.l[w0 + i][j];
-        O[k] += e * sh.o[i][j][d];
-      }
+      for (int d = 0; d < ND; ++d) sh.o[w][j][d * 16 + r16] = o[d][i];
     }
   }
+  lds_barrier();
+  if (tid < 16 * GR) {  // 16 lanes a head: the waves' factors, once
+    const int j = tid / 16, i = tid % 16;
+    const float mi = i < NW ? sh.m[i % NW][j] : -INFINITY, li = i < NW ? sh.l[i % NW][j] : 0.f;
+    const float tm = rest > 0 ? sh.tm[j] : -INFINITY, tl = rest > 0 ? sh.tl[j] : 0.f;
+    const float M = fmaxf(row_max(mi), tm), mz = M == -INFINITY ? 0.f : M;
+    // 0 for a wave without slots; one whose scores are all NaN has maximum -inf and sum NaN, which the factor 0 keeps
+    const float e = __builtin_amdgcn_exp2f(mi - mz), et = __builtin_amdgcn_exp2f(tm - mz);
+    const float L = row_sum(e * li) + et * tl;
+    if (i < NW) sh.m[i][j] = e;
+    if (i == 0) {
+      sh.tm[j] = et;
+      sh.tl[j] = L;
+      sh.top[j] = M;
+    }
+  }
+  lds_barrier();
 #pragma unroll
   for (int k = 0; k < OUT; ++k) {
     const int t = tid + k * THREADS, j = t / HD, d = t % HD;
     if (j >= grp) break;
-    if (rest > 0) {
-      const float e = __builtin_amdgcn_exp2f(sh.tm[j] - (M[k] == -INFINITY ? 0.f : M[k]));
-      L[k] += e * sh.tl[j];
-      O[k] += e * tx[k];
-    }
+    const float L = sh.tl[j];
+    float out = rest > 0 ? sh.tm[j] * tx[k] : 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) out += sh.m[i][j] * sh.o[i][j][d];
     if (a.nsplit == 1) {
-      Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L[k] == 0.f ? 0.f : O[k] / L[k]);
+      Act<T>::put(a.out, r, a.H * HD, (kvh * grp + j) * HD + d, L == 0.f ? 0.f : out / L);
     } else {
       const size_t rec = (pair * a.nsplit + split) * grp + j;
-      a.part[rec * HD + d] = O[k];
+      a.part[rec * HD + d] = out;
       if (d == 0) {
         float* ml = a.part + (size_t)a.R * a.H * a.nsplit * HD + 2 * rec;
-        ml[0] = M[k];
-        ml[1] = L[k];
+        ml[0] = sh.top[j];
+        ml[1] = L;
       }
     }
   }
@@ -1290,12 +1281,11 @@ int select_t(const Kv8SelectArgs& a, Stream s) {
 }
 template <typename T, int HD>
 int attention_t(const Kv8AttnArgs& a, Stream s) {
-  const dim3 grid(a.nsplit, a.Hk, a.R), block(64 * ATT_WAVES<T>);
   const auto kernel = [&](auto list) {
     constexpr bool LIST = decltype(list)::value;
     return a.grp <= 4 ? k_kv8_attn<T, HD, 4, LIST> : a.grp <= 8 ? k_kv8_attn<T, HD, 8, LIST> : k_kv8_attn<T, HD, 16, LIST>;
   };
-  launch_k(a.blocks ? kernel(std::true_type{}) : kernel(std::false_type{}), grid, block, 0, s, a);
+  launch_k(a.blocks ? kernel(std::true_type{}) : kernel(std::false_type{}), dim3(a.nsplit, a.Hk, a.R), dim3(64 * ATT_WAVES), 0, s, a);
   if (a.nsplit > 1) launch_k((k_kv8_combine<T, HD>), dim3(a.grp, a.Hk, a.R), dim3(COMB_THREADS), 0, s, a);
   return 0;
 }

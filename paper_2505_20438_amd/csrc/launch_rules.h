@@ -73,31 +73,33 @@ inline PromptAttnGrid prompt_attn_grid(int R, int s0, int T, int H, int Hkv) {
 }
 
 // Splits of the attention over the 8-bit cache for R rows of Hk kv heads of which the longest reads `blocks` blocks of 32
-// slots.  One workgroup of 16 waves runs per CU.  Its 16 blocks (one a wave) take 2.3 us at head dim 128 and 1.45 at 64
-// alone and half as much again with all 256 CUs at work, but no less than its share of memory: a block of every CU's takes
-// 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk * splits workgroups take ceil(... / 256)
-// rounds, the first 5.4 us and the others 2 beside that, and a split launch 2.5 us more for the combine.  The count with the
-// least estimate, the lowest of equal ones.  8 kv heads of 128, us at the splits here / at 256 / (R * Hk) rounded up:
-// 4 rows x 33,300 slots 45.9 / 48.1, 5 x 33,300 55 / 74, 12 x 4,096 21 / 27, 20 x 4,096 29 / 40, 40 x 4,096 62 / 65 (and
-// 1 x 1,000 11.4 unsplit / 11.5).  The best of 1 .. 48 splits was at most 4% below it at 13 of 15 shapes tried, 7% at two.
-// A row's blocks are shared by its own splits alone, so a long row among short ones is a serial chain (1,040 blocks 155 us
-// unsplit, 48 in four): from 512 blocks on a row gets one split for every 256, up to four; where all rows are long that
-// costs up to a twentieth (32 x 33,300 319 -> 333).
+// slots.  Workgroups of 8 waves, two a CU.  Their 8 blocks (one a wave) take 1.14 us at head dim 128 and 0.75 at 64 alone
+// and half as much again with all 256 CUs at work, as long again for the second workgroup of a CU, but no less than their
+// share of memory: a block of every CU's takes 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk *
+// splits workgroups take ceil(... / 512) rounds, the first 5.4 us (4 at head dim 64) and the others 2 beside that, and a split
+// launch 2.5 us more for the combine.  The count with the least estimate, the lowest of equal ones.
+// 8 kv heads of 128, us at the splits here / at 256 / (R * Hk) rounded up: 4 rows x 33,300 slots 45.1 / 46.6, 5 x 33,300
+// 54 / 71, 12 x 4,096 21 / 27, 20 x 4,096 28 / 37, 40 x 4,096 58 / 62 (and unsplit: 1 x 1,000 9.0 / 10.0, 4 x 64 listed blocks
+// 10.5 / 15.3).  At 23 shapes the best of 1 .. 48 splits was at most 3% below it.
+// A row's blocks are shared by its own splits alone, so a long row among short ones is a serial chain (1,040 blocks 153 us
+// unsplit, 46 in four): from 512 blocks on a row gets one split for every 256, up to four; where all rows are long that
+// costs up to a twentieth (32 x 33,300 314 -> 326).
 constexpr int KV8_MOST_WGS = 1024;  // workgroups of a split launch, unless four splits of every pair are more
 inline int kv8_attn_splits(int R, int Hk, int hd, int blocks) {
   const long long pairs = (long long)R * Hk;
   const int least = std::max(1, std::min(4, blocks / 256));
-  const int most = (int)std::max<long long>(least, std::min<long long>({(blocks + 15) / 16, KV8_MOST_WGS / pairs, MAX_ATTN_SPLIT}));
-  const double wave = hd == 128 ? 2.3 : 1.45, share = hd == 128 ? 0.30 : 0.15;
+  const int most = (int)std::max<long long>(least, std::min<long long>({(blocks + 7) / 8, KV8_MOST_WGS / pairs, MAX_ATTN_SPLIT}));
+  const double wave = hd == 128 ? 1.14 : 0.75, share = hd == 128 ? 0.30 : 0.15, rest = hd == 128 ? 5.4 : 4.0;
   int best = least;
   double best_t = 1e30;
   for (int s = least; s <= most; ++s) {
     const int u = (blocks + s - 1) / s;
-    const double rounds = (double)((pairs * s + 255) / 256), last = (double)(pairs * s) / 256 - (rounds - 1);
-    const auto time = [&](double fill) {
-      return std::max(wave * (1 + 0.55 * fill) * ((u + 15) / 16), share * (0.85 + 0.15 * fill) * u * fill);
+    const long long rounds = (pairs * s + 511) / 512;
+    const auto time = [&](long long wgs) {
+      const double fill = (double)wgs / 256, busy = std::min(fill, 1.0);
+      return std::max(wave * (1 + 0.55 * busy) * ((wgs + 255) / 256) * ((u + 7) / 8), share * (0.85 + 0.15 * busy) * u * fill);
     };
-    const double t = 5.4 + (rounds - 1) * (2 + time(1)) + time(last) + (s > 1 ? 2.5 : 0);
+    const double t = rest + (rounds - 1) * (2 + time(512)) + time(pairs * s - (rounds - 1) * 512) + (s > 1 ? 2.5 : 0);
     if (t < best_t - 1e-9) {
       best_t = t;
       best = s;
