@@ -171,8 +171,9 @@ int ham_op_kv8_info(const ham_kv8_shape* shape, size_t* codes, size_t* scales, s
  *                the new slots (the rest is left as it is), or NULL
  * Codes, scales and bounds of the blocks that fill up, and the open block's new
  * slots, are written, nothing else.  HAM_EINVAL on a bad shape, null or
- * misaligned (16 bytes) pointer or n_tokens outside 1..2^24, HAM_ENOMEM if
- * the cache buffer is too small. */
+ * misaligned (16 bytes) pointer, n_tokens outside 1..2^24, or rows * n_tokens
+ * past one launch (rows * (n_tokens + 31) / 32 * n_kv_heads * head_dim about
+ * 2^30); HAM_ENOMEM if the cache buffer is too small. */
 int ham_op_kv8_append(const ham_kv8_shape* shape, int32_t n_tokens, const float* d_qkv, const float* d_cos,
                       const float* d_sin, const int32_t* d_start, const int32_t* d_count, void* d_cache,
                       size_t cache_bytes, void* d_q, int32_t* d_err, void* hip_stream);

@@ -526,7 +526,7 @@ __device__ __forceinline__ float block_score(double twice, float scale) { return
 
 // Scores of `per` (at most SCORE_BLOCKS) blocks of a (row, kv head) a workgroup, up to kv_max (blocks that are there, whatever
 // the length).  Bound by fp64 instructions: ~250 of a wave for 512 / hd blocks, ~150 before its first.  4 rows x 1,040 blocks,
-// 8 kv heads of 128: 7 us (8.5 MB).
+// 8 kv heads of 128: 7.1 us (8.5 MB).
 constexpr int SCORE_NW = 4, SCORE_BLOCKS = 64;
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, int nb_max, int per) {
@@ -616,9 +616,9 @@ __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int 
 // the keys' range in 1,024 bins, the bin in which the count from above reaches the number wanted, and so on within it until
 // it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.
 // Those above the key and the first of those equal to it are then written in the order of the blocks.  The keys stay in
-// registers, UN a thread; rows of more than 16 a thread are read again for each step.  Every step is a few dependent instructions and a
-// barrier, and a lone wave issues one instruction in eight to ten cycles: sixteen waves, not four (4 x 1,040 blocks 17 -> 13
-// us with the scores, 12 with the counts shared by the waves).
+// registers, UN a thread; rows of more than 16 a thread are read again for each step.  Every step is a few dependent
+// instructions and a barrier, and a lone wave issues one instruction in eight to ten cycles: sixteen waves, not four (4 x
+// 1,040 blocks 17 -> 13 us with the scores, 12 with the counts shared by the waves, of which this kernel 5).
 constexpr int PICK_BINS = 1024, PICK_CAND = 128;  // counting 256 keys takes as long as three rounds of bins
 // inclusive sum over the lanes up to this one, of a row of 16 and of the wave
 __device__ __forceinline__ int row_scan(int v) {
@@ -879,10 +879,11 @@ __device__ __forceinline__ float pair32_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 __device__ __forceinline__ float group_sum(float v) { return pair32_sum(pair16_sum(v)); }
-// Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2,
-// and P V; then x holds block `next`.  q: fragments in LDS (registers would not do for four waves a SIMD).  `scale` is log2(e) / sqrt(hd).  m is that of the row in all four lane groups, l this
-// lane's slots alone.  LIST: a block that is not `there` (zeros) counts for nothing.  SPARE > 0: the operand rows from SPARE on
-// repeat the queries of those before, and take the third plane of their weights in the first product.
+// Scores of the 16 query rows against the block (lane: row r, slots 8 g ..), the softmax update of (m, l, o) in base 2, and
+// P V; then x holds block `next`.  q: fragments in LDS (registers would not do for four waves a SIMD).  `scale` is log2(e) /
+// sqrt(hd).  m is that of the row in all four lane groups, l this lane's slots alone.  LIST: a block that is not `there`
+// (zeros) counts for nothing.  SPARE > 0: the operand rows from SPARE on repeat the queries of those before, and take the
+// third plane of their weights in the first product.
 template <int HD, int N, bool LIST, int SPARE>
 __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64], float scale, float& m, float& l, f4* o,
                                              const uint8_t* codes, const float* scales, int next, bool there) {
@@ -969,15 +970,18 @@ struct AttLds {
 };
 
 // One workgroup per (split, kv head, row).  Wave w of NW of split s takes the blocks (or list entries) NW s + w, NW
-// (s + nsplit) + w, ...: which block is first depends on nothing in memory, so its loads are under way before the row's length is known
-// (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split 0 attends over
-// the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
+// (s + nsplit) + w, ...: which block is first depends on nothing in memory, so its loads are under way before the row's
+// length is known (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split
+// 0 attends over the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
+// A wave's block is 64 conversions and 32 matrix instructions among 290 at head dim 128, for 8.2 KB.  8 kv heads of 128, 4
+// q-heads each, bf16: 4 rows x 33,300 slots 44 us and 32 x 2,560 28 (6.2 TB/s; memory); 4 rows x 64 listed blocks 7.8 and
+// 1 x 700 slots of 8 heads of 64 7.0 (latency: arguments, length or list, blocks, softmax, the waves' sums).
 template <typename T, int HD, int GR, bool LIST>
 __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, PL = Act<T>::PL;
   // a bf16 model's weights have a third plane where the 16 operand rows have room for it: 24 significant bits and not 16
   constexpr int SPARE = N == 2 && GR < 16 ? GR : 0;
-  constexpr int NW = ATT_WAVES, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;            // open block: lanes of a slot, channels a lane
+  constexpr int NW = ATT_WAVES, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;  // open block: lanes of a slot, channels a lane
   constexpr int OUT = (GR * HD + THREADS - 1) / THREADS;  // outputs of a thread
   __shared__ AttLds<HD, GR, N> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
@@ -1206,7 +1210,8 @@ __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_a
 }
 
 // Log-sum-exp combine of the splits of one (row, q-head), in split order.  The outputs are on their way while the weights
-// are formed: one round trip to memory, which with the launch is most of its time.
+// are formed: one round trip to memory, which with the launch is most of its time (4 x 32 heads of 128, 6 or 8 splits: 2.0 to
+// 4.6 us).
 constexpr int COMB_THREADS = 256;
 template <typename T, int HD>
 __global__ __launch_bounds__(COMB_THREADS) void k_kv8_combine(Kv8AttnArgs a) {

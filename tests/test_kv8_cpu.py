@@ -87,6 +87,12 @@ def test_append_refusals(lib, at, value, code):
     assert lib.ham_last_error()
 
 
+def test_append_past_one_launch_is_refused(lib):
+    s = ham.kv8_shape(BF16, 4096, 32, 8, 128, 1 << 24)
+    args = [1 << 20, 256, 256, 256, 256, 256, 256, 1 << 60, 256, 256]
+    assert lib.ham_op_kv8_append(ctypes.byref(s), *args, None) == ham.HAM_EINVAL and b"too large" in lib.ham_last_error()
+
+
 @pytest.mark.parametrize("at,value,code", [
     (0, None, "EINVAL"), (0, 8, "EINVAL"), (1, None, "EINVAL"), (2, 31, "EINVAL"), (2, 0, "EINVAL"), (3, None, "EINVAL"), (4, -1, "EINVAL"),
     (4, 4097, "EINVAL"), (5, None, "EINVAL"), (6, 5, "ENOMEM"), (7, None, "EINVAL")])
