@@ -359,8 +359,8 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
 
 // ---------------------------------------------------------------- pack
 // One workgroup per (block, kv head, row): a full block is coded, the slots past the last full block go to the open one.
-// Every value is read once, into registers, and coded from there.  Bound by memory: 4 rows x 8,190 slots, 8 kv heads of 128,
-// bf16, 36 us (134 MB read, 71 written, 5.7 TB/s).
+// Every value is read once, into registers, and coded from there.  Bound by memory: 4 rows of up to 8,190 slots, 8 kv heads of
+// 128, bf16, 36 us (120 MB read, 62 written, 5.0 TB/s).
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_kv8_pack(Kv8PackArgs a) {
   constexpr int B = KV8_BLOCK, THREADS = 2 * HD;
@@ -974,7 +974,7 @@ struct AttLds {
 // length is known (a cache holds blocks up to kv_max, whatever the length), and rows of any length are shared evenly.  Split
 // 0 attends over the open block too, in fp32 on the vector units (at most 31 slots), while its first blocks are on their way.
 // A wave's block is 64 conversions and 32 matrix instructions among 290 at head dim 128, for 8.2 KB.  8 kv heads of 128, 4
-// q-heads each, bf16: 4 rows x 33,300 slots 44 us and 32 x 2,560 28 (6.2 TB/s; memory); 4 rows x 64 listed blocks 7.8 and
+// q-heads each, bf16: 4 rows x 33,300 slots 45 us and 32 x 2,560 28 (6.0 TB/s; memory); 4 rows x 64 listed blocks 7.8 and
 // 1 x 700 slots of 8 heads of 64 7.0 (latency: arguments, length or list, blocks, softmax, the waves' sums).
 template <typename T, int HD, int GR, bool LIST>
 __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_attn(Kv8AttnArgs a) {
