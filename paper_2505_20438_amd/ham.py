@@ -286,22 +286,34 @@ def ham_op_kv8_info(shape: HamKv8Shape) -> dict:
     return {k: x.value for k, x in zip(("codes", "scales", "bounds", "open"), v)}
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 def _fits(*tensors) -> bool:
-    """Whether tensors hold what a call reads and writes of them: (tensor, bytes) pairs, on a GPU, packed and large enough."""
-    for t, need in tensors:
-        if t.nbytes < need or not t.is_cuda or not t.is_contiguous():
+    """Whether tensors hold what a call reads and writes of them: (tensor, bytes, bytes of a value or 0 for any), on the
+    current device, packed and large enough."""
+    device = tensors[0][0].get_device()
+    for t, need, size in tensors:
+        if t.nbytes < need or size and t.itemsize != size or t.get_device() != device or not t.is_contiguous():
             return False
-    return True
+    return device >= 0 and device == _current_device()
 
 
 def _refuse(**tensors) -> None:
-    for name, (t, need) in tensors.items():
+    for name, (t, need, size) in tensors.items():
         if t.nbytes < need:
             raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
+        if size and t.itemsize != size:
+            raise HamError(HAM_EINVAL, f"{name} holds values of {t.itemsize} bytes, the call reads {size}")
         if not t.is_contiguous():
             raise HamError(HAM_EINVAL, f"{name} must be contiguous")
+    for name, (t, _, _) in tensors.items():
         if not t.is_cuda:
             raise HamError(HAM_EINVAL, f"{name} must be on a GPU")
+        if t.get_device() != _current_device():
+            raise HamError(HAM_EINVAL, f"{name} must be on the current device")
 
 
 def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int) -> None:
@@ -311,10 +323,13 @@ def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q,
     width = (H + 2 * shape.n_kv_heads) * hd
     n = qkv.numel() // (rows * width or 1)
     rope, act, i4 = rows * n * hd * 2, rows * n * H * hd * 4, 4 * rows   # act rows: fp32, or a bf16 hi/lo pair
-    if not (_fits((qkv, rows * n * width * 4), (cos, rope), (sin, rope), (start, i4), (count, i4), (cache, 0), (err, i4))
-            and (q is None or _fits((q, act)))):
-        _refuse(qkv=(qkv, rows * n * width * 4), cos=(cos, rope), sin=(sin, rope), start=(start, i4), count=(count, i4),
-                cache=(cache, 0), err=(err, i4), q=(err if q is None else q, 0 if q is None else act))
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    args = dict(qkv=(qkv, rows * n * width * 4, 4), cos=(cos, rope, 4), sin=(sin, rope, 4), start=(start, i4, 4), count=(count, i4, 4),
+                cache=(cache, 0, 0), err=(err, i4, 4))
+    if q is not None:
+        args["q"] = (q, act, es)
+    if not _fits(*args.values()):
+        _refuse(**args)
     _check(load_library().ham_op_kv8_append(
         ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), start.data_ptr(), count.data_ptr(),
         cache.data_ptr(), cache.nbytes, None if q is None else q.data_ptr(), err.data_ptr(), stream))
@@ -324,9 +339,11 @@ def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, 
     """A filled cache of the storage type, k [rows][n_kv_heads][slots][head_dim] and vt its V tiles, into 8 bits."""
     rows, pairs = shape.rows, shape.rows * shape.n_kv_heads
     slots = k.numel() // (pairs * shape.head_dim or 1)
-    need, i4 = pairs * slots * shape.head_dim * (2 if shape.dtype == HAM_BF16 else 4), 4 * rows
-    if not _fits((k, need), (vt, need), (kv_len, i4), (cache, 0), (err, i4)):
-        _refuse(k=(k, need), vt=(vt, need), kv_len=(kv_len, i4), cache=(cache, 0), err=(err, i4))
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    need, i4 = pairs * slots * shape.head_dim * es, 4 * rows
+    args = dict(k=(k, need, es), vt=(vt, need, es), kv_len=(kv_len, i4, 4), cache=(cache, 0, 0), err=(err, i4, 4))
+    if not _fits(*args.values()):
+        _refuse(**args)
     _check(load_library().ham_op_kv8_pack(
         ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), cache.nbytes,
         err.data_ptr(), stream))
@@ -338,9 +355,11 @@ def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int,
     int32 [rows][n_kv_heads][n_blocks]; how many into ``count`` int32 [rows][n_kv_heads]."""
     i4, act = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4
     lists, counts = i4 * shape.n_kv_heads * n_blocks, i4 * shape.n_kv_heads
-    if not _fits((q, act), (cache, 0), (kv_len, i4), (enable, i4), (blocks, lists), (count, counts), (err, i4), (workspace, 0)):
-        _refuse(q=(q, act), cache=(cache, 0), kv_len=(kv_len, i4), enable=(enable, i4), blocks=(blocks, lists), count=(count, counts),
-                err=(err, i4), workspace=(workspace, 0))
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    args = dict(q=(q, act, es), cache=(cache, 0, 0), kv_len=(kv_len, i4, 4), enable=(enable, i4, 4), blocks=(blocks, lists, 4),
+                count=(count, counts, 4), err=(err, i4, 4), workspace=(workspace, 0, 0))
+    if not _fits(*args.values()):
+        _refuse(**args)
     _check(load_library().ham_op_kv8_select(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         n_blocks, keep_first, keep_last, blocks.data_ptr(), count.data_ptr(), err.data_ptr(), workspace.data_ptr(),
@@ -352,12 +371,17 @@ def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: i
     """Attention of one act row per sequence over an 8-bit cache: every block, or those of ``blocks`` and ``count``
     (ham_op_kv8_select), and the open one."""
     i4, act, pairs = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4, shape.rows * shape.n_kv_heads
-    most = 0 if blocks is None else blocks.numel() // (pairs or 1)
-    if not (_fits((q, act), (cache, 0), (kv_len, i4), (enable, i4), (out, act), (err, i4), (workspace, 0))
-            and (blocks is None or _fits((blocks, 4 * pairs * most))) and (count is None or _fits((count, 4 * pairs)))):
-        _refuse(q=(q, act), cache=(cache, 0), kv_len=(kv_len, i4), enable=(enable, i4), out=(out, act), err=(err, i4),
-                workspace=(workspace, 0), blocks=(err if blocks is None else blocks, 0 if blocks is None else 4 * pairs * most),
-                count=(err if count is None else count, 0 if count is None else 4 * pairs))
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    args = dict(q=(q, act, es), cache=(cache, 0, 0), kv_len=(kv_len, i4, 4), enable=(enable, i4, 4), out=(out, act, es), err=(err, i4, 4),
+                workspace=(workspace, 0, 0))
+    most = 0
+    if blocks is not None:
+        most = blocks.numel() // (pairs or 1)
+        args["blocks"] = (blocks, 4 * pairs * most, 4)
+    if count is not None:
+        args["count"] = (count, 4 * pairs, 4)
+    if not _fits(*args.values()):
+        _refuse(**args)
     _check(load_library().ham_op_kv8_attention(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         None if blocks is None else blocks.data_ptr(), None if count is None else count.data_ptr(), most, out.data_ptr(),

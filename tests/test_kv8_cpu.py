@@ -145,6 +145,11 @@ def test_binding_refuses_tensors_that_are_too_small_or_strided(lib):
             attend(**bad)
     with pytest.raises(ham.HamError, match="on a GPU"):   # host memory never reaches a kernel
         attend()
+    for bad in (dict(kv_len=i32.long()), dict(enable=i32.long()), dict(err=i32.long()), dict(q=torch.zeros(2, 256)),
+                dict(out=torch.zeros(2, 256)), dict(blocks=blocks.long(), count=blocks[:, :, 0].contiguous()),
+                dict(blocks=blocks, count=torch.zeros(2, 2, dtype=torch.int64))):
+        with pytest.raises(ham.HamError, match="values of"):  # lengths in 64 bits, rows of the other storage type
+            attend(**bad)
     for bad in (dict(cos=cs[:1]), dict(sin=cs[:, :, ::2]), dict(start=i32[:1]), dict(q=q[:1]), dict(qkv=qkv[:1])):
         a = dict(qkv=qkv, cos=cs, sin=cs, start=i32, count=i32, cache=cache, q=q, err=i32, stream=0)
         with pytest.raises(ham.HamError):
