@@ -288,10 +288,10 @@ def ham_op_kv8_info(shape: HamKv8Shape) -> dict:
 
 def _current_device() -> int:
     import torch
-    return torch.cuda.current_device()
+    return torch._C._cuda_getDevice()   # of a process that holds a tensor on a GPU
 
 
-def _fits(*tensors) -> bool:
+def _fits(tensors) -> bool:
     """Whether tensors hold what a call reads and writes of them: (tensor, bytes, bytes of a value or 0 for any), on the
     current device, packed and large enough."""
     device = tensors[0][0].get_device()
@@ -301,15 +301,15 @@ def _fits(*tensors) -> bool:
     return device >= 0 and device == _current_device()
 
 
-def _refuse(**tensors) -> None:
-    for name, (t, need, size) in tensors.items():
+def _refuse(names: str, tensors) -> None:
+    for name, (t, need, size) in zip(names.split(), tensors):
         if t.nbytes < need:
             raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
         if size and t.itemsize != size:
             raise HamError(HAM_EINVAL, f"{name} holds values of {t.itemsize} bytes, the call reads {size}")
         if not t.is_contiguous():
             raise HamError(HAM_EINVAL, f"{name} must be contiguous")
-    for name, (t, _, _) in tensors.items():
+    for name, (t, _, _) in zip(names.split(), tensors):
         if not t.is_cuda:
             raise HamError(HAM_EINVAL, f"{name} must be on a GPU")
         if t.get_device() != _current_device():
@@ -324,12 +324,11 @@ def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q,
     n = qkv.numel() // (rows * width or 1)
     rope, act, i4 = rows * n * hd * 2, rows * n * H * hd * 4, 4 * rows   # act rows: fp32, or a bf16 hi/lo pair
     es = 2 if shape.dtype == HAM_BF16 else 4
-    args = dict(qkv=(qkv, rows * n * width * 4, 4), cos=(cos, rope, 4), sin=(sin, rope, 4), start=(start, i4, 4), count=(count, i4, 4),
-                cache=(cache, 0, 0), err=(err, i4, 4))
+    args = ((qkv, rows * n * width * 4, 4), (cos, rope, 4), (sin, rope, 4), (start, i4, 4), (count, i4, 4), (cache, 0, 0), (err, i4, 4))
     if q is not None:
-        args["q"] = (q, act, es)
-    if not _fits(*args.values()):
-        _refuse(**args)
+        args += ((q, act, es),)
+    if not _fits(args):
+        _refuse("qkv cos sin start count cache err q", args)
     _check(load_library().ham_op_kv8_append(
         ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), start.data_ptr(), count.data_ptr(),
         cache.data_ptr(), cache.nbytes, None if q is None else q.data_ptr(), err.data_ptr(), stream))
@@ -341,9 +340,9 @@ def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, 
     slots = k.numel() // (pairs * shape.head_dim or 1)
     es = 2 if shape.dtype == HAM_BF16 else 4
     need, i4 = pairs * slots * shape.head_dim * es, 4 * rows
-    args = dict(k=(k, need, es), vt=(vt, need, es), kv_len=(kv_len, i4, 4), cache=(cache, 0, 0), err=(err, i4, 4))
-    if not _fits(*args.values()):
-        _refuse(**args)
+    args = ((k, need, es), (vt, need, es), (kv_len, i4, 4), (cache, 0, 0), (err, i4, 4))
+    if not _fits(args):
+        _refuse("k vt kv_len cache err", args)
     _check(load_library().ham_op_kv8_pack(
         ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), cache.nbytes,
         err.data_ptr(), stream))
@@ -356,10 +355,10 @@ def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int,
     i4, act = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4
     lists, counts = i4 * shape.n_kv_heads * n_blocks, i4 * shape.n_kv_heads
     es = 2 if shape.dtype == HAM_BF16 else 4
-    args = dict(q=(q, act, es), cache=(cache, 0, 0), kv_len=(kv_len, i4, 4), enable=(enable, i4, 4), blocks=(blocks, lists, 4),
-                count=(count, counts, 4), err=(err, i4, 4), workspace=(workspace, 0, 0))
-    if not _fits(*args.values()):
-        _refuse(**args)
+    args = ((q, act, es), (cache, 0, 0), (kv_len, i4, 4), (enable, i4, 4), (blocks, lists, 4), (count, counts, 4), (err, i4, 4),
+            (workspace, 0, 0))
+    if not _fits(args):
+        _refuse("q cache kv_len enable blocks count err workspace", args)
     _check(load_library().ham_op_kv8_select(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         n_blocks, keep_first, keep_last, blocks.data_ptr(), count.data_ptr(), err.data_ptr(), workspace.data_ptr(),
@@ -372,16 +371,15 @@ def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: i
     (ham_op_kv8_select), and the open one."""
     i4, act, pairs = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4, shape.rows * shape.n_kv_heads
     es = 2 if shape.dtype == HAM_BF16 else 4
-    args = dict(q=(q, act, es), cache=(cache, 0, 0), kv_len=(kv_len, i4, 4), enable=(enable, i4, 4), out=(out, act, es), err=(err, i4, 4),
-                workspace=(workspace, 0, 0))
+    args = ((q, act, es), (cache, 0, 0), (kv_len, i4, 4), (enable, i4, 4), (out, act, es), (err, i4, 4), (workspace, 0, 0))
     most = 0
     if blocks is not None:
         most = blocks.numel() // (pairs or 1)
-        args["blocks"] = (blocks, 4 * pairs * most, 4)
+        args += ((blocks, 4 * pairs * most, 4),)
     if count is not None:
-        args["count"] = (count, 4 * pairs, 4)
-    if not _fits(*args.values()):
-        _refuse(**args)
+        args += ((count, 4 * pairs, 4),)
+    if not _fits(args):
+        _refuse("q cache kv_len enable out err workspace" + ("" if blocks is None else " blocks") + " count", args)
     _check(load_library().ham_op_kv8_attention(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         None if blocks is None else blocks.data_ptr(), None if count is None else count.data_ptr(), most, out.data_ptr(),
