@@ -808,8 +808,8 @@ __global__ __launch_bounds__(1024) void k_kv8_pick(Kv8SelectArgs a, int nb_max) 
 }
 
 // ---------------------------------------------------------------- attention
-// bf16 planes of an fp32 operand: v = p0 + p1 (+ p2), 16 or 24 significant bits.  A bf16 model's activations are pairs
-// anyway; with three planes the products of an fp32 model lose nothing, as codes are exact in bf16.
+// bf16 planes of an fp32 operand: v = p0 + p1 (+ p2), 16 or 24 significant bits.  Queries have the planes of the model's
+// activations, two where those are pairs and three in fp32: nothing of them is lost, as codes are exact in bf16.
 template <typename T> struct Planes;
 template <> struct Planes<bf16> { static constexpr int N = 2; };
 template <> struct Planes<float> { static constexpr int N = 3; };
@@ -930,8 +930,8 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
     l += p[e];
     p[e] *= vs;
   }
-  u4 pp[SPARE > 0 ? 3 : N];
-  to_planes<(SPARE > 0 ? 3 : N)>(p, pp);
+  u4 pp[3];
+  to_planes<3>(p, pp);
   if constexpr (SPARE > 0) {
     const bool third = threadIdx.x & SPARE;
 #pragma unroll
@@ -946,7 +946,7 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
     for (int h = 0; h < 2; ++h) {
       const u4 v = codes_bf16(x.v[i][2 * h], x.v[i][2 * h + 1]);
 #pragma unroll
-      for (int n = 0; n < N; ++n) Frag<bf16>::mma(o[2 * i + h], pp[n], v);
+      for (int n = 0; n < (SPARE > 0 ? 2 : 3); ++n) Frag<bf16>::mma(o[2 * i + h], pp[n], v);
     }
   x.load_v(codes, scales, next);
 }
@@ -979,7 +979,8 @@ struct AttLds {
 template <typename T, int HD, int GR, bool LIST>
 __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_attn(Kv8AttnArgs a) {
   constexpr int N = Planes<T>::N, NF = HD / 32, ND = HD / 16, B = KV8_BLOCK, PL = Act<T>::PL;
-  // a bf16 model's weights have a third plane where the 16 operand rows have room for it: 24 significant bits and not 16
+  // the weights' third plane (24 significant bits; with 16 the outputs were 3 times as far off) shares the first one's product
+  // where a bf16 model's queries leave half of the 16 operand rows
   constexpr int SPARE = N == 2 && GR < 16 ? GR : 0;
   constexpr int NW = ATT_WAVES, THREADS = 64 * NW, LPS = THREADS / B, CPL = HD / LPS;  // open block: lanes of a slot, channels a lane
   constexpr int OUT = (GR * HD + THREADS - 1) / THREADS;  // outputs of a thread
