@@ -9,7 +9,7 @@
 //
 // k_kv8_append   RoPE of projection rows, K and V into the cache, q out.
 // k_kv8_pack     a filled cache of the storage type into the 8-bit cache.
-// k_kv8_scores, k_kv8_pick   the blocks whose keys' upper bounds are greatest.
+// k_kv8_scores, k_kv8_pick   the blocks whose keys' upper bounds are greatest (k_kv8_pick_few: short rows in one launch).
 // k_kv8_attn, k_kv8_combine  attention of one query row per sequence over all or listed blocks and the open one.
 #include <algorithm>
 #include <type_traits>

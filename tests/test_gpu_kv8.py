@@ -636,3 +636,31 @@ def test_offsets_beyond_32_bits(ham):
             k, v = torch.cat([k, opened[1, h, 0, :lens[1] % B].double()]), torch.cat([v, opened[1, h, 1, :lens[1] % B].double()])
             ref = (torch.softmax(k @ qd[1, h] / hd ** 0.5, 0) @ v).cpu()
             assert float((out[1, h] - ref).abs().max()) <= FILLED_TOL[BF16] * float(ref.square().mean().sqrt()), h
+
+
+def test_two_graphs_share_a_workspace(ham):
+    lens = [20000, 9001]
+    s, ref, cache, q, _ = filled(ham, BF16, 16, 2, 64, lens)
+    n, on, err = i32(lens), i32([1, 1]), i32([0, 0])
+    ws = torch.zeros(ham.ham_op_kv8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    blocks, count = torch.zeros(2, 2, 30, dtype=torch.int32, device=DEV), torch.zeros(2, 2, dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(q)
+    calls = [lambda: ham.ham_op_kv8_select(s, q, cache, n, on, 20000, 30, 1, 1, blocks, count, err, ws, stream()),
+             lambda: ham.ham_op_kv8_attention(s, q, cache, n, on, 20000, None, None, out, err, ws, stream())]
+    graphs, side = [torch.cuda.CUDAGraph() for _ in calls], torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for graph, call in zip(graphs, calls):
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    for i in range(6):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)))
+        for call in calls:
+            call()
+        want = blocks.clone(), count.clone(), out.clone()
+        for t in (blocks, count, out):
+            t.zero_()
+        for graph in (graphs if i % 2 else graphs[::-1]):
+            graph.replay()
+        for a, b in zip(want, (blocks, count, out)):
+            assert torch.equal(a, b), i
+    assert err.tolist() == [0, 0]
