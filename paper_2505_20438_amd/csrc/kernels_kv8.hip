@@ -225,7 +225,7 @@ __device__ __forceinline__ void write_bounds(const CodeLds<HD>& sh, int d, float
 // what the open block held (so no other workgroup touches it).  The other (if q is wanted): q of 32 tokens, 8 pairs a
 // thread.  All of one step of a row run on one XCD (workgroups go round the eight of them), whose L2 then holds the step's
 // RoPE factors: with a row's heads on every XCD 22% more bytes were read.  Bound by memory: 8 kv heads of 128, 4 q-heads each,
-// bf16, 4 rows x 4,001 tokens 133 us (645 MB, 4.9 TB/s; K and V alone 43 us); 32 rows x 1 token 2.8 us, 6.6 where all 256
+// bf16, 4 rows x 4,001 tokens 133 us (645 MB, 4.9 TB/s; K and V alone 43 us); 32 rows x 1 token 2.8 us, 5.7 where all 256
 // blocks fill up (a chain of loads, maximum, barrier and stores, once).
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) {
@@ -286,6 +286,14 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
       const int t = max(base + kt.slot, 0);
       const float* p = ksrc + (size_t)t * ld + kt.d0;
       f4 x[4], y[4], c[4], sv[4];
+      Raw<T, 4> ox[4], oy[4];
+      if (base < 0) {  // the row's first block: slots from the open one
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ox[i].load(open + kt.slot * HD + kt.d0 + 4 * i);
+          oy[i].load(open + kt.slot * HD + kt.d0 + HALF + 4 * i);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[i] = *reinterpret_cast<const f4*>(p + 4 * i);
@@ -300,9 +308,12 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
         rotate(x[i], y[i], c[i], sv[i]);
         x[i] = stored4<T>(x[i]);
         y[i] = stored4<T>(y[i]);
-        if (base < 0 && base + kt.slot < 0) {  // the row's first block: slots from the open one
-          x[i] = ld4<T>(open + kt.slot * HD + kt.d0 + 4 * i);
-          y[i] = ld4<T>(open + kt.slot * HD + kt.d0 + HALF + 4 * i);
+        if (base < 0 && base + kt.slot < 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[i][e] = ox[i].at(e);
+            y[i][e] = oy[i].at(e);
+          }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -319,15 +330,22 @@ __global__ __launch_bounds__(2 * HD) void k_kv8_append(Kv8AppendArgs a, int nb) 
     } else {  // V: channels d .. d + 3 of slots 8 g ..
       const int d = (tid - HD) % (HD / 4) * 4, g = (tid - HD) / (HD / 4);
       f4 v[8];
+      Raw<T, 4> ov[8];
       uint32_t top = 0;
+      if (base < 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ov[i].load(open + (B + 8 * g + i) * HD + d);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f4*>(vsrc + (size_t)max(base + 8 * g + i, 0) * ld + d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         v[i] = stored4<T>(v[i]);
-        if (base < 0 && base + 8 * g + i < 0) v[i] = ld4<T>(open + (B + 8 * g + i) * HD + d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = magnitude(top, v[i][e]);
+        for (int e = 0; e < 4; ++e) {
+          if (base < 0 && base + 8 * g + i < 0) v[i][e] = ov[i].at(e);
+          top = magnitude(top, v[i][e]);
+        }
       }
       wave_top(sh.top, top);
       __syncthreads();
@@ -567,6 +585,7 @@ struct Choice {
 // three more count the blocks that go before it, a quarter of them each.  32 rows x 80 blocks, 8 kv heads of 128: 6.1 us,
 // latency.  PICK_FEW, us here / as two launches at 128, 160 and 192 blocks of 128: 1 row 6.7 / 7.0, 7.8 / 7.2, 8.8 / 7.1;
 // 4 rows 7.1 / 7.6, 8.3 / 8.1, 9.2 / 8.4; 32 rows 7.3 / 10.0, 8.5 / 10.8, 9.4 / 11.2; head dim 64 faster here at all of them.
+// MOST: the workgroup that just holds the row (32 rows x 80 blocks 6.1 us with 8 waves for 128 blocks, 6.8 with 16 for 256).
 constexpr int PICK_FEW = 192;
 template <typename T, int HD, int MOST>
 __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int nb_max) {
