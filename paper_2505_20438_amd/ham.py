@@ -291,22 +291,29 @@ def _current_device() -> int:
     return torch._C._cuda_getDevice()   # of a process that holds a tensor on a GPU
 
 
-def _fits(tensors) -> bool:
-    """Whether tensors hold what a call reads and writes of them: (tensor, bytes, bytes of a value or 0 for any), on the
-    current device, packed and large enough."""
+def _rows_as_read(t, rows: int, need: int) -> bool:
+    """Whether a tensor of another size than the call's `need` bytes holds more rows of the same extent: a call reads row r
+    at r * need / rows, which in a tensor of longer rows is another place."""
+    return t.nbytes > need and t.dim() > 0 and t.nbytes * rows == need * t.shape[0]
+
+
+def _fits(rows: int, tensors) -> bool:
+    """Whether tensors hold what a call reads and writes of them: (tensor, bytes of `rows` rows or 0 for any number, bytes of a
+    value or 0 for any), on the current device, packed, and rows where the call expects them."""
     device = tensors[0][0].get_device()
     for t, need, size in tensors:
-        if t.nbytes < need or size and t.itemsize != size or t.get_device() != device or not t.is_contiguous():
+        if (need and t.nbytes != need and not _rows_as_read(t, rows, need) or size and t.itemsize != size
+                or t.get_device() != device or not t.is_contiguous()):
             return False
     return device >= 0 and device == _current_device()
 
 
-def _refuse(names: str, tensors) -> None:
+def _refuse(rows: int, names: str, tensors) -> None:
     for name, (t, need, size) in zip(names.split(), tensors):
-        if t.nbytes < need:
-            raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
         if size and t.itemsize != size:
             raise HamError(HAM_EINVAL, f"{name} holds values of {t.itemsize} bytes, the call reads {size}")
+        if need and t.nbytes != need and not _rows_as_read(t, rows, need):
+            raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need} ({rows} rows, or more of the same extent)")
         if not t.is_contiguous():
             raise HamError(HAM_EINVAL, f"{name} must be contiguous")
     for name, (t, _, _) in zip(names.split(), tensors):
@@ -316,33 +323,44 @@ def _refuse(names: str, tensors) -> None:
             raise HamError(HAM_EINVAL, f"{name} must be on the current device")
 
 
-def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int) -> None:
+def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int, n_tokens=None) -> None:
     """RoPE and append of ``count[r]`` slots per row (include/ham_ops.h): qkv fp32 [rows][n_tokens][...], q act rows of
-    the same tokens or None."""
+    the same tokens or None.  ``n_tokens`` is taken from qkv if not given: its first dimension is then ``rows``."""
     rows, hd, H = shape.rows, shape.head_dim, shape.n_heads
     width = (H + 2 * shape.n_kv_heads) * hd
-    n = qkv.numel() // (rows * width or 1)
+    n = n_tokens
+    if n is None:
+        if qkv.dim() == 0 or qkv.shape[0] != rows:
+            raise HamError(HAM_EINVAL, f"qkv's first dimension must be the {rows} rows, or n_tokens given")
+        n = qkv.numel() // (rows * width or 1)
     rope, act, i4 = rows * n * hd * 2, rows * n * H * hd * 4, 4 * rows   # act rows: fp32, or a bf16 hi/lo pair
     es = 2 if shape.dtype == HAM_BF16 else 4
     args = ((qkv, rows * n * width * 4, 4), (cos, rope, 4), (sin, rope, 4), (start, i4, 4), (count, i4, 4), (cache, 0, 0), (err, i4, 4))
     if q is not None:
         args += ((q, act, es),)
-    if not _fits(args):
-        _refuse("qkv cos sin start count cache err q", args)
+    if not _fits(rows, args):
+        _refuse(rows, "qkv cos sin start count cache err q", args)
     _check(load_library().ham_op_kv8_append(
         ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), start.data_ptr(), count.data_ptr(),
         cache.data_ptr(), cache.nbytes, None if q is None else q.data_ptr(), err.data_ptr(), stream))
 
 
-def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, stream: int) -> None:
-    """A filled cache of the storage type, k [rows][n_kv_heads][slots][head_dim] and vt its V tiles, into 8 bits."""
-    rows, pairs = shape.rows, shape.rows * shape.n_kv_heads
-    slots = k.numel() // (pairs * shape.head_dim or 1)
+def ham_op_kv8_pack(shape: HamKv8Shape, k, vt, kv_len, kv_max: int, cache, err, stream: int, src_slots=None) -> None:
+    """A filled cache of the storage type, k [rows][n_kv_heads][slots][head_dim] and vt its V tiles, into 8 bits.
+    ``src_slots`` (slots of a row of k and vt) is taken from k's dimensions if not given; of a k without them (a flat view of
+    a state buffer) it is the shape's slots_cap."""
+    rows, Hk, hd = shape.rows, shape.n_kv_heads, shape.head_dim
+    pairs, slots = rows * Hk, src_slots
+    if slots is None:
+        if k.dim() >= 4 and k.shape[1] == Hk:
+            slots = k.numel() // (k.shape[0] * Hk * hd or 1)
+        else:
+            slots = k.shape[1] if k.dim() == 3 and k.shape[0] == pairs else shape.slots_cap
     es = 2 if shape.dtype == HAM_BF16 else 4
-    need, i4 = pairs * slots * shape.head_dim * es, 4 * rows
+    need, i4 = pairs * slots * hd * es, 4 * rows
     args = ((k, need, es), (vt, need, es), (kv_len, i4, 4), (cache, 0, 0), (err, i4, 4))
-    if not _fits(args):
-        _refuse("k vt kv_len cache err", args)
+    if not _fits(rows, args):
+        _refuse(rows, "k vt kv_len cache err", args)
     _check(load_library().ham_op_kv8_pack(
         ctypes.byref(shape), k.data_ptr(), vt.data_ptr(), slots, kv_len.data_ptr(), kv_max, cache.data_ptr(), cache.nbytes,
         err.data_ptr(), stream))
@@ -357,8 +375,8 @@ def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int,
     es = 2 if shape.dtype == HAM_BF16 else 4
     args = ((q, act, es), (cache, 0, 0), (kv_len, i4, 4), (enable, i4, 4), (blocks, lists, 4), (count, counts, 4), (err, i4, 4),
             (workspace, 0, 0))
-    if not _fits(args):
-        _refuse("q cache kv_len enable blocks count err workspace", args)
+    if not _fits(shape.rows, args):
+        _refuse(shape.rows, "q cache kv_len enable blocks count err workspace", args)
     _check(load_library().ham_op_kv8_select(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         n_blocks, keep_first, keep_last, blocks.data_ptr(), count.data_ptr(), err.data_ptr(), workspace.data_ptr(),
@@ -367,19 +385,19 @@ def ham_op_kv8_select(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int,
 
 def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: int, blocks, count, out, err, workspace,
                          stream: int) -> None:
-    """Attention of one act row per sequence over an 8-bit cache: every block, or those of ``blocks`` and ``count``
-    (ham_op_kv8_select), and the open one."""
+    """Attention of one act row per sequence over an 8-bit cache: every block, or those of ``blocks`` [rows][n_kv_heads][most]
+    and ``count`` (ham_op_kv8_select), and the open one."""
     i4, act, pairs = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4, shape.rows * shape.n_kv_heads
     es = 2 if shape.dtype == HAM_BF16 else 4
     args = ((q, act, es), (cache, 0, 0), (kv_len, i4, 4), (enable, i4, 4), (out, act, es), (err, i4, 4), (workspace, 0, 0))
     most = 0
     if blocks is not None:
-        most = blocks.numel() // (pairs or 1)
+        most = blocks.shape[-1] if blocks.dim() else 0
         args += ((blocks, 4 * pairs * most, 4),)
     if count is not None:
         args += ((count, 4 * pairs, 4),)
-    if not _fits(args):
-        _refuse("q cache kv_len enable out err workspace" + ("" if blocks is None else " blocks") + " count", args)
+    if not _fits(shape.rows, args):
+        _refuse(shape.rows, "q cache kv_len enable out err workspace" + ("" if blocks is None else " blocks") + " count", args)
     _check(load_library().ham_op_kv8_attention(
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         None if blocks is None else blocks.data_ptr(), None if count is None else count.data_ptr(), most, out.data_ptr(),

@@ -163,6 +163,41 @@ def test_pack_writes_what_it_says_and_nothing_else(ham, dtype, Hk, hd, lens, S):
     assert torch.equal(cache.cpu(), ref.buf) and err.tolist() == [0] * R
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_buffers_for_more_rows(ham, given):
+    # two of the three rows that every buffer has room for, with the extents taken from the tensors' dimensions or given
+    R, H, Hk, hd, S, n = 3, 4, 2, 64, 1024, 5
+    s, all_rows = (ham.kv8_shape(BF16, r, H, Hk, hd, S) for r in (2, R))
+    g = torch.Generator().manual_seed(14)
+    K, V = (torch.randn(R, Hk, S, hd, generator=g).to(torch.bfloat16) for _ in range(2))
+    lens = [900, 777]
+    ref, cache = new_cache(ham, s)
+    vt, err = tiled_v(torch, V).to(DEV), i32([0] * R)
+    ham.ham_op_kv8_pack(s, K.to(DEV), vt, i32(lens + [900]), S, cache, err, stream(), S if given else None)
+    x = tokens(g, all_rows, 40)
+    q = torch.full((R, 40, 2 * H * hd), 7.0, dtype=torch.bfloat16, device=DEV)
+    if given:
+        ham.ham_op_kv8_append(s, *(t.reshape(R, 40, -1).to(DEV) for t in x), i32(lens + [0]), i32([40, 33, 40]), cache, q, err, stream(), 40)
+    else:
+        append(ham, s, [t[:2] for t in x], lens, [40, 33], cache, err, q)
+    _, k, v = rotated(x, all_rows)
+    for r, m in enumerate((40, 33)):
+        ref.append(r, 0, K[r, :, :lens[r]].transpose(0, 1).double(), V[r, :, :lens[r]].transpose(0, 1).double())
+        ref.append(r, lens[r], k[r, :m], v[r, :m])
+    assert torch.equal(cache.cpu(), ref.buf) and torch.all(q[2] == 7.0) and torch.all(q[0] != 7.0) and err.tolist() == [0] * R
+    lens = [940, 810]
+    qa = act_rows(torch, torch.randn(R, H * hd, generator=g).to(DEV), BF16)
+    qd = from_act(torch, qa, H * hd, BF16).double().cpu().view(R, H, hd)[:2]
+    blocks, count = (torch.full(d, 77, dtype=torch.int32, device=DEV) for d in ((R, Hk, n), (R, Hk)))
+    out, on = torch.full_like(qa, 7.0), i32([1] * R)
+    ws = torch.zeros(ham.ham_op_kv8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    ham.ham_op_kv8_select(s, qa, cache, i32(lens), on, 940, n, 0, 0, blocks, count, err, ws, stream())
+    ham.ham_op_kv8_attention(s, qa, cache, i32(lens), on, 940, blocks, count, out, err, ws, stream())
+    pairs = [[ref.select(qd, r, h, lens[r], n) for h in range(Hk)] for r in range(2)]
+    assert blocks[:2].tolist() == pairs and torch.all(blocks[2] == 77) and torch.all(out[2] == 7.0) and err.tolist() == [0] * R
+    near(from_act(torch, out, H * hd, BF16).double().cpu().view(R, H, hd)[:2], ref.attention(qd, lens, pairs), BF16)
+
+
 def test_pack_of_a_length_out_of_range_writes_nothing(ham):
     s = ham.kv8_shape(BF16, 3, 4, 2, 64, 96)
     ref, cache = new_cache(ham, s)

@@ -156,6 +156,69 @@ def test_binding_refuses_tensors_that_are_too_small_or_strided(lib):
             ham.ham_op_kv8_append(s, *dict(a, **bad).values())
 
 
+def host(*dims, dtype=torch.int32):
+    return torch.zeros(*dims, dtype=dtype)
+
+
+def test_binding_refuses_rows_of_another_extent(lib):
+    # a call reads row r at r times the extent that its shape gives; where a tensor's rows are longer (a list buffer with room
+    # for more blocks, a prompt's q rows), or where its size leaves the extent open (a flat buffer for more rows), it would read
+    # other data without an error.  Host tensors: what passes these checks ends with "on a GPU".
+    s = ham.kv8_shape(BF16, 2, 4, 2, 64, 64)
+    i32, bf = host(2), torch.bfloat16
+    cache = host(ham.ham_op_kv8_cache_bytes(s), dtype=torch.uint8)
+    ws = host(ham.ham_op_kv8_workspace_bytes(s), dtype=torch.uint8)
+    q, W = host(2, 512, dtype=bf), 512
+
+    def attend(**kw):
+        a = dict(q=q, cache=cache, kv_len=i32, enable=i32, kv_max=64, blocks=None, count=None, out=q, err=i32, workspace=ws, stream=0)
+        ham.ham_op_kv8_attention(s, *dict(a, **kw).values())
+
+    def select(n, **kw):
+        a = dict(q=q, cache=cache, kv_len=i32, enable=i32, kv_max=64, n_blocks=n, keep_first=0, keep_last=0, blocks=host(2, 2, n),
+                 count=host(2, 2), err=i32, workspace=ws, stream=0)
+        ham.ham_op_kv8_select(s, *dict(a, **kw).values())
+
+    def append(n_tokens=None, **kw):
+        a = dict(qkv=torch.zeros(2, 3, 512), cos=torch.zeros(2, 3, 32), sin=torch.zeros(2, 3, 32), start=i32, count=i32, cache=cache,
+                 q=host(2, 3, 512, dtype=bf), err=i32, stream=0)
+        ham.ham_op_kv8_append(s, *dict(a, **kw).values(), n_tokens)
+
+    def pack(src_slots=None, **kw):
+        a = dict(k=host(2, 2, 96, 64, dtype=bf), vt=host(2, 2, 3, 64, 32, dtype=bf), kv_len=i32, kv_max=64, cache=cache, err=i32, stream=0)
+        ham.ham_op_kv8_pack(s, *dict(a, **kw).values(), src_slots)
+
+    lists, counts = host(2, 2, 2), host(2, 2)
+    refused = [
+        (attend, dict(q=host(2, 3, W, dtype=bf))), (attend, dict(q=host(2, 2 * W, dtype=bf))), (attend, dict(out=host(3, W + 128, dtype=bf))),
+        (attend, dict(blocks=host(3 * 2 * 2), count=counts)), (attend, dict(blocks=host(2, 4), count=counts)),
+        (attend, dict(blocks=host(2, 3, 2), count=counts)), (attend, dict(blocks=lists, count=host(2, 3))),
+        (select, dict(n=1, blocks=host(2, 2, 2))), (select, dict(n=2, blocks=host(12))), (select, dict(n=1, count=host(2, 3))),
+        (append, dict(qkv=torch.zeros(4, 3, 512))), (append, dict(qkv=torch.zeros(6, 512))), (append, dict(qkv=torch.zeros(2, 3, 520))),
+        (append, dict(qkv=torch.zeros(2 * 3 * 512))), (append, dict(cos=torch.zeros(2, 4, 32))), (append, dict(sin=torch.zeros(2, 3, 64))),
+        (append, dict(q=host(2, 5, 512, dtype=bf))), (append, dict(n_tokens=2)), (append, dict(n_tokens=4)),
+        (pack, dict(k=host(4 * 2 * 64 * 64, dtype=bf), vt=host(4 * 2 * 64 * 64, dtype=bf))), (pack, dict(vt=host(2, 2, 4, 64, 32, dtype=bf))),
+        (pack, dict(k=host(2, 96, 2, 64, dtype=bf))), (pack, dict(src_slots=64)), (pack, dict(src_slots=192)), (pack, dict(k=host(2, 4, 96, 64, dtype=bf)))]
+    for call, kw in refused:
+        with pytest.raises(ham.HamError) as e:
+            call(**kw)
+        assert e.value.code == ham.HAM_EINVAL and "on a GPU" not in str(e.value), (call.__name__, kw.keys(), str(e.value))
+    taken = [   # exact sizes whatever the dimensions, and more rows of the same extent
+        (attend, {}), (attend, dict(q=host(5, W, dtype=bf), out=host(4, 1, W, dtype=bf), kv_len=host(7), blocks=host(3, 2, 2), count=host(3, 2))),
+        (attend, dict(q=host(2 * W, dtype=bf), blocks=lists, count=counts)), (attend, dict(blocks=host(4, 2), count=host(4))),
+        (select, dict(n=2)), (select, dict(n=2, blocks=host(5, 2, 2), count=host(5, 2))), (select, dict(n=2, blocks=host(8))),
+        (append, {}), (append, dict(qkv=torch.zeros(2, 3, 8, 64), cos=torch.zeros(4, 3, 32), q=None)), (append, dict(q=host(3, 3, 512, dtype=bf))),
+        (append, dict(qkv=torch.zeros(6, 512), n_tokens=3)), (append, dict(qkv=torch.zeros(3, 3, 512), n_tokens=3)),
+        (append, dict(qkv=torch.zeros(2, 512), cos=torch.zeros(2, 32), sin=torch.zeros(2, 32), q=q)),
+        (pack, {}), (pack, dict(k=host(4, 2, 96, 64, dtype=bf), vt=host(4, 2, 3, 64, 32, dtype=bf))), (pack, dict(src_slots=96)),
+        (pack, dict(k=host(4, 96, 64, dtype=bf))), (pack, dict(k=host(2, 2, 3, 32, 64, dtype=bf))),
+        (pack, dict(k=host(2 * 2 * 64 * 64, dtype=bf), vt=host(2 * 2 * 64 * 64, dtype=bf))),
+        (pack, dict(k=host(2 * 2 * 96 * 64, dtype=bf), vt=host(2 * 2 * 96 * 64, dtype=bf), src_slots=96))]
+    for call, kw in taken:
+        with pytest.raises(ham.HamError, match="on a GPU"):
+            call(**kw)
+
+
 @pytest.fixture(scope="module")
 def splits():
     """kv8_attn_splits of csrc/launch_rules.h, compiled on its own."""
