@@ -192,8 +192,9 @@ int ham_op_kv8_pack(const ham_kv8_shape* shape, const void* d_k, const void* d_v
  *   scale_K * sum_d max(q_d least_d, q_d greatest_d),
  * an upper bound of q . k over its keys, summed in fp64 and rounded to fp32:
  * no key of a block that is left out scores above the least score chosen.
- * Equal scores: the lower block first; NaN counts as greatest.  The first
- * keep_first and the last keep_last closed blocks are always chosen.
+ * Equal scores: the lower block first.  A block whose K or V holds an infinity
+ * or NaN scores NaN, which counts as greatest.  The first keep_first and the last
+ * keep_last closed blocks are always chosen.
  *  d_q         act rows [rows][n_heads*head_dim], RoPE applied
  *  kv_max      host upper bound of kv_len
  *  d_blocks    int32 [rows][n_kv_heads][n_blocks], ascending, then -1

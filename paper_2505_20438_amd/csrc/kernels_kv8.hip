@@ -540,6 +540,11 @@ __device__ __forceinline__ void score_blocks(const Kv8SelectArgs& a, int r, int 
     }
   }
 }
+// K's scale, or NaN for a block whose K or V holds an infinity or NaN: the block is then among the chosen and is seen
+__device__ __forceinline__ float score_scale(const float* scales, size_t blk) {
+  const float2 s = *reinterpret_cast<const float2*>(scales + 2 * blk);
+  return s.y != s.y ? s.y : s.x;
+}
 __device__ __forceinline__ float block_score(double twice, float scale) { return (float)(0.5 * twice * (double)scale) + 0.0f; }
 
 // Scores of `per` (at most SCORE_BLOCKS) blocks of a (row, kv head) a workgroup, up to kv_max (blocks that are there, whatever
@@ -552,7 +557,7 @@ __global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, i
   const int kvh = blockIdx.y, r = blockIdx.z, b0 = blockIdx.x * per, b1 = min(nb_max, b0 + per);
   const size_t pair = (size_t)r * a.Hk + kvh;
   const int i = threadIdx.x;
-  const float scale = i < b1 - b0 ? a.c.scales[2 * (pair * a.c.NB + b0 + i)] : 0.f;
+  const float scale = i < b1 - b0 ? score_scale(a.c.scales, pair * a.c.NB + b0 + i) : 0.f;
   score_blocks<T, HD, SCORE_NW>(a, r, kvh, pair, b0, b1, [&](int b, double v, bool first) {
     best[b - b0] = first ? v : max_nan(best[b - b0], v);
   });
@@ -561,7 +566,7 @@ __global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, i
 }
 
 // The n best blocks of a (row, kv head), in the order of their indices.  Equal scores: the lower index.  A NaN (a block
-// with an infinity or NaN) counts as greatest, so that it is read and seen.  Blocks [f, l) are chosen by score, those before
+// with an infinity or NaN in K or V) counts as greatest, so that it is read and seen.  Blocks [f, l) are chosen by score, those before
 // and after are always taken.
 __device__ __forceinline__ uint32_t score_key(float s) {
   const uint32_t u = __float_as_uint(s);
@@ -595,7 +600,7 @@ __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int 
   __shared__ int wsum[MOST / 64], parts[PARTS][MOST];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kvh = blockIdx.x, r = blockIdx.y, n = a.kv_len[r], on = a.enable[r];
   const size_t pair = (size_t)r * a.Hk + kvh;
-  const float scale = tid < nb_max ? a.c.scales[2 * (pair * a.c.NB + tid)] : 0.f;
+  const float scale = tid < nb_max ? score_scale(a.c.scales, pair * a.c.NB + tid) : 0.f;
   score_blocks<T, HD, MOST / 16>(a, r, kvh, pair, 0, nb_max, [&](int b, double v, bool first) {
     best[b] = first ? v : max_nan(best[b], v);
   });

@@ -124,7 +124,8 @@ class Cache:
         lo, hi = b[:, :, 0].reshape(-1, 1, hd), b[:, :, 1].reshape(-1, 1, hd)
         qs = q[r, h * H // Hk:(h + 1) * H // Hk]
         top = torch.maximum(qs * lo, qs * hi).sum(-1).amax(1) if n // B else torch.zeros(0, dtype=torch.float64)
-        return (top * self.scales[r, h, :n // B, 0].double()).float()
+        s = self.scales[r, h, :n // B].double()
+        return (top * torch.where(torch.isnan(s[:, 1]), s[:, 1], s[:, 0])).float()
 
     def select(self, q, r, h, n, n_blocks, first=0, last=0):
         s = self.scores(q, r, h, n).double()

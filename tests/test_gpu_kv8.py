@@ -471,6 +471,26 @@ def test_negative_and_nan_scores(ham):
     assert choose(ham, s, q, cache, lens, lens[0], 2)[0][0, 0].tolist() == [40, 1200]
 
 
+@pytest.mark.parametrize("dtype,blocks", [(BF16, 20), (BF16, 128), (F32, 192), (BF16, 193), (F32, 1500), (BF16, 5000)])
+def test_a_nan_value_is_among_the_chosen_and_seen(ham, dtype, blocks):
+    # blocks of which V alone holds a NaN, whose keys score lowest; in one launch (up to 192 blocks) and in two
+    lens = [B * blocks + 3, B * blocks]
+    s, ref, cache, q, qd = filled(ham, dtype, 4, 2, 64, lens)
+    bad = [blocks // 3, blocks - 2]
+    ref.scales[0, 1, bad, 1] = float("nan")
+    ref.bounds[0, 1, bad] = 0
+    ref.bounds[0, 1, bad[0]] = 0x80
+    cache.copy_(ref.buf)
+    for n in (2, 5):
+        chosen, count, err = choose(ham, s, q, cache, lens, max(lens), n)
+        for r in range(2):
+            for h in range(2):
+                assert chosen[r, h].tolist() == ref.select(qd, r, h, lens[r], n), (n, r, h)
+        assert set(bad) <= set(chosen[0, 1].tolist()) and err == [0, 0]
+        got, _ = attend(ham, s, q, cache, lens, max(lens), chosen, count)
+        assert torch.isnan(got).all(-1).tolist() == [[False, False, True, True], [False] * 4]
+
+
 def test_no_key_of_a_block_left_out_beats_the_least_chosen_score(ham):
     lens = [4000, 1700]
     s, ref, cache, q, qd = filled(ham, BF16, 8, 2, 128, lens)
