@@ -3,9 +3,9 @@ to fp32, the storage type and e4m3 exactly where it says so.
 
 Tolerances.  Cache contents (codes, scales, bounds, open block, rotated q) are rounded step by step by the definition: they
 are held to it bit for bit, and so are chosen blocks (scores are fp64 sums; an fp32 rounding of two such sums in different
-order can differ only where they straddle a border, at 2^-53 against 2^-24).  Attention: FILLED_TOL of attention_bounds.py,
-whose terms are the same here (probabilities and outputs as hi/lo pairs, fp32 scores over the head dim; fp32 models: three
-bf16 planes, 24 bits).
+order can differ only where they straddle a border, at 2^-53 against 2^-24).  Attention: FILLED_TOL of attention_bounds.py, which
+a lost or doubled slot exceeds; the terms here are smaller (weights of 24 significant bits, outputs as hi/lo pairs or fp32,
+fp32 scores over the head dim).  kv8_planes.py has the bounds that a lost bf16 plane exceeds.
 """
 import numpy as np
 import torch

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from synth.configs import BF16, F32
-from tests import kv8_ref
+from tests import kv8_planes, kv8_ref
 from tests.attention_bounds import FILLED_TOL
 from tests.gpu_util import act_rows, from_act, tiled_v
 from tests.kv8_ref import B, F8, Cache, act64, rope64, storage, stored
@@ -298,6 +298,25 @@ def test_attention_over_every_slot(ham, dtype, H, Hk, hd, lens):
     assert err == [0] * len(lens)
     got, err = attend(ham, s, q, cache, lens, s.slots_cap)   # a loose bound: another split
     near(got, want, dtype)
+
+
+# q-heads to a kv head from 1 to 16: rows of the matrix products that carry the weights' third plane, and none left for it
+PLANES = [(BF16, 4, 4, 64), (BF16, 9, 3, 128), (BF16, 8, 2, 128), (BF16, 8, 2, 64), (BF16, 10, 2, 128), (BF16, 16, 2, 64),
+          (BF16, 9, 1, 64), (BF16, 13, 1, 128), (BF16, 16, 1, 64), (F32, 4, 4, 64), (F32, 8, 2, 128), (F32, 16, 2, 64), (F32, 16, 1, 128)]
+
+
+@pytest.mark.parametrize("lens", [[4100, 333], [220, 192]])
+@pytest.mark.parametrize("dtype,H,Hk,hd", PLANES)
+def test_no_bf16_plane_is_lost(ham, dtype, H, Hk, hd, lens):
+    # over every slot, split and not, and over listed blocks
+    for pairs in (True, False):
+        s, ref, q, qd = kv8_planes.inputs(ham, dtype, H, Hk, hd, lens, pairs)
+        q, cache = q.to(DEV), ref.buf.to(DEV)
+        some = [[sorted(range(h % 2, n // B, 2)) for h in range(Hk)] for n in lens]
+        for lists in (None, some):
+            got, err = attend(ham, s, q, cache, lens, max(lens), *((None, None) if lists is None else lists_of(lists, lens[0] // B)))
+            part = kv8_planes.errors(got, *kv8_planes.expected(ref, qd, lens, lists), dtype)
+            assert float(part.max()) <= 1.0 and err == [0, 0], (pairs, lists is None, part)
 
 
 def test_rows_switched_off_or_out_of_range_are_zero(ham):
