@@ -104,6 +104,68 @@ def test_append_writes_what_it_says_and_nothing_else(ham, dtype, H, Hk, hd, star
     assert torch.equal(cache.cpu(), again)
 
 
+@pytest.mark.parametrize("dtype,H,Hk,hd,start,count,T", APPENDS)
+def test_append_without_q_writes_the_same_cache(ham, dtype, H, Hk, hd, start, count, T):
+    R = len(start)
+    s = ham.kv8_shape(dtype, R, H, Hk, hd, (max(a + b for a, b in zip(start, count)) + 31) // 32 * 32)
+    ref, cache = new_cache(ham, s)
+    g = torch.Generator().manual_seed(15)
+    ref.open.copy_(torch.randn(ref.open.shape, generator=g).to(storage(dtype)))
+    cache.copy_(ref.buf)
+    x, err = tokens(g, s, T), i32([0] * R)
+    append(ham, s, x, start, count, cache, err, None)
+    _, k, v = rotated(x, s)
+    for r in range(R):
+        ref.append(r, start[r], k[r, :count[r]], v[r, :count[r]])
+    assert torch.equal(cache.cpu(), ref.buf) and err.tolist() == [0] * R
+
+
+def same(a, b):
+    """Equal values (not bits: a zero's sign, a NaN's payload)."""
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+
+@pytest.mark.parametrize("dtype,hd", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+def test_append_of_extreme_values(ham, dtype, hd):
+    # as test_blocks_of_extreme_values; K and V of one head each, in old slots of the open block and in new tokens
+    s = ham.kv8_shape(dtype, 1, 4, 2, hd, 32 * 9)
+    ref, cache = new_cache(ham, s)
+    g = torch.Generator().manual_seed(16)
+    ref.open[0, :, :, :20] = torch.randn(2, 2, 20, hd, generator=g).to(storage(dtype))
+    ref.open[0, 0, 0, 3, 5] = float("inf")
+    ref.open[0, 1, 1, 19, hd - 1] = float("nan")
+    cache.copy_(ref.buf)
+    qkv, c, sn = tokens(g, s, 250)
+    k, v = qkv[0, :, 4:6], qkv[0, :, 6:8]
+
+    def block(b):
+        return slice(32 * b - 20, 32 * b + 12)
+    k[block(1), 0], v[block(1), 0] = 0, -0.0
+    k[block(2)] *= 1e-37
+    v[block(2), 1] *= 1e-40
+    k[block(3)] *= 5e37
+    v[block(3)] *= 1e-30
+    k[32 * 4 - 20 + 7, 0, 1] = float("nan")
+    v[32 * 4 - 20 + 31, 1, 0] = float("-inf")
+    k[32 * 5 - 20, 1, hd // 2] = float("inf")
+    v[block(6), 0] = torch.linspace(-1, 1, hd)
+    v[32 * 8 - 20 + 2, 0, 9] = float("nan")      # stays in the open block
+    k[32 * 8 - 20 + 3, 1, 9] = float("inf")
+    x, err = (qkv, c, sn), i32([0])
+    append(ham, s, x, [20], [250], cache, err)
+    _, k, v = rotated(x, s)
+    ref.append(0, 20, k[0], v[0])
+    got = Cache(s, ham.ham_op_kv8_info(s), cache.numel(), cache.cpu())
+    closed = 270 // B
+    scales, want = got.scales[0, :, :closed], ref.scales[0, :, :closed]
+    assert same(scales, want)
+    assert torch.isnan(want).nonzero().tolist() == [[0, 0, 0], [0, 4, 0], [1, 0, 1], [1, 4, 1], [1, 5, 0]]
+    fine = ~torch.isnan(want)
+    assert same(got.codes[0, :, :closed][fine].view(F8).float(), ref.codes[0, :, :closed][fine].view(F8).float())
+    assert same(got.bounds[0, :, :closed][fine[..., 0]].view(F8).float(), ref.bounds[0, :, :closed][fine[..., 0]].view(F8).float())
+    assert same(got.open[0, :, :, :270 % B].float(), ref.open[0, :, :, :270 % B].float()) and err.tolist() == [0]
+
+
 @pytest.mark.parametrize("dtype,hd,cuts", [(BF16, 128, [1] * 70), (BF16, 64, [31, 1, 2, 36]), (F32, 64, [33, 31, 6]), (BF16, 128, [70])])
 def test_the_cache_does_not_depend_on_how_its_slots_arrive(ham, dtype, hd, cuts):
     s = ham.kv8_shape(dtype, 2, 6, 2, hd, 96)
