@@ -76,10 +76,8 @@ struct Raw {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
       }
-    } else if constexpr (W == 1) {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-      static_assert(W == 2, "4, 8 or a multiple of 16 bytes");
+      static_assert(W == 2, "8 or a multiple of 16 bytes");
       const uint2 v = *reinterpret_cast<const uint2*>(p);
       w[0] = v.x;
       w[1] = v.y;
@@ -1029,6 +1027,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_a
   // this thread's share of the open block: slot ts, channels tc ..
   const int ts = tid / LPS, tc = tid % LPS * CPL;
   static_assert(GR * HD / 4 <= THREADS, "four query channels a thread");
+  static_assert(LPS == 16, "row_sum adds up the lanes of a slot");
   Raw<T, CPL> tk, tv;
   Raw<T, 4> tq[PL];
   const T* qrow = (const T*)a.q + (size_t)r * PL * a.H * HD + kvh * grp * HD;  // hi plane of the kv head's q-heads
@@ -1118,7 +1117,6 @@ __global__ __launch_bounds__(64 * ATT_WAVES, Act<T>::SPLIT ? 4 : 2) void k_kv8_a
 #pragma unroll
       for (int e = 0; e < CPL; ++e) s += sh.q[j][tc + e] * tk.at(e);
       s = row_sum(s);
-      if constexpr (LPS == 32) s += __shfl_xor(s, 16, WAVE);
       if (tid % LPS == 0) sh.p[j][ts] = ts < rest ? s * scale : -INFINITY;
     }
     lds_barrier();
