@@ -1,15 +1,18 @@
 /*
- * libham single-kernel entry points, for parity tests and diagnostics.
+ * libham single-operator entry points, on caller-provided buffers.
  *
- * They run one kernel of the decode loop on caller-provided buffers, so a test
- * can check one step at shapes where running the whole model through a CPU
- * reference is too slow (e.g. attention over a 32K-slot cache):
+ * The first ones run one kernel of the decode loop, for parity tests and
+ * diagnostics: a test can check one step at shapes where running the whole model
+ * through a CPU reference is too slow (e.g. attention over a 32K-slot cache):
  *  - ham_op_attention_step runs the fused decode-attention step that every
  *    base layer of ham_macro_step launches, with the same split choice for the
  *    same batch and slot bound;
  *  - ham_op_decode_attention runs the attention over an already filled cache
  *    that a prompt batch's last base layer and the micro decoder's first step
  *    use (a different kernel).
+ * The ham_op_kv8_* operators are for a decode loop of the caller's own: they keep
+ * a KV cache in 8 bits, which ham_prefill and ham_macro_step neither write nor
+ * read (ham_op_kv8_pack takes what a prefill left).
  * Same conventions as include/ham.h: C functions, HAM_OK or a negative
  * HAM_E* code, ham_last_error() for the message, "d_" = device pointers, work
  * enqueued on `hip_stream` and valid after it is synchronised.
@@ -124,7 +127,12 @@ int ham_op_attention_step_splits(int32_t dtype, int32_t rows, int32_t n_kv_heads
  * The slots past the last full block (kv_len % 32) are in the open block, in the
  * storage type.  A block is coded once, when its 32nd slot arrives, so the cache
  * is the same, bit for bit, whether its slots came one by one or together.  A
- * row may be shortened by slots of its open block, or to a multiple of 32.
+ * row may be shortened by slots of its open block, or to a multiple of 32; at any
+ * other lower kv_len the open block holds other slots than those past the last
+ * full block, and what is read of it is wrong.  So each query row attends over the
+ * slots its cache holds at the time: there is no causal attention of a prompt's
+ * rows over this cache (a prompt appended in one call has its own attention, for
+ * which ham_op_kv8_append gives q, before or beside it; or goes token by token).
  *
  * The cache is one caller-owned buffer of ham_op_kv8_cache_bytes bytes, 256-byte
  * aligned; it needs no clearing.  Regions (ham_op_kv8_info), pair = row *
@@ -143,7 +151,10 @@ int ham_op_attention_step_splits(int32_t dtype, int32_t rows, int32_t n_kv_heads
  * is one without slots.  Other streams or host threads may read one cache at
  * the same time, with workspaces and outputs of their own; a call that writes
  * it is ordered against them by the caller.  Nothing is allocated and no call
- * waits for the GPU: all of them can be captured into a graph. */
+ * waits for the GPU: all of them can be captured into a graph.  A workspace needs
+ * no clearing and keeps nothing between calls.  kv_max is a bound that a captured
+ * graph keeps: ham_op_kv8_select scores blocks up to it whatever the lengths, and
+ * ham_op_kv8_attention splits its work, and so orders its sums, by it. */
 #define HAM_KV8_BLOCK 32
 
 typedef struct ham_kv8_shape {
@@ -208,7 +219,9 @@ int ham_op_kv8_select(const ham_kv8_shape* shape, const void* d_q, const void* d
 /* GQA attention of one query row per sequence:
  *   out[r, h] = softmax_j(q[r, h] . K[r, h/(H/Hkv), j] / sqrt(hd)) V[...]
  * over the slots j < kv_len[r] of every closed block, or with d_blocks of the
- * listed ones, and of the open block.  A row without slots gets zeros.
+ * listed ones, and of the open block.  A row without slots, or whose scores are all
+ * -infinity, gets zeros.  Weights times V's scale are sums of three bf16 values, 24
+ * bits while V's magnitudes are above 1e-31 and fewer below.
  *  d_blocks, d_n_blocks  lists as ham_op_kv8_select writes them, max_blocks
  *              entries apart, or both NULL: an entry that is not above the one
  *              before it or not a closed block of the row is left out, a count

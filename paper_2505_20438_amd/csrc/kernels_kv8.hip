@@ -546,8 +546,9 @@ __device__ __forceinline__ float score_scale(const float* scales, size_t blk) {
 __device__ __forceinline__ float block_score(double twice, float scale) { return (float)(0.5 * twice * (double)scale) + 0.0f; }
 
 // Scores of `per` (at most SCORE_BLOCKS) blocks of a (row, kv head) a workgroup, up to kv_max (blocks that are there, whatever
-// the length).  Bound by fp64 instructions: ~250 of a wave for 512 / hd blocks, ~150 before its first.  4 rows x 1,040 blocks,
-// 8 kv heads of 128: 7.1 us (8.5 MB).
+// the length).  Bound by latency: ~150 instructions of a wave before its first 512 / hd blocks, then ~250, most of them fp64, in
+// chains for each of them, with about two waves a SIMD at 4 rows.  4 rows x 1,040 blocks, 8 kv heads of 128: 7.0 us (8.8 MB),
+// of which the 1.72 M vector instructions take 2.8 to issue (four cycles each, 1,024 SIMDs).
 constexpr int SCORE_NW = 4, SCORE_BLOCKS = 64;
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * SCORE_NW) void k_kv8_scores(Kv8SelectArgs a, int nb_max, int per) {
@@ -638,7 +639,8 @@ __global__ __launch_bounds__(4 * MOST) void k_kv8_pick_few(Kv8SelectArgs a, int 
 // the keys' range in 1,024 bins, the bin in which the count from above reaches the number wanted, and so on within it until
 // it holds few enough keys to count for each what lies above it (after one round, unless many are equal), or one value.
 // Those above the key and the first of those equal to it are then written in the order of the blocks.  The keys stay in
-// registers, UN a thread; rows of more than 16 a thread are read again for each step.  Every step is a few dependent
+// registers, UN a thread (at 16 the masks of the ballots overflow the scalar registers: 76 are kept in a vector register); rows
+// of more than 16 a thread are read again for each step.  Every step is a few dependent
 // instructions and a barrier, and a lone wave issues one instruction in eight to ten cycles: sixteen waves, not four (4 x
 // 1,040 blocks 17 -> 13 us with the scores, 12 with the counts shared by the waves, of which this kernel 5).
 constexpr int PICK_BINS = 1024, PICK_CAND = 128;  // counting 256 keys takes as long as three rounds of bins
@@ -973,7 +975,8 @@ __device__ __forceinline__ void attend_block(CodeBlock<HD>& x, const u4 (*q)[64]
   x.load_v(codes, scales, next);
 }
 
-// Waves of a workgroup: two a SIMD, and two workgroups a CU (four waves of 128 registers) for a bf16 model.  A SIMD takes its
+// Waves of a workgroup: two a SIMD, and two workgroups a CU (four waves of 128 registers) for a bf16 model with up to 8 q-heads a
+// kv head.  At head dim 128 one workgroup a CU with 16 (93 KB of LDS) and in fp32 (140 registers and more).  A SIMD takes its
 // waves' blocks one after the other, the oldest wave first (0.6 us a block at head dim 128), so a few blocks want many CUs:
 // 4 rows x 64 listed blocks 12.9 us with 16 waves, 10.4 with 8, 1 x 4,096 slots 10.5 and 8.4, 4 x 33,300 45.8 and 45.3.
 constexpr int ATT_WAVES = 8;

@@ -73,7 +73,9 @@ inline PromptAttnGrid prompt_attn_grid(int R, int s0, int T, int H, int Hkv) {
 }
 
 // Splits of the attention over the 8-bit cache for R rows of Hk kv heads of which the longest reads `blocks` blocks of 32
-// slots.  Workgroups of 8 waves, two a CU.  Their 8 blocks (one a wave) take 1.14 us at head dim 128 and 0.75 at 64 alone
+// slots.  Workgroups of 8 waves, two a CU (as a bf16 model's with up to 8 q-heads a kv head at head dim 128; with 9 to 16, or in
+// fp32, registers or LDS leave one there, and at head dim 64 three fit: for those the rule is the same and was not fitted).
+// Their 8 blocks (one a wave) take 1.14 us at head dim 128 and 0.75 at 64 alone
 // and half as much again with all 256 CUs at work, as long again for the second workgroup of a CU, but no less than their
 // share of memory: a block of every CU's takes 0.30 us (7 TB/s; 5% less at three CUs of four) at 128, half at 64.  R * Hk *
 // splits workgroups take ceil(... / 512) rounds, the first 5.4 us (4 at head dim 64) and the others 2 beside that, and a split

@@ -381,6 +381,35 @@ def test_no_bf16_plane_is_lost(ham, dtype, H, Hk, hd, lens):
             assert float(part.max()) <= 1.0 and err == [0, 0], (pairs, lists is None, part)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_values_of_1e_30(ham, dtype):
+    # weights times V's scale, in three bf16 planes, are normal numbers down to there: errors scale with the values
+    lens = [1500, 220]
+    s, ref, q, qd = kv8_planes.inputs(ham, dtype, 8, 2, 64, lens, True)
+    ref.scales[..., 1] *= 2.0 ** -100
+    ref.open[:, :, 1] *= 2.0 ** -100
+    got, _ = attend(ham, s, q.to(DEV), ref.buf.to(DEV), lens, 1500)
+    part = kv8_planes.errors(got, *kv8_planes.expected(ref, qd, lens), dtype)
+    assert float(part.max()) <= 1.0, part
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scores_of_minus_infinity(ham, dtype):
+    # keys of -infinity in the open block: alone they leave zeros, beside others they count for nothing
+    lens = [3, 20, 64 + 5, 31]
+    s, ref, cache, q, _ = filled(ham, dtype, 8, 2, 64, lens)
+    for r, slots in ((0, 3), (1, 7), (2, 5), (3, 31)):
+        ref.open[r, :, 0, :slots] = float("-inf")
+    cache.copy_(ref.buf)
+    q = act_rows(torch, 0.1 + torch.rand(4, 8 * 64, generator=torch.Generator().manual_seed(17)), dtype).to(DEV)
+    qd = from_act(torch, q, 8 * 64, dtype).double().cpu().view(4, 8, 64)
+    got, err = attend(ham, s, q, cache, lens, max(lens))
+    want = ref.attention(qd, lens)
+    assert torch.isnan(want[[0, 3]]).all()   # 0 / 0
+    near(got, torch.nan_to_num(want), dtype)
+    assert err == [0] * 4
+
+
 def test_rows_switched_off_or_out_of_range_are_zero(ham):
     lens = [100, 64, 70, 200, 130]
     s, ref, cache, q, qd = filled(ham, BF16, 8, 2, 64, lens)
