@@ -131,8 +131,8 @@ int ham_op_attention_step_splits(int32_t dtype, int32_t rows, int32_t n_kv_heads
  * other lower kv_len the open block holds other slots than those past the last
  * full block, and what is read of it is wrong.  So each query row attends over the
  * slots its cache holds at the time: there is no causal attention of a prompt's
- * rows over this cache (a prompt appended in one call has its own attention, for
- * which ham_op_kv8_append gives q, before or beside it; or goes token by token).
+ * rows over this cache.  The caller attends over such a prompt by other means
+ * (ham_op_kv8_append gives its rotated q), or appends it token by token.
  *
  * The cache is one caller-owned buffer of ham_op_kv8_cache_bytes bytes, 256-byte
  * aligned; it needs no clearing.  Regions (ham_op_kv8_info), pair = row *
