@@ -1,8 +1,8 @@
 """Timed cases of the operators on a paged KV cache (``ham_op_paged_*``), beside their plain forms.
 
 A layer's pool holds pages of ``page_slots`` slots of every kv head, K and V in the storage type; row r's slot s lies in page
-``table[r][s // page_slots]``, and ``refs`` counts the rows that hold a page.  Kinds of case, by the entry point that a pass
-calls:
+``table[r][s // page_slots]`` (K of 16 slots in the order of the matrix cores' rows), and ``refs`` counts the rows that hold a
+page.  Kinds of case, by the entry point that a pass calls:
 
 * ``append``   RoPE of packed projection rows of sequences of different lengths, K and V into pages (``ham_op_paged_append``)
 * ``attn``     attention of one query row per sequence over its pages (``ham_op_paged_attention``)
@@ -125,7 +125,7 @@ def _to_page(k, v, case):
     """K and V [..., page, hd] in the order of the pool, [..., 2, page * hd]."""
     lead, P, hd, E = k.shape[:-2], case["page"], case["hd"], _unit(case)
     n = len(lead)
-    k = k.reshape(*lead, P // 16, 16, hd // E, E).transpose(n + 1, n + 2).reshape(*lead, P * hd)
+    k = k.reshape(*lead, P // 16, 2, 2, 4, hd // E, E).permute(*range(n), n, n + 4, n + 2, n + 1, n + 3, n + 5).reshape(*lead, P * hd)
     v = v.reshape(*lead, P // E, E, hd).transpose(n + 1, n + 2).reshape(*lead, P * hd)
     return torch.stack([k, v], n)
 
@@ -135,7 +135,7 @@ def _from_page(x, case):
     lead, P, hd, E = x.shape[:-2], case["page"], case["hd"], _unit(case)
     n = len(lead)
     k, v = x[..., 0, :], x[..., 1, :]
-    k = k.reshape(*lead, P // 16, hd // E, 16, E).transpose(n + 1, n + 2).reshape(*lead, P, hd)
+    k = k.reshape(*lead, P // 16, hd // E, 2, 2, 4, E).permute(*range(n), n, n + 3, n + 2, n + 4, n + 1, n + 5).reshape(*lead, P, hd)
     v = v.reshape(*lead, P // E, hd, E).transpose(n + 1, n + 2).reshape(*lead, P, hd)
     return k, v
 
@@ -241,8 +241,8 @@ def prepare(case, seed):
 def _workspace_bytes(case):
     """What a caller keeps for the kernels' intermediate records: at least ham_op_paged_workspace_bytes."""
     row_pages, n_pages = _capacity(case)
-    R, pairs = case["rows"], case["rows"] * case["Hk"]
-    return (2048 + 5 * pairs) * (case["H"] // case["Hk"]) * (case["hd"] + 2) * 4 + (R * row_pages + 4 * n_pages + 16 * R) * 4 + (1 << 16)
+    R, pairs, group = case["rows"], case["rows"] * case["Hk"], case["H"] // case["Hk"]
+    return max((2048 + 5 * pairs) * group, 1 << 17) * (case["hd"] + 2) * 4 + (R * row_pages + 4 * n_pages + 16 * R) * 4 + (1 << 16)
 
 
 # ---------------------------------------------------------------- one pass, plain
@@ -270,7 +270,7 @@ def _plain_append(s):
     page = s["table"][row, slot // P].long()
     at = (slot % P).long()[:, None]
     d = torch.arange(hd, device=DEV)
-    k_at = (at // 16 * (hd // E) + d // E) * 16 * E + at % 16 * E + d % E
+    k_at = ((at // 16 * (hd // E) + d // E) * 16 + at // 4 % 2 * 8 + at // 8 % 2 * 4 + at % 4) * E + d % E
     v_at = (at // E * hd + d) * E + at % E
     first = (page[:, None] * Hk + torch.arange(Hk, device=DEV))[..., None] * (2 * P * hd)
     pool = s["pool"].view(-1)
@@ -473,7 +473,8 @@ def _row64(s, r, n):
     hd, P, E = case["hd"], case["page"], _unit(case)
     i, d = torch.arange(n, device=DEV), torch.arange(hd, device=DEV)[None]
     pages, at = s["table"][r].long()[i // P], (i % P)[:, None]
-    k = (at // 16 * (hd // E) + d // E) * 16 * E + at % 16 * E + d % E
+    place = torch.tensor([0, 1, 2, 3, 8, 9, 10, 11, 4, 5, 6, 7, 12, 13, 14, 15], device=DEV)[at % 16]
+    k = ((at // 16 * (hd // E) + d // E) * 16 + place) * E + d % E
     v = (at // E * hd + d) * E + at % E
     x = s["pool"][0][pages]                                      # [n][Hk][2][P * hd]
     x = torch.stack([x[:, :, 0].gather(2, k[:, None].expand(n, case["Hk"], hd)), x[:, :, 1].gather(2, v[:, None].expand(n, case["Hk"], hd))])
@@ -496,13 +497,14 @@ def exact(case, seed):
             return y.float().double()
         rot = torch.cat([f32(f32(a * c) - f32(b * sn)), f32(f32(b * c) + f32(a * sn))], -1)
         pool = s["pool"].double()
+        place = torch.tensor([0, 1, 2, 3, 8, 9, 10, 11, 4, 5, 6, 7, 12, 13, 14, 15], device=DEV)
         for r in range(R):
             n = off[r + 1] - off[r]
             slot = lens[r] + torch.arange(n, device=DEV)
             pages, at = s["table"][r].long()[slot // P], slot % P
             kv = _stored64(rot[off[r]:off[r + 1], H:H + Hk], case), _stored64(x[off[r]:off[r + 1], H + Hk:], case)
             for d in range(hd):
-                pool[0][pages, :, 0, (at // 16 * (hd // E) + d // E) * 16 * E + at % 16 * E + d % E] = kv[0][..., d]
+                pool[0][pages, :, 0, ((at // 16 * (hd // E) + d // E) * 16 + place[at % 16]) * E + d % E] = kv[0][..., d]
                 pool[0][pages, :, 1, (at // E * hd + d) * E + at % E] = kv[1][..., d]
         return {"q": _pair64(rot[:, :H].reshape(-1, H * hd), case), "pool": pool, "err": None}
     q = _from_act(s["q"], case).double().view(-1, H, hd)
