@@ -12,7 +12,8 @@
  *    use (a different kernel).
  * The ham_op_kv8_* operators are for a decode loop of the caller's own: they keep
  * a KV cache in 8 bits, which ham_prefill and ham_macro_step neither write nor
- * read (ham_op_kv8_pack takes what a prefill left).
+ * read (ham_op_kv8_pack takes what a prefill left).  The ham_op_paged_* operators
+ * keep one in pages, with prompts' attention and the pages' bookkeeping.
  * Same conventions as include/ham.h: C functions, HAM_OK or a negative
  * HAM_E* code, ham_last_error() for the message, "d_" = device pointers, work
  * enqueued on `hip_stream` and valid after it is synchronised.
@@ -233,6 +234,129 @@ int ham_op_kv8_attention(const ham_kv8_shape* shape, const void* d_q, const void
                          const int32_t* d_kv_len, const int32_t* d_enable, int32_t kv_max, const int32_t* d_blocks,
                          const int32_t* d_n_blocks, int32_t max_blocks, void* d_out, int32_t* d_err,
                          void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------- paged KV cache
+ * K and V of `rows` sequences in pages of a pool, in the storage type: writers, the
+ * attention of one new token of each sequence and of whole prompts over them, and
+ * the pages' bookkeeping on the device: rows that share pages (a common prompt, the
+ * beams of a search), free them and get new ones.  For a decode loop of the caller's
+ * own, as the 8-bit cache above.
+ *
+ * Pool, table, references.  A layer's pool is one caller-owned buffer of
+ * ham_op_paged_pool_bytes bytes, 256-byte aligned; those of n_layers layers follow
+ * one another, and all layers have the same tables.  It needs no clearing.
+ *   d_table  int32 [rows][row_pages]: slot s of row r lies in page
+ *            table[r][s / page_slots], at s % page_slots
+ *   d_refs   int32 [n_pages]: how many rows hold the page (table entries of slots
+ *            below the rows' lengths); 0 = free.  All zeros at first, with lengths 0
+ * A caller may count references of its own (a kept prompt), which keep pages too.
+ * A page is [n_kv_heads][2][page_slots * head_dim]: K, then V; with E = 16 bytes of
+ * values (8 in bf16, 4 in fp32), (slot s, channel d) is at
+ *   K ((s/16*(head_dim/E) + d/E)*16 + s/4%2*8 + s/8%2*4 + s%4)*E + d%E
+ *   V (s/E*head_dim + d)*E + s%E
+ *
+ * Packed rows.  New tokens of all sequences follow one another, n_tokens rows in
+ * all; row r's are d_offsets[r] .. d_offsets[r + 1] - 1 (int32 [rows + 1], not
+ * descending, within 0..n_tokens; a row may have none).  Rows of the arrays before
+ * the first and behind the last are neither read nor written.
+ *
+ * Errors on the device: d_err[r] (int32 [rows], in/out, bits are only set).  8: a
+ * length, count or offset that does not fit; the row is then one without slots (the
+ * attention of one token writes zeros, the others leave the row's part as it is).
+ * 32: a table entry outside the pool among the slots that a call reads or writes;
+ * page 0 is read in its place and nothing is written, so that the row's results mean
+ * nothing.  64: no pages left.
+ *
+ * Nothing is allocated and no call waits for the GPU: all of them can be captured
+ * into a graph.  A workspace needs no clearing and keeps nothing between calls.
+ * Other streams or host threads may read one pool at the same time, with workspaces
+ * and outputs of their own; a call that writes it, or tables, is ordered against them
+ * by the caller. */
+typedef struct ham_paged_shape {
+  int32_t dtype;      /* storage type of the pool and of activations: HAM_F32 or HAM_BF16 */
+  int32_t rows;       /* sequences, 1..4096 */
+  int32_t n_heads, n_kv_heads;  /* n_heads <= 1024, a multiple (1..16) of n_kv_heads */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t page_slots; /* 16, 32, 64, 128 or 256 */
+  int32_t n_pages;    /* of the pool, 1..2^22 */
+  int32_t row_pages;  /* table entries of a row; row_pages * page_slots <= 2^24 */
+} ham_paged_shape;
+
+/* Bytes of a layer's pool, and of the workspace that any call of this shape needs; 0
+ * for an invalid shape. */
+size_t ham_op_paged_pool_bytes(const ham_paged_shape* shape);
+size_t ham_op_paged_workspace_bytes(const ham_paged_shape* shape);
+
+/* RoPE and append of a layer: the packed tokens of row r become slots d_start[r] ..,
+ * whose pages the table has (ham_op_paged_advance).
+ *  d_qkv         fp32 [n_tokens][(n_heads + 2*n_kv_heads)*head_dim]: all q heads, then
+ *                k, then v, before RoPE
+ *  d_cos, d_sin  fp32 [n_tokens][head_dim/2]; rotate-half RoPE, each product and each
+ *                sum rounded to fp32
+ *  d_q           act rows [n_tokens][n_heads*head_dim]: the rotated q, or NULL
+ * K and V are rounded to the storage type; of the pages nothing but the new slots is
+ * written.  HAM_EINVAL on a bad shape, null or misaligned (16 bytes) pointer, n_tokens
+ * outside 1..2^24, or n_tokens * n_kv_heads past one launch (2^26); HAM_ENOMEM if the
+ * pool is too small. */
+int ham_op_paged_append(const ham_paged_shape* shape, int32_t n_tokens, const float* d_qkv, const float* d_cos,
+                        const float* d_sin, const int32_t* d_offsets, const int32_t* d_start, const int32_t* d_table,
+                        void* d_pool, size_t pool_bytes, void* d_q, int32_t* d_err, void* hip_stream);
+
+/* GQA attention of one query row per sequence over its pages:
+ *   out[r, h] = softmax_j(q[r, h] . K[r, h/(H/Hkv), j] / sqrt(hd)) V[...], j < kv_len[r].
+ * A row without slots (kv_len or enable 0), or whose scores are all -infinity, gets
+ * zeros.  Softmax statistics and sums are fp32; bf16 weights are sums of three bf16
+ * values (24 bits).  K is finite: an infinity in it may make the rows that see it NaN.
+ *  d_q, d_out  act rows [rows][n_heads*head_dim]
+ *  kv_max      host upper bound of kv_len; it chooses the split of the slots over
+ *              workgroups and so the order of the sums */
+int ham_op_paged_attention(const ham_paged_shape* shape, const void* d_q, const void* d_pool, size_t pool_bytes,
+                           const int32_t* d_table, const int32_t* d_kv_len, const int32_t* d_enable, int32_t kv_max,
+                           void* d_out, int32_t* d_err, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Causal GQA attention of packed tokens over their sequences' pages, which hold them
+ * already: row r's c tokens are the last c of its kv_len[r] slots, and token i of them
+ * sees the slots up to its own, kv_len - c + i, those before the packed tokens
+ * included.  An infinity or NaN in K or V reaches the tokens that see its slot and no
+ * other (in K it may make them NaN).  Numbers as in ham_op_paged_attention.
+ *  d_q, d_out  act rows [n_tokens][n_heads*head_dim]
+ *  kv_max      host upper bound of kv_len; with n_tokens, rows and heads it chooses
+ *              the split of the work and so the order of the sums */
+int ham_op_paged_prompt(const ham_paged_shape* shape, int32_t n_tokens, const void* d_q, const int32_t* d_offsets,
+                        const void* d_pool, size_t pool_bytes, const int32_t* d_table, const int32_t* d_kv_len,
+                        int32_t kv_max, void* d_out, int32_t* d_err, void* d_workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/* A step of the pages' bookkeeping, in place.  First, with d_parent, row r takes over
+ * the pages and the length of row parent[r] as they were before the call (r itself:
+ * no change; -1: none, the row's own pages are given up): a sequence forks, beams
+ * change places, a finished one is freed.  Then count[r] slots are added to the row,
+ * or taken away if it is negative, and pages with no holder left are free again.
+ *   - Pages that the new slots need are the lowest free ones, in the order of the rows.
+ *   - A page that already holds slots of the row and gets new ones is copied, in all
+ *     layers, if other rows hold it (refs > 1): the copy comes before the row's other
+ *     new pages.  Where all of its holders get new slots in this call, the lowest of
+ *     them keeps the page.
+ *   - If the free pages do not do for all rows, no row gets slots, and those with
+ *     count > 0 have 64 in d_err; the rest of the call has taken effect.
+ * kv_len[r] is then the new length and start[r] the first new slot (kv_len[r] where
+ * there are none); table entries that the row no longer holds are -1, those behind them
+ * are left.  8 in d_err: a parent outside -1..rows-1 or of an impossible length (the
+ * row keeps its own), a count that leaves less than 0 or more than row_pages *
+ * page_slots slots (it is taken as 0). */
+int ham_op_paged_advance(const ham_paged_shape* shape, int32_t n_layers, const int32_t* d_parent, const int32_t* d_count,
+                         int32_t* d_kv_len, int32_t* d_start, int32_t* d_table, int32_t* d_refs, void* d_pool,
+                         size_t pool_bytes, int32_t* d_err, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The pages in use (refs > 0) to the front of the pool: with U of them, those at U and
+ * above move, in order, to the free places below U, the lowest first, in all layers;
+ * references and tables follow.
+ *  d_map     int32 [n_pages]: the new place of each page, -1 for free ones
+ *  d_n_used  int32 [1]: U
+ * The pages from U on keep what they held. */
+int ham_op_paged_compact(const ham_paged_shape* shape, int32_t n_layers, const int32_t* d_kv_len, int32_t* d_table,
+                         int32_t* d_refs, void* d_pool, size_t pool_bytes, int32_t* d_map, int32_t* d_n_used,
+                         int32_t* d_err, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libham.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["kernels_gemm.hip", "kernels_prompt.hip", "kernels_attn.hip", "kernels_attn_prompt.hip", "kernels_misc.hip",
-           "kernels_kv8.hip", "ham.cpp", "kv8.cpp"]
+           "kernels_kv8.hip", "kernels_paged.hip", "kernels_paged_prompt.hip", "ham.cpp", "kv8.cpp", "paged.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 # packed fp32 VALU forms are kept out of every kernel

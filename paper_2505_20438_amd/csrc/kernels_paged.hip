@@ -1,0 +1,805 @@
+// Operators on a paged KV cache (layout: kernels_paged.h; bf16 prompts: kernels_paged_prompt.hip).
+//
+// k_paged_append    RoPE of packed projection rows, K and V into the rows' pages, q out.
+// k_paged_attn      attention of up to 16 query rows that share a kv head over their row's pages: the q-heads of one new token
+//                   of each sequence, or 16 (token, q-head) pairs of packed rows; k_paged_join joins its splits.
+// k_paged_take, k_paged_give, k_paged_copy  rows take over other rows' pages, give up theirs, get new ones; pages that two rows
+//                   share are copied before one writes to them.
+// k_paged_compact   pages in use to the front of the pool (and k_paged_copy).
+#include <algorithm>
+
+#include "launch_rules.h"
+#include "paged_device.h"
+
+namespace ham {
+
+namespace {
+
+// ---------------------------------------------------------------- append
+// A step is 32 slots (aligned) of a row that get new tokens.  For each step and kv head one workgroup writes K and V and, if
+// q is wanted, another rotates its q-heads; those of a step run on one XCD, whose L2 then holds the step's RoPE factors.
+// Bound by memory.  K: a thread has 8 RoPE pairs of a slot, so that 16 lanes write 256 bytes and 4 read 128.  V: a thread has a
+// channel of the E slots that lie together; at the ends of the new tokens, where some of them are others', values one by one.
+__device__ __forceinline__ int append_count(const PagedAppendArgs& a, int r) {  // -1: does not fit
+  const int c = packed_count(a.offsets, r, a.N), s = a.start[r];
+  return s >= 0 && (long long)s + c <= (long long)a.z.row_pages << a.z.lgP ? c : -1;
+}
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
+  constexpr int HALF = HD / 2, E = 16 / (int)sizeof(T), B = 32;
+  const PagedSizes& z = a.z;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kinds = a.q ? 2 : 1;
+  const uint32_t s8 = blockIdx.x / 8, step = s8 / (uint32_t)(kinds * z.Hk) * 8 + blockIdx.x % 8;
+  const int head = (int)(s8 % (uint32_t)(kinds * z.Hk)), kvh = head % z.Hk;
+  if (blockIdx.x == 0)
+    for (int r = tid; r < z.R; r += 256)
+      if (append_count(a, r) < 0) atomicOr(a.err + r, 8);
+  const Share sh = find_share(z.R, (int)step, [&](int r) {
+    const int c = append_count(a, r), s = a.start[r];
+    return c > 0 ? (s + c - 1) / B - s / B + 1 : 0;
+  });
+  if (sh.r < 0) return;
+  const int r = sh.r, o = a.offsets[r], c = a.offsets[r + 1] - o, s0 = a.start[r];
+  const int base = (s0 / B + sh.at) * B, lo = max(base, s0), hi = min(base + B, s0 + c);  // slots [lo, hi)
+  const size_t ld = (size_t)(z.H + 2 * z.Hk) * HD;
+  const size_t tok = (size_t)o - s0;  // packed row of slot 0
+  if (head >= z.Hk) {  // q
+    const int items = (hi - lo) * z.grp * (HALF / 8);
+    for (int q = tid; q < items; q += 256) {
+      const int i = q % (HALF / 8) * 8, hq = q / (HALF / 8), h = kvh * z.grp + hq % z.grp;
+      const size_t t = tok + lo + hq / z.grp;
+      const float* p = a.qkv + t * ld + h * HD + i;
+      f4 x[2], y[2], cs[2], sn[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        x[u] = *reinterpret_cast<const f4*>(p + 4 * u);
+        y[u] = *reinterpret_cast<const f4*>(p + HALF + 4 * u);
+        cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
+        sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
+      put_act8<T>(a.q, t, z.H * HD, h * HD + i, x);
+      put_act8<T>(a.q, t, z.H * HD, h * HD + i + HALF, y);
+    }
+    return;
+  }
+  const int* table = a.table + (size_t)r * z.row_pages;
+  const int P = 1 << z.lgP;
+  const size_t run = (size_t)P * HD;  // K, or V, of a kv head in a page
+  // where slot s's page holds the kv head, or null
+  const auto place = [&](int s) -> T* {
+    const int id = table[s >> z.lgP];
+    if ((unsigned)id >= (unsigned)z.n_pages) {
+      atomicOr(a.err + r, 32);
+      return nullptr;
+    }
+    return (T*)a.pool + ((size_t)id * z.Hk + kvh) * 2 * run;
+  };
+  const float* ksrc = a.qkv + (size_t)(z.H + kvh) * HD;
+  const float* vsrc = ksrc + (size_t)z.Hk * HD;
+  {
+    const int s = base + (w & 1) * 16 + (lane & 15), i = ((w >> 1) * 4 + (lane >> 4)) * 8;
+    if (i < HALF && s >= lo && s < hi) {
+      const size_t t = tok + s;
+      f4 x[2], y[2], cs[2], sn[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        x[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + i + 4 * u);
+        y[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + HALF + i + 4 * u);
+        cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
+        sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+      }
+      T* out = place(s);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
+      if (out != nullptr) {
+        const int at = s & (P - 1);
+#pragma unroll
+        for (int u = 0; u < 8; u += 4) {  // of 8 channels that lie together (fp32: 4 and 4)
+          st4<T>(out + paged_k_index<E>(at, i + u, HD), x[u / 4]);
+          st4<T>(out + paged_k_index<E>(at, HALF + i + u, HD), y[u / 4]);
+        }
+      }
+    }
+  }
+  for (int q = tid; q < B / E * HD; q += 256) {
+    const int d = q % HD, s = base + q / HD * E;  // slots s .. s + E - 1, in one page
+    if (s + E <= lo || s >= hi) continue;
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = s + e >= lo && s + e < hi ? vsrc[(tok + s + e) * ld + d] : 0.f;
+    T* out = place(max(s, lo));
+    if (out == nullptr) continue;
+    out += run + paged_v_index<E>(s & (P - 1), d, HD);
+    if (s >= lo && s + E <= hi) {
+      u4 x;
+      if constexpr (E == 8) x = pack_frag_bf16(v);
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __float_as_uint(v[e]);
+      *reinterpret_cast<u4*>(out) = x;
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (s + e >= lo && s + e < hi) out[e] = from_f<T>(v[e]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention
+// A block of B slots (32 in bf16, 16 in fp32) in registers, as operands of 16-row products: K row r of product t (16 slots
+// each, hd in pieces of 4 E channels), V^T row d (all B slots).  ka and kb are its first and (bf16) second 16 slots.
+template <typename T, int HD> struct KvBlock {
+  static constexpr int E = 16 / (int)sizeof(T), B = 4 * E, KT = B / 16, NF = HD / (4 * E), ND = HD / 16;
+  u4 k[KT][NF], v[ND];
+  static __device__ __forceinline__ u4 ld(const char* p, bool stream) { return stream ? ld16_stream(p) : ld16(p); }
+  // !there: nothing is wanted; the pool's first bytes, which no loop of these loads then needs a branch for
+  template <bool STREAM> __device__ __forceinline__ void load_k(const char* ka, const char* kb, bool there, const char* pool) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const char* p;
+    if constexpr (KT == 2) p = (r & 8 ? kb : ka) + (g * 16 + (r & 7)) * 16;
+    else p = ka + (g * 16 + r) * 16;
+    p = there ? p : pool;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) k[t][f] = ld(p + (4 * f * 16 + 8 * t) * 16, STREAM);
+  }
+  template <bool STREAM> __device__ __forceinline__ void load_v(const char* va, const char* vb, bool there, const char* pool) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const char* p;
+    if constexpr (KT == 2) p = (g & 2 ? vb : va) + ((g & 1) * HD + r) * 16;
+    else p = va + (((g & 1) << 1 | g >> 1) * HD + r) * 16;
+    p = there ? p : pool;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) v[d] = ld(p + d * 256, STREAM);
+  }
+};
+// first slot, within a block, of the E that lane group g has
+template <typename T> __device__ __forceinline__ int lane_slot(int g) {
+  return sizeof(T) == 2 ? 8 * g : 4 * ((g & 1) << 1 | g >> 1);
+}
+
+// Waves of a workgroup take blocks in turn; queries and the softmax of a column (16 of them: lane l & 15) are fp32, weights
+// three bf16 planes (24 significant bits), queries the two of an activation row, or all fp32.
+constexpr int PATT_WAVES = 8;
+template <int HD> struct PattLds {
+  float o[PATT_WAVES][16][HD + 4];
+  float m[PATT_WAVES][16], l[PATT_WAVES][16];
+  float top[16], sum[16];
+};
+
+// One workgroup per (split, kv head, tile).  PACKED: a tile is 16 (token, q-head) pairs of a row's packed tokens, each of which
+// sees the slots up to its token's; else the q-heads of the row's newest token, which see all.  Wave w of split s takes blocks
+// 8 s + w, 8 (s + nsplit) + w, ...; a block's K is loaded as soon as the one before it is used up, its V likewise.
+template <typename T, int HD, bool PACKED>
+__global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs a) {
+  using Blk = KvBlock<T, HD>;
+  constexpr int NW = PATT_WAVES, E = Blk::E, B = Blk::B, NF = Blk::NF, ND = Blk::ND, KT = Blk::KT, NP = sizeof(T) == 2 ? 3 : 1;
+  __shared__ PattLds<HD> sh;
+  const PagedSizes& z = a.z;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g = lane >> 4;
+  const int tile = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk), split = blockIdx.y;
+  const int first = split * NW + w, stride = a.nsplit * NW;
+  int r = tile, n, end, limit, col = c16;   // slots of the row, slots that any column sees, that this lane's column sees
+  size_t q_row;                             // activation row of this lane's column
+  int head;
+  bool live;
+  if constexpr (PACKED) {
+    if (blockIdx.x == 0 && split == 0)
+      for (int i = tid; i < z.R; i += 64 * NW)
+        if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
+    const Share s = find_share(z.R, tile, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
+    if (s.r < 0) return;
+    r = s.r;
+    const int o = a.offsets[r], c = a.offsets[r + 1] - o;
+    n = a.kv_len[r];
+    col = s.at * 16 + c16;
+    live = col < c * z.grp;
+    const int t = live ? col / z.grp : 0;
+    limit = live ? n - c + t + 1 : 0;
+    end = n - c + min(c, (s.at * 16 + 15) / z.grp + 1);
+    q_row = (size_t)o + t;
+    head = kvh * z.grp + (live ? col % z.grp : 0);
+  } else {
+    q_row = r;
+    live = c16 < z.grp;
+    head = kvh * z.grp + (live ? c16 : 0);
+  }
+  const int* table = a.table + (size_t)r * z.row_pages;
+  // entries of the wave's first 64 blocks, before the row's length is known
+  const auto entry = [&](int slot) { return min(slot >> z.lgP, z.row_pages - 1); };
+  int id0 = 0, id1 = 0;
+  if constexpr (!PACKED) {
+    const int slot = (first + lane * stride) * B;
+    id0 = table[entry(slot)];
+    if (KT == 2 && z.lgP == 4) id1 = table[entry(slot + 16)];
+  }
+  // queries: piece f holds channels 4 E f + E g ..
+  u4 qh[NF], ql[NF];
+  {
+    const int W = z.H * HD;
+    const T* p = (const T*)a.q + q_row * Act<T>::PL * W + (size_t)head * HD + E * g;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      qh[f] = live ? ld16(p + 4 * E * f) : zero16();
+      if constexpr (Act<T>::SPLIT) ql[f] = live ? ld16(p + W + 4 * E * f) : zero16();
+    }
+  }
+  if constexpr (!PACKED) {
+    n = a.kv_len[r];
+    const int on = a.enable[r];
+    if (n < 0 || n > a.kv_max) {
+      if (split == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
+      n = 0;
+    }
+    if (!on) n = 0;
+    end = limit = n;
+  }
+  const int nb = (end + B - 1) / B;
+  const size_t run = (size_t)(HD * sizeof(T)) << z.lgP, page = 2 * run * z.Hk;
+  const char* pool = (const char*)a.pool;
+  const char* mine0 = pool + 2 * run * kvh;
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  f4 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  Blk x;
+  const int least = __builtin_amdgcn_readfirstlane(limit);  // column 0 sees least
+  for (int e0 = first; e0 < nb; e0 += 64 * stride) {
+    const int mine = min(64, (nb - e0 + stride - 1) / stride);
+    if (PACKED || e0 > first) {
+      const int slot = (e0 + min(lane, mine - 1) * stride) * B;
+      id0 = table[entry(slot)];
+      if (KT == 2 && z.lgP == 4) id1 = table[entry(slot + 16)];
+    }
+    if (lane < mine) {
+      id0 = checked_page(id0, z, a.err + r);
+      if (KT == 2 && z.lgP == 4) id1 = (e0 + lane * stride) * B + 16 < end ? checked_page(id1, z, a.err + r) : id0;
+    }
+    asm volatile("" : "+v"(id0), "+v"(id1));  // waited for here, not with blocks under way
+    const char *ka, *kb;
+    const auto at = [&](int j) {
+      const int slot = (e0 + j * stride) * B;
+      ka = mine0 + (size_t)__builtin_amdgcn_readlane(id0, j) * page + (size_t)((slot & ((1 << z.lgP) - 1)) * HD) * sizeof(T);
+      kb = ka + 16 * HD * sizeof(T);
+      if (KT == 2 && z.lgP == 4) kb = mine0 + (size_t)__builtin_amdgcn_readlane(id1, j) * page;
+    };
+    at(0);
+    x.template load_k<!PACKED>(ka, kb, true, pool);
+    x.template load_v<!PACKED>(ka + run, kb + run, true, pool);
+    for (int j = 0; j < mine; ++j) {
+      const int base = (e0 + j * stride) * B;
+      const bool masked = base + B > least, more = j + 1 < mine;
+      if (more) at(j + 1);
+      float sc[4 * KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        f4 s = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) mma_act_b<T>(s, x.k[t][f], qh[f], ql[f]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[4 * t + e] = s[e];
+      }
+      x.template load_k<!PACKED>(ka, kb, more, pool);
+      const int mine_slot = base + lane_slot<T>(g);  // this lane's E slots
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (mine_slot + e >= limit) sc[e] = -INFINITY;
+      }
+      float top = sc[0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) top = fmaxf(top, sc[e]);
+      top *= scale;
+      if (__any(top > m)) {  // rarely, once a column has seen many keys
+        const float mnew = fmaxf(m, group_max(top));
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= alpha;
+        m = mnew;
+      }
+      const float mz = m == -INFINITY ? 0.f : m;  // scores of -infinity alone: all weights 0
+      float p[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale, -mz));
+        l += p[e];
+      }
+      u4 pp[NP];
+      if constexpr (NP == 3) to_planes<3>(p, pp);
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pp[0][e] = __float_as_uint(p[e]);
+      if (masked) {
+        bool odd = false;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)  // what lies past the slots that are seen may be NaN
+            if (mine_slot + e >= end) {
+              if constexpr (E == 8) x.v[d][e / 2] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+              else x.v[d][e] = 0u;
+            }
+          if constexpr (PACKED) odd |= any_nonfinite<T>(x.v[d]);
+        }
+        if (PACKED && __any(odd)) {
+          u4 seen;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 8)
+              seen[i] = (mine_slot + 2 * i < limit ? 0x3F80u : 0u) | (mine_slot + 2 * i + 1 < limit ? 0x3F800000u : 0u);
+            else seen[i] = mine_slot + i < limit ? 0x3F800000u : 0u;
+          }
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            u4 up, down;
+            f4 cu = f4{0.f, 0.f, 0.f, 0.f}, cd = cu;
+            split_nonfinite<T>(x.v[d], up, down);
+            Frag<T>::mma(cu, up, seen);
+            Frag<T>::mma(cd, down, seen);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] += seen_nonfinite(cu[i], cd[i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) Frag<T>::mma(o[d], x.v[d], pp[i]);
+      x.template load_v<!PACKED>(ka + run, kb + run, more, pool);
+    }
+  }
+  // per wave: maximum, sum and unnormalised outputs of each column
+  l = group_sum(l);
+  if (g == 0) {
+    sh.m[w][c16] = m;
+    sh.l[w][c16] = l;
+  }
+#pragma unroll
+  for (int d = 0; d < ND; ++d) *reinterpret_cast<f4*>(&sh.o[w][c16][16 * d + 4 * g]) = o[d];
+  __syncthreads();
+  if (tid < 16) {
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) M = fmaxf(M, sh.m[i][tid]);
+    const float mz = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      // 0 for a wave without slots; one whose scores are all NaN has maximum -infinity and sum NaN, which the factor 0 keeps
+      const float e = __builtin_amdgcn_exp2f(sh.m[i][tid] - mz);
+      L += e * sh.l[i][tid];
+      sh.m[i][tid] = e;
+    }
+    sh.top[tid] = M;
+    sh.sum[tid] = L;
+  }
+  __syncthreads();
+  const int rows = PACKED ? 16 : z.grp;
+  for (int t = tid; t < rows * (HD / 8); t += 64 * NW) {
+    const int j = t / (HD / 8), d = t % (HD / 8) * 8;
+    f4 v[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float e = sh.m[i][j];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) v[u] += e * *reinterpret_cast<const f4*>(&sh.o[i][j][d + 4 * u]);
+    }
+    if (a.nsplit == 1) {
+      const float L = sh.sum[j];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[u][e] = L == 0.f ? 0.f : v[u][e] / L;
+      size_t row = q_row;
+      int h = kvh * z.grp + j;
+      if constexpr (PACKED) {
+        const int i = col - c16 + j, o0 = a.offsets[r], c = a.offsets[r + 1] - o0;
+        if (i >= c * z.grp) break;
+        row = (size_t)o0 + i / z.grp;
+        h = kvh * z.grp + i % z.grp;
+      }
+      put_act8<T>(a.out, row, z.H * HD, h * HD + d, v);
+    } else {
+      const size_t rec = ((size_t)blockIdx.x * a.nsplit + split) * rows + j;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) *reinterpret_cast<f4*>(a.part + rec * HD + d + 4 * u) = v[u];
+      if (d == 0) {
+        float* ml = a.part + (size_t)gridDim.x * a.nsplit * rows * HD + 2 * rec;
+        ml[0] = sh.top[j];
+        ml[1] = sh.sum[j];
+      }
+    }
+  }
+}
+
+// The splits of a tile's query rows joined, a wave a row.
+template <typename T, int HD, bool PACKED>
+__global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
+  constexpr int V = HD / 64;
+  const PagedSizes& z = a.z;
+  const int lane = threadIdx.x & 63, rows = PACKED ? 16 : z.grp, j = blockIdx.y * 4 + (threadIdx.x >> 6);
+  const int tile = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
+  size_t row = tile;
+  int h = kvh * z.grp + j;
+  if constexpr (PACKED) {
+    const Share s = find_share(z.R, tile, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
+    if (s.r < 0) return;
+    const int o = a.offsets[s.r], c = a.offsets[s.r + 1] - o, i = s.at * 16 + j;
+    if (i >= c * z.grp) return;
+    row = (size_t)o + i / z.grp;
+    h = kvh * z.grp + i % z.grp;
+  } else if (j >= rows) {
+    return;
+  }
+  float v[V];
+  join_row<HD>(a.part, a.part + (size_t)gridDim.x * a.nsplit * rows * HD, (size_t)blockIdx.x * a.nsplit * rows + j, rows, a.nsplit, v);
+#pragma unroll
+  for (int i = 0; i < V; ++i) Act<T>::put(a.out, row, z.H * HD, h * HD + lane * V + i, v[i]);
+}
+
+// ---------------------------------------------------------------- pages
+__device__ __forceinline__ int pages_of(int slots, int lgP) { return (int)(((long long)slots + (1 << lgP) - 1) >> lgP); }
+__device__ __forceinline__ bool fits(long long slots, const PagedSizes& z) { return slots >= 0 && slots <= (long long)z.row_pages << z.lgP; }
+__device__ __forceinline__ bool in_pool(int id, const PagedSizes& z) { return (unsigned)id < (unsigned)z.n_pages; }
+
+// With `parent`: a row takes over the entries of another as they were, -1 for what it had beyond them; pages count the rows
+// that hold them.  The tables are written back at the end (k_paged_copy), when every row has been read.  A workgroup a row.
+__global__ __launch_bounds__(256) void k_paged_take(PagedAdvanceArgs a) {
+  const PagedSizes& z = a.z;
+  const int r = blockIdx.x, tid = threadIdx.x, had = a.kv_len[r];
+  int from = a.parent[r], len = 0, old = 0;
+  bool bad = false;
+  if (!fits(had, z)) {            // nothing is known of the row's pages: it stays as it is
+    bad = true;
+    from = r;
+    len = had;
+  } else {
+    old = pages_of(had, z.lgP);
+    if (from >= 0) {
+      bad = from >= z.R || !fits(a.kv_len[from], z);
+      if (bad) from = r;
+      len = a.kv_len[from];
+    } else if (from < -1) {
+      bad = true;
+      from = r;
+      len = had;
+    }
+  }
+  const int now = fits(len, z) ? pages_of(len, z.lgP) : 0;
+  if (tid == 0) {
+    if (bad) atomicOr(a.err + r, 8);
+    a.taken_len[r] = len;
+    a.span[r] = max(old, now);
+  }
+  const int* mine = a.table + (size_t)r * z.row_pages;
+  const int* theirs = a.table + (size_t)max(from, 0) * z.row_pages;
+  int* out = a.taken + (size_t)r * z.row_pages;
+  for (int e = tid; e < max(old, now); e += 256) {
+    const int id = e < now ? theirs[e] : -1;
+    out[e] = id;
+    if (from == r) continue;
+    if (e < old) {
+      const int was = mine[e];
+      if (in_pool(was, z)) atomicSub(a.refs + was, 1);
+      else atomicOr(a.err + r, 32);
+    }
+    if (e < now) {
+      if (in_pool(id, z)) atomicAdd(a.refs + id, 1);
+      else atomicOr(a.err + r, 32);
+    }
+  }
+}
+
+constexpr int GIVE_THREADS = 1024;
+constexpr int PAGED_MAX_ROWS = 4096;
+
+// inclusive sums over the workgroup's threads; `total` of all
+__device__ __forceinline__ int block_scan(int v, int* waves, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  v = wave_scan(v);
+  __syncthreads();
+  if (lane == 63) waves[w] = v;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int i = 0; i < GIVE_THREADS / 64; ++i) {
+    const int x = waves[i];
+    before += i < w ? x : 0;
+    all += x;
+  }
+  total = all;
+  return before + v;
+}
+// what other threads of the workgroup and its atomics wrote to global memory is seen after it
+__device__ __forceinline__ void global_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+}
+
+// One workgroup: gives up the pages of slots that rows drop, finds out which shared pages have to be copied and how many
+// pages each row needs, and hands out the lowest free ones in the order of the rows.  A row whose page has other holders gets
+// a copy, except, where all holders write to it in this call, the lowest of them.
+__global__ __launch_bounds__(GIVE_THREADS) void k_paged_give(PagedAdvanceArgs a) {
+  __shared__ int ends[PAGED_MAX_ROWS];      // pages wanted by the rows up to this one
+  __shared__ unsigned char copied[PAGED_MAX_ROWS];
+  __shared__ int waves[GIVE_THREADS / 64];
+  const PagedSizes& z = a.z;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, P = 1 << z.lgP;
+  constexpr int PER = PAGED_MAX_ROWS / GIVE_THREADS;  // rows of a thread, one after the other
+  const int per = (z.R + GIVE_THREADS - 1) / GIVE_THREADS;
+  int* table = a.parent ? a.taken : a.table;
+  const auto length = [&](int r) { return a.parent ? a.taken_len[r] : a.kv_len[r]; };
+  // what row r's slots change by, 0 where they cannot
+  const auto change = [&](int r, int len) { return fits(len, z) && fits((long long)len + a.count[r], z) ? a.count[r] : 0; };
+  // dropped slots: a wave a row
+  for (int r = w; r < z.R; r += GIVE_THREADS / 64) {
+    const int len = length(r), c = change(r, len);
+    if (c >= 0) continue;
+    for (int e = pages_of(len + c, z.lgP) + lane; e < pages_of(len, z.lgP); e += 64) {
+      int& entry = table[(size_t)r * z.row_pages + e];
+      if (in_pool(entry, z)) atomicSub(a.refs + entry, 1);
+      else atomicOr(a.err + r, 32);
+      entry = -1;
+    }
+  }
+  global_barrier();
+  // rows whose last page is written to and has other holders
+  int page[PER];
+  bool shared[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * per + i;
+    page[i] = -1;
+    shared[i] = false;
+    if (i >= per || r >= z.R) continue;
+    const int len = length(r), c = change(r, len);
+    if (!fits(len, z) || (c == 0 && a.count[r] != 0)) atomicOr(a.err + r, 8);
+    if (c > 0 && len % P > 0) {
+      const int id = table[(size_t)r * z.row_pages + len / P];
+      if (in_pool(id, z)) {
+        page[i] = id;
+        shared[i] = a.refs[id] > 1;
+        if (shared[i]) {
+          a.owner[2 * id] = 0;
+          a.owner[2 * id + 1] = z.R;
+        }
+      } else {
+        atomicOr(a.err + r, 32);
+      }
+    }
+  }
+  global_barrier();
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (shared[i]) {
+      atomicAdd(a.owner + 2 * page[i], 1);
+      atomicMin(a.owner + 2 * page[i] + 1, tid * per + i);
+    }
+  global_barrier();
+  int need[PER], sum = 0, ncopy = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * per + i;
+    need[i] = 0;
+    if (i >= per || r >= z.R) continue;
+    const int len = length(r), c = change(r, len);
+    const bool cp = shared[i] && !(a.owner[2 * page[i]] == a.refs[page[i]] && a.owner[2 * page[i] + 1] == r);
+    copied[r] = cp;
+    if (c > 0) need[i] = pages_of(len + c, z.lgP) - pages_of(len, z.lgP) + cp;
+    sum += need[i];
+    ncopy += cp;
+  }
+  int total, copies;
+  int before = block_scan(sum, waves, total) - sum;
+  const int my_copies = block_scan(ncopy, waves, copies) - ncopy;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * per + i;
+    if (i >= per || r >= z.R) continue;
+    before += need[i];
+    ends[r] = before;
+  }
+  // the lowest free pages, until there are enough
+  int found = 0;
+  for (int p0 = 0; p0 < z.n_pages && found < total; p0 += 4 * GIVE_THREADS) {
+    int free[4], n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + 4 * tid + i;
+      free[i] = p < z.n_pages && a.refs[p] <= 0;
+      n += free[i];
+    }
+    int here;
+    int at = found + block_scan(n, waves, here) - n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (free[i]) {
+        if (at < total) a.pages[at] = p0 + 4 * tid + i;
+        ++at;
+      }
+    found += here;
+  }
+  const bool enough = found >= total;
+  global_barrier();
+  if (enough) {
+    int at = my_copies;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int r = tid * per + i;
+      if (i >= per || r >= z.R || !copied[r]) continue;
+      a.copies[2 + 2 * at] = page[i];
+      a.copies[3 + 2 * at] = a.pages[ends[r] - need[i]];
+      atomicSub(a.refs + page[i], 1);
+      ++at;
+    }
+    for (int k = tid; k < total; k += GIVE_THREADS) {
+      int lo = 0, hi = z.R - 1;  // the first row with ends > k
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (ends[mid] > k) hi = mid;
+        else lo = mid + 1;
+      }
+      const int r = lo, i = k - (r ? ends[r - 1] : 0), held = pages_of(length(r), z.lgP), id = a.pages[k];
+      table[(size_t)r * z.row_pages + held + i - copied[r]] = id;
+      a.refs[id] = 1;
+    }
+  }
+  if (tid == 0) a.copies[0] = enough ? copies : 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * per + i;
+    if (i >= per || r >= z.R) continue;
+    const int len = length(r);
+    int c = change(r, len);
+    if (c > 0 && !enough) {
+      atomicOr(a.err + r, 64);
+      c = 0;
+    }
+    a.kv_len[r] = len + c;
+    a.start[r] = len + min(c, 0);
+    if (a.parent && fits(len, z)) a.span[r] = max(a.span[r], pages_of(len + c, z.lgP));
+  }
+}
+
+// Pages `copies` of every layer, in pieces; with `span`: the tables' entries written back.  A grid of fixed size goes round.
+constexpr int COPY_THREADS = 256, COPY_PIECE = 16 * 1024;  // bytes of a workgroup at a time
+__global__ __launch_bounds__(COPY_THREADS) void k_paged_copy(PagedCopyArgs c, const int* taken, const int* span, int* table, int R,
+                                                             int row_pages) {
+  const int tid = threadIdx.x;
+  const int n = c.copies[0], pieces = (c.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
+  if (span)
+    for (int r = blockIdx.x; r < R; r += gridDim.x)
+      for (int e = tid; e < span[r]; e += COPY_THREADS) table[(size_t)r * row_pages + e] = taken[(size_t)r * row_pages + e];
+  const uint32_t items = (uint32_t)n * c.layers * pieces;  // below 2^31
+  for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
+    const int piece = (int)(i % pieces), layer = (int)(i / pieces % c.layers), k = (int)(i / pieces / c.layers);
+    const size_t from = (size_t)c.copies[2 + 2 * k] * c.page_bytes, to = (size_t)c.copies[3 + 2 * k] * c.page_bytes;
+    char* base = c.pool + (size_t)layer * c.layer_bytes + (size_t)piece * COPY_PIECE;
+    const int left = c.page_bytes - piece * COPY_PIECE;
+    u4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int b = (u * COPY_THREADS + tid) * 16;
+      if (b < left) v[u] = ld16_stream(base + from + b);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int b = (u * COPY_THREADS + tid) * 16;
+      if (b < left) *reinterpret_cast<u4*>(base + to + b) = v[u];
+    }
+  }
+}
+
+// Pages with holders move to the free places below their number, the lowest first.  One workgroup finds them, counts and map
+// follow; the tables are rewritten by k_paged_remap beside the copies.
+__global__ __launch_bounds__(GIVE_THREADS) void k_paged_compact(PagedCompactArgs a) {
+  __shared__ int waves[GIVE_THREADS / 64];
+  const int tid = threadIdx.x, n = a.z.n_pages;
+  int mine = 0, used;
+  for (int p = tid; p < n; p += GIVE_THREADS) mine += a.refs[p] > 0;
+  block_scan(mine, waves, used);
+  int holes = 0, moves = 0;  // so far
+  for (int p0 = 0; p0 < n; p0 += 4 * GIVE_THREADS) {
+    int kind[4], h = 0, m = 0;  // 1: a free place below `used`, 2: a page that moves
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + 4 * tid + i;
+      const bool live = p < n && a.refs[p] > 0;
+      kind[i] = p >= n ? 0 : live ? (p >= used ? 2 : 0) : (p < used ? 1 : 0);
+      if (p < n) a.map[p] = live && p < used ? p : -1;
+      h += kind[i] == 1;
+      m += kind[i] == 2;
+    }
+    int th, tm;
+    int ah = holes + block_scan(h, waves, th) - h, am = moves + block_scan(m, waves, tm) - m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + 4 * tid + i;
+      if (kind[i] == 1) a.copies[3 + 2 * ah++] = p;
+      if (kind[i] == 2) a.copies[2 + 2 * am++] = p;
+    }
+    holes += th;
+    moves += tm;
+  }
+  if (tid == 0) {
+    a.copies[0] = moves;
+    a.used[0] = used;
+  }
+  global_barrier();
+  for (int k = tid; k < moves; k += GIVE_THREADS) {
+    const int from = a.copies[2 + 2 * k], to = a.copies[3 + 2 * k];
+    a.map[from] = to;
+    a.refs[to] = a.refs[from];
+    a.refs[from] = 0;
+  }
+}
+
+// The rows' entries by the map.  A workgroup a row.
+__global__ __launch_bounds__(256) void k_paged_remap(PagedCompactArgs a) {
+  const int r = blockIdx.x, n = a.kv_len[r];
+  if (!fits(n, a.z)) {
+    if (threadIdx.x == 0) atomicOr(a.err + r, 8);
+    return;
+  }
+  int* table = a.table + (size_t)r * a.z.row_pages;
+  for (int e = threadIdx.x; e < pages_of(n, a.z.lgP); e += 256) {
+    const int id = table[e], to = in_pool(id, a.z) ? a.map[id] : -1;
+    if (to < 0) atomicOr(a.err + r, 32);
+    else table[e] = to;
+  }
+}
+
+template <typename T, int HD>
+int append_t(const PagedAppendArgs& a, Stream s) {
+  const long long steps = std::min<long long>(a.N, ((long long)a.N + 62ll * a.z.R) / 32);
+  const unsigned blocks = (unsigned)((steps + 7) / 8 * 8 * a.z.Hk * (a.q ? 2 : 1));
+  launch_k((k_paged_append<T, HD>), dim3(blocks), dim3(256), 0, s, a);
+  return 0;
+}
+template <typename T, int HD>
+int attention_t(const PagedAttnArgs& a, Stream s) {
+  const PagedSizes& z = a.z;
+  if (a.offsets) {
+    const unsigned x = (unsigned)(paged_tiles(a.N, z.R, z.grp, 16) * z.Hk);
+    launch_k((k_paged_attn<T, HD, true>), dim3(x, a.nsplit), dim3(64 * PATT_WAVES), 0, s, a);
+    if (a.nsplit > 1) launch_k((k_paged_join<T, HD, true>), dim3(x, 4), dim3(256), 0, s, a);
+  } else {
+    const unsigned x = (unsigned)z.R * z.Hk;
+    launch_k((k_paged_attn<T, HD, false>), dim3(x, a.nsplit), dim3(64 * PATT_WAVES), 0, s, a);
+    if (a.nsplit > 1) launch_k((k_paged_join<T, HD, false>), dim3(x, (z.grp + 3) / 4), dim3(256), 0, s, a);
+  }
+  return 0;
+}
+
+#define PAGED_DISPATCH(fn)                                                  \
+  do {                                                                      \
+    if (hd == 64) return dtype == 1 ? fn<bf16, 64>(a, s) : fn<float, 64>(a, s);    \
+    if (hd == 128) return dtype == 1 ? fn<bf16, 128>(a, s) : fn<float, 128>(a, s); \
+    return -1;                                                              \
+  } while (0)
+
+}  // namespace
+
+int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s) { PAGED_DISPATCH(append_t); }
+int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, Stream s) { PAGED_DISPATCH(attention_t); }
+
+int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s) {
+  if (a.parent) launch_k(k_paged_take, dim3(a.z.R), dim3(256), 0, s, a);
+  launch_k(k_paged_give, dim3(1), dim3(GIVE_THREADS), 0, s, a);
+  launch_k(k_paged_copy, dim3(1024), dim3(COPY_THREADS), 0, s, c, (const int*)a.taken, (const int*)(a.parent ? a.span : nullptr), a.table, a.z.R,
+           a.z.row_pages);
+  return 0;
+}
+int launch_paged_compact(const PagedCompactArgs& a, const PagedCopyArgs& c, Stream s) {
+  launch_k(k_paged_compact, dim3(1), dim3(GIVE_THREADS), 0, s, a);
+  launch_k(k_paged_remap, dim3(a.z.R), dim3(256), 0, s, a);
+  launch_k(k_paged_copy, dim3(2048), dim3(COPY_THREADS), 0, s, c, (const int*)nullptr, (const int*)nullptr, (int*)nullptr, 0, 0);
+  return 0;
+}
+
+}  // namespace ham

@@ -110,4 +110,32 @@ inline int kv8_attn_splits(int R, int Hk, int hd, int blocks) {
   return best;
 }
 
+// Shares of `width` (token, q-head) pairs, at most, of N packed tokens of R rows with grp <= width q-heads a kv head: a row's
+// last share may be partly filled, and a share has a token at least.
+inline long long paged_tiles(long long N, long long R, long long grp, long long width) {
+  return std::min(N, (N * grp + (width - 1) * R) / width);
+}
+
+// Splits of the paged attention (kernels_paged.hip) for `tiles` tiles of Hk kv heads each over up to kv_max slots in blocks of
+// `block` slots: workgroups for two of them a CU, a block at least for each of a workgroup's eight waves.
+inline int paged_attn_splits(long long tiles, int Hk, int hd, int kv_max, int block) {
+  const long long pairs = tiles * Hk;
+  const int blocks = (kv_max + block - 1) / block;
+  const long long most = std::max<long long>(1, std::min<long long>({(blocks + 7) / 8, 1024 / pairs, 64}));
+  return (int)std::min<long long>(most, std::max<long long>(1, 512 / pairs));
+}
+
+// Shares of the keys within a workgroup (1 or 2) and splits over workgroups of the prompt attention (kernels_paged_prompt.hip)
+struct PagedPromptGrid {
+  int shares, splits;
+};
+inline PagedPromptGrid paged_prompt_grid(int N, int R, int Hk, int grp, int kv_max) {
+  const long long wide = paged_tiles(N, R, grp, 256) * Hk;
+  if (wide > 128) return PagedPromptGrid{1, 1};
+  const long long narrow = paged_tiles(N, R, grp, 128) * Hk;
+  const long long stages = (kv_max + 63) / 64;
+  const long long splits = std::max<long long>(1, std::min<long long>({256 / narrow, stages / 4, 32}));
+  return PagedPromptGrid{2, (int)splits};
+}
+
 }  // namespace ham

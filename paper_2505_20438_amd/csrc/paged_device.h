@@ -1,0 +1,134 @@
+// Device code shared by the kernels of the paged KV cache: packed rows, pages, values that are not finite.
+#pragma once
+#include "kernels_paged.h"
+#include "lane_ops.h"
+
+namespace ham {
+
+// Where a workgroup's share of packed rows lies.  Each row has need(r) of them, in the order of the rows; share `i` is number
+// `at` of row `r` (r < 0: there are no more).  Every wave looks for itself, 64 rows at a time.
+struct Share {
+  int r, at;
+};
+template <typename Need>
+__device__ __forceinline__ Share find_share(int R, int i, const Need& need) {
+  const int lane = threadIdx.x & 63;
+  for (int r0 = 0; r0 < R; r0 += 64) {
+    const int r = r0 + lane, n = r < R ? need(r) : 0, end = wave_scan(n);
+    const int total = __builtin_amdgcn_readlane(end, 63);
+    if (i < total) {
+      const int l = __builtin_ctzll(__ballot(end > i));
+      return Share{r0 + l, i - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(n, l))};
+    }
+    i -= total;
+  }
+  return Share{-1, 0};
+}
+
+// A row's packed tokens [o, o + c): c < 0 where they do not lie in the call's N.
+__device__ __forceinline__ int packed_count(const int* offsets, int r, int N) {
+  const int o = offsets[r], e = offsets[r + 1];
+  return o >= 0 && e >= o && e <= N ? e - o : -1;
+}
+// ... of a prompt's row, which also needs them among its n slots
+__device__ __forceinline__ int prompt_count(const PagedAttnArgs& a, int r) {
+  const int c = packed_count(a.offsets, r, a.N), n = a.kv_len[r];
+  return n <= a.kv_max && c <= n ? c : -1;
+}
+
+// A page id of a table.  One outside the pool is an error, and page 0 is read in its place.
+__device__ __forceinline__ int checked_page(int id, const PagedSizes& z, int* err) {
+  if ((unsigned)id < (unsigned)z.n_pages) return id;
+  atomicOr(err, 32);
+  return 0;
+}
+
+// Whether any of the E values of 16 bytes is an infinity or NaN
+template <typename T> __device__ __forceinline__ bool any_nonfinite(const u4& v);
+template <> __device__ __forceinline__ bool any_nonfinite<bf16>(const u4& v) {
+  uint32_t f = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f |= (v[i] & 0x7F807F80u) + 0x00800080u;  // carries into the sign bit from an exponent of ones
+  return (f & 0x80008000u) != 0;
+}
+template <> __device__ __forceinline__ bool any_nonfinite<float>(const u4& v) {
+  uint32_t f = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f |= (v[i] & 0x7F800000u) + 0x00800000u;
+  return (f & 0x80000000u) != 0;
+}
+
+// Rows of one product see different slots, and a value that a row does not see has weight 0, but 0 times an infinity or NaN
+// is NaN.  split_nonfinite takes such values out of v and marks them: `up` has 1 for infinity, `down` for -infinity, both for
+// NaN.  Products of the marks with the slots that a row sees count them, and what a row has seen of them is added to its sums.
+template <typename T> __device__ __forceinline__ void split_nonfinite(u4& v, u4& up, u4& down);
+template <> __device__ __forceinline__ void split_nonfinite<bf16>(u4& v, u4& up, u4& down) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    up[i] = down[i] = 0;
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const uint32_t x = v[i] >> h & 0xFFFFu;
+      if ((x & 0x7F80u) != 0x7F80u) continue;
+      const bool nan = (x & 0x7Fu) != 0;
+      if (nan || !(x & 0x8000u)) up[i] |= 0x3F80u << h;
+      if (nan || (x & 0x8000u)) down[i] |= 0x3F80u << h;
+      v[i] &= ~(0xFFFFu << h);
+    }
+  }
+}
+template <> __device__ __forceinline__ void split_nonfinite<float>(u4& v, u4& up, u4& down) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    up[i] = down[i] = 0;
+    const uint32_t x = v[i];
+    if ((x & 0x7F800000u) != 0x7F800000u) continue;
+    const bool nan = (x & 0x7FFFFFu) != 0;
+    if (nan || !(x & 0x80000000u)) up[i] = 0x3F800000u;
+    if (nan || (x & 0x80000000u)) down[i] = 0x3F800000u;
+    v[i] = 0;
+  }
+}
+__device__ __forceinline__ float seen_nonfinite(float up, float down) {
+  const float inf = __uint_as_float(0x7F800000u);
+  return up > 0.f ? (down > 0.f ? __uint_as_float(0x7FC00000u) : inf) : (down > 0.f ? -inf : 0.f);
+}
+
+// Joins the splits' records of one query row: the weights of split s in lane s, relative to the greatest maximum; a lane's
+// values of hd / 64 channels are added up in the order of the splits.
+template <int HD>
+__device__ __forceinline__ void join_row(const float* part, const float* ml, size_t rec, size_t step, int ns, float* o) {
+  constexpr int V = HD / 64, UN = 8;
+  const int lane = threadIdx.x & 63;
+  const float* p = part + rec * HD + lane * V;
+  float x[UN][V];
+#pragma unroll
+  for (int u = 0; u < UN; ++u)
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[u][v] = u < ns ? p[(size_t)u * step * HD + v] : 0.f;
+  float m = -INFINITY, l = 0.f;
+  if (lane < ns) {
+    m = ml[2 * (rec + (size_t)lane * step)];
+    l = ml[2 * (rec + (size_t)lane * step) + 1];
+  }
+  const float M = group_max(row_max(m)), mz = M == -INFINITY ? 0.f : M;
+  const float e = __builtin_amdgcn_exp2f(m - mz);
+  const float L = group_sum(row_sum(e * l));
+  const float w = L == 0.f ? 0.f : e / L;
+#pragma unroll
+  for (int v = 0; v < V; ++v) o[v] = 0.f;
+#pragma unroll
+  for (int u = 0; u < UN; ++u)
+    if (u < ns) {
+      const float wu = __shfl(w, u, WAVE);
+#pragma unroll
+      for (int v = 0; v < V; ++v) o[v] += wu * x[u][v];
+    }
+  for (int s = UN; s < ns; ++s) {
+    const float ws = __shfl(w, s, WAVE);
+#pragma unroll
+    for (int v = 0; v < V; ++v) o[v] += ws * p[(size_t)s * step * HD + v];
+  }
+}
+
+}  // namespace ham

@@ -28,7 +28,9 @@ EXPORTED = ("ham_weights_bytes", "ham_state_bytes", "ham_workspace_bytes", "ham_
             "ham_op_attention_workspace_bytes", "ham_op_decode_attention", "ham_op_attention_step",
             "ham_op_attention_step_splits", "ham_state_save", "ham_state_restore", "ham_op_attention_step_noalloc",
             "ham_op_attention_step_noalloc_max_bytes", "ham_op_kv8_cache_bytes", "ham_op_kv8_workspace_bytes",
-            "ham_op_kv8_info", "ham_op_kv8_append", "ham_op_kv8_pack", "ham_op_kv8_select", "ham_op_kv8_attention")
+            "ham_op_kv8_info", "ham_op_kv8_append", "ham_op_kv8_pack", "ham_op_kv8_select", "ham_op_kv8_attention",
+            "ham_op_paged_pool_bytes", "ham_op_paged_workspace_bytes", "ham_op_paged_append", "ham_op_paged_attention",
+            "ham_op_paged_prompt", "ham_op_paged_advance", "ham_op_paged_compact")
 
 
 class HamConfig(ctypes.Structure):
@@ -58,6 +60,11 @@ class HamProfT(ctypes.Structure):
 
 class HamKv8Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "rows", "n_heads", "n_kv_heads", "head_dim", "slots_cap")]
+
+
+class HamPagedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "rows", "n_heads", "n_kv_heads", "head_dim", "page_slots", "n_pages",
+                                              "row_pages")]
 
 
 class HamError(RuntimeError):
@@ -115,6 +122,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ham_op_kv8_pack.argtypes = [k8, P, P, I32, P, I32, P, SZ, P, P]
     lib.ham_op_kv8_select.argtypes = [k8, P, P, SZ, P, P, I32, I32, I32, I32, P, P, P, P, SZ, P]
     lib.ham_op_kv8_attention.argtypes = [k8, P, P, SZ, P, P, I32, P, P, I32, P, P, P, SZ, P]
+    pg = ctypes.POINTER(HamPagedShape)
+    for n in ("ham_op_paged_pool_bytes", "ham_op_paged_workspace_bytes"):
+        getattr(lib, n).argtypes = [pg]
+        getattr(lib, n).restype = SZ
+    lib.ham_op_paged_append.argtypes = [pg, I32, P, P, P, P, P, P, P, SZ, P, P, P]
+    lib.ham_op_paged_attention.argtypes = [pg, P, P, SZ, P, P, P, I32, P, P, P, SZ, P]
+    lib.ham_op_paged_prompt.argtypes = [pg, I32, P, P, P, SZ, P, P, I32, P, P, P, SZ, P]
+    lib.ham_op_paged_advance.argtypes = [pg, I32, P, P, P, P, P, P, P, SZ, P, P, SZ, P]
+    lib.ham_op_paged_compact.argtypes = [pg, I32, P, P, P, P, SZ, P, P, P, P, SZ, P]
     lib.ham_state_save.argtypes = [P, P, SZ]
     lib.ham_state_restore.argtypes = [P, P, SZ]
     lib.ham_last_error.restype = ctypes.c_char_p
@@ -123,7 +139,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for n in ("ham_init_weights", "ham_prefill", "ham_prefill_embeds", "ham_state_info", "ham_macro_step", "ham_kv_stats", "ham_set_debug",
               "ham_steps_done", "ham_tensor_info", "ham_set_graph", "ham_profile", "ham_profile_read",
               "ham_state_save", "ham_state_restore", "ham_op_kv8_info", "ham_op_kv8_append", "ham_op_kv8_pack",
-              "ham_op_kv8_select", "ham_op_kv8_attention"):
+              "ham_op_kv8_select", "ham_op_kv8_attention", "ham_op_paged_append", "ham_op_paged_attention", "ham_op_paged_prompt",
+              "ham_op_paged_advance", "ham_op_paged_compact"):
         getattr(lib, n).restype = I32
     _lib = lib
     return lib
@@ -323,6 +340,22 @@ def _refuse(rows: int, names: str, tensors) -> None:
             raise HamError(HAM_EINVAL, f"{name} must be on the current device")
 
 
+def _fits_exactly(tensors) -> bool:
+    """_fits of tensors that hold just what the call reads and writes."""
+    device = tensors[0][0].get_device()
+    for t, need, size in tensors:
+        if need and t.nbytes != need or size and t.itemsize != size or t.get_device() != device or not t.is_contiguous():
+            return False
+    return device >= 0 and device == _current_device()
+
+
+def _refuse_inexact(names: str, tensors) -> None:
+    for name, (t, need, _) in zip(names.split(), tensors):
+        if need and t.nbytes != need:
+            raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
+    _refuse(1, names, tensors)
+
+
 def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int, n_tokens=None) -> None:
     """RoPE and append of ``count[r]`` slots per row (include/ham_ops.h): qkv fp32 [rows][n_tokens][...], q act rows of
     the same tokens or None.  ``n_tokens`` is taken from qkv if not given: its first dimension is then ``rows``."""
@@ -402,6 +435,102 @@ def ham_op_kv8_attention(shape: HamKv8Shape, q, cache, kv_len, enable, kv_max: i
         ctypes.byref(shape), q.data_ptr(), cache.data_ptr(), cache.nbytes, kv_len.data_ptr(), enable.data_ptr(), kv_max,
         None if blocks is None else blocks.data_ptr(), None if count is None else count.data_ptr(), most, out.data_ptr(),
         err.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream))
+
+
+def paged_shape(dtype: int, rows: int, n_heads: int, n_kv_heads: int, head_dim: int, page_slots: int, n_pages: int,
+                row_pages: int) -> HamPagedShape:
+    """Shape of a paged KV cache (include/ham_ops.h): ``n_pages`` pages of the pool, tables of ``row_pages`` entries."""
+    return HamPagedShape(dtype, rows, n_heads, n_kv_heads, head_dim, page_slots, n_pages, row_pages)
+
+
+def ham_op_paged_pool_bytes(shape: HamPagedShape) -> int:
+    """Bytes of one layer's pool."""
+    return load_library().ham_op_paged_pool_bytes(ctypes.byref(shape))
+
+
+def ham_op_paged_workspace_bytes(shape: HamPagedShape) -> int:
+    return load_library().ham_op_paged_workspace_bytes(ctypes.byref(shape))
+
+
+def _pool_bytes(shape: HamPagedShape, layers: int = 1) -> int:
+    """Bytes that a call takes `pool` to hold: a pool of more pages would have its layers elsewhere."""
+    return layers * shape.n_pages * shape.n_kv_heads * 2 * shape.page_slots * shape.head_dim * (2 if shape.dtype == HAM_BF16 else 4)
+
+
+def ham_op_paged_append(shape: HamPagedShape, qkv, cos, sin, offsets, start, table, pool, q, err, stream: int) -> None:
+    """RoPE of packed projection rows, fp32 [n_tokens][...], and the append of their K and V to a layer's pool
+    (include/ham_ops.h): row r's tokens offsets[r] .. offsets[r + 1] - 1 become slots start[r] ..; q act rows of the same tokens or
+    None."""
+    rows, hd, H = shape.rows, shape.head_dim, shape.n_heads
+    n = qkv.shape[0] if qkv.dim() else 0
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    i4 = 4 * rows
+    args = ((qkv, n * (H + 2 * shape.n_kv_heads) * hd * 4, 4), (cos, n * hd * 2, 4), (sin, n * hd * 2, 4), (offsets, i4 + 4, 4),
+            (start, i4, 4), (table, i4 * shape.row_pages, 4), (pool, _pool_bytes(shape), es), (err, i4, 4))
+    if q is not None:
+        args += ((q, n * H * hd * 4, es),)
+    if not _fits_exactly(args):
+        _refuse_inexact("qkv cos sin offsets start table pool err q", args)
+    _check(load_library().ham_op_paged_append(
+        ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), offsets.data_ptr(), start.data_ptr(), table.data_ptr(),
+        pool.data_ptr(), pool.nbytes, None if q is None else q.data_ptr(), err.data_ptr(), stream))
+
+
+def ham_op_paged_attention(shape: HamPagedShape, q, pool, table, kv_len, enable, kv_max: int, out, err, workspace, stream: int) -> None:
+    """Attention of one act row per sequence over its pages of a layer's pool."""
+    i4, act = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    args = ((q, act, es), (pool, _pool_bytes(shape), es), (table, i4 * shape.row_pages, 4), (kv_len, i4, 4), (enable, i4, 4), (out, act, es), (err, i4, 4),
+            (workspace, 0, 0))
+    if not _fits_exactly(args):
+        _refuse_inexact("q pool table kv_len enable out err workspace", args)
+    _check(load_library().ham_op_paged_attention(
+        ctypes.byref(shape), q.data_ptr(), pool.data_ptr(), pool.nbytes, table.data_ptr(), kv_len.data_ptr(), enable.data_ptr(), kv_max,
+        out.data_ptr(), err.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream))
+
+
+def ham_op_paged_prompt(shape: HamPagedShape, q, offsets, pool, table, kv_len, kv_max: int, out, err, workspace, stream: int) -> None:
+    """Causal attention of packed act rows, the last offsets[r + 1] - offsets[r] of the kv_len[r] slots of each row, over their
+    pages of a layer's pool."""
+    i4, n = 4 * shape.rows, q.shape[0] if q.dim() else 0
+    act = n * shape.n_heads * shape.head_dim * 4
+    es = 2 if shape.dtype == HAM_BF16 else 4
+    args = ((q, act, es), (offsets, i4 + 4, 4), (pool, _pool_bytes(shape), es), (table, i4 * shape.row_pages, 4), (kv_len, i4, 4), (out, act, es),
+            (err, i4, 4), (workspace, 0, 0))
+    if not _fits_exactly(args):
+        _refuse_inexact("q offsets pool table kv_len out err workspace", args)
+    _check(load_library().ham_op_paged_prompt(
+        ctypes.byref(shape), n, q.data_ptr(), offsets.data_ptr(), pool.data_ptr(), pool.nbytes, table.data_ptr(), kv_len.data_ptr(),
+        kv_max, out.data_ptr(), err.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream))
+
+
+def ham_op_paged_advance(shape: HamPagedShape, n_layers: int, parent, count, kv_len, start, table, refs, pool, err, workspace,
+                         stream: int) -> None:
+    """Rows take over the pages of rows ``parent`` (or None: their own), then get ``count`` more slots, or fewer; in place.
+    ``pool`` holds n_layers layers' pools."""
+    i4 = 4 * shape.rows
+    args = ((count, i4, 4), (kv_len, i4, 4), (start, i4, 4), (table, i4 * shape.row_pages, 4), (refs, 4 * shape.n_pages, 4),
+            (pool, _pool_bytes(shape, n_layers), 0), (err, i4, 4), (workspace, 0, 0))
+    if parent is not None:
+        args += ((parent, i4, 4),)
+    if not _fits_exactly(args):
+        _refuse_inexact("count kv_len start table refs pool err workspace parent", args)
+    _check(load_library().ham_op_paged_advance(
+        ctypes.byref(shape), n_layers, None if parent is None else parent.data_ptr(), count.data_ptr(), kv_len.data_ptr(),
+        start.data_ptr(), table.data_ptr(), refs.data_ptr(), pool.data_ptr(), pool.nbytes, err.data_ptr(), workspace.data_ptr(),
+        workspace.nbytes, stream))
+
+
+def ham_op_paged_compact(shape: HamPagedShape, n_layers: int, kv_len, table, refs, pool, map, used, err, workspace, stream: int) -> None:
+    """Pages in use to the front of the pool: ``map`` int32 [n_pages] their new places, ``used`` int32 [1] their number."""
+    i4 = 4 * shape.rows
+    args = ((kv_len, i4, 4), (table, i4 * shape.row_pages, 4), (refs, 4 * shape.n_pages, 4), (pool, _pool_bytes(shape, n_layers), 0),
+            (map, 4 * shape.n_pages, 4), (used, 4, 4), (err, i4, 4), (workspace, 0, 0))
+    if not _fits_exactly(args):
+        _refuse_inexact("kv_len table refs pool map used err workspace", args)
+    _check(load_library().ham_op_paged_compact(
+        ctypes.byref(shape), n_layers, kv_len.data_ptr(), table.data_ptr(), refs.data_ptr(), pool.data_ptr(), pool.nbytes, map.data_ptr(),
+        used.data_ptr(), err.data_ptr(), workspace.data_ptr(), workspace.nbytes, stream))
 
 
 def ham_steps_done(model: int) -> int:
