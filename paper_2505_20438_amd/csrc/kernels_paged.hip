@@ -336,13 +336,14 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
           }
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            u4 up, down;
-            f4 cu = f4{0.f, 0.f, 0.f, 0.f}, cd = cu;
-            split_nonfinite<T>(x.v[d], up, down);
-            Frag<T>::mma(cu, up, seen);
-            Frag<T>::mma(cd, down, seen);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[d][i] += seen_nonfinite(cu[i], cd[i]);
+            for (int k = 0; k < 2; ++k) {
+              f4 n = f4{0.f, 0.f, 0.f, 0.f};
+              Frag<T>::mma(n, mark_nonfinite<T>(x.v[d], k), seen);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[d][i] += n[i] > 0.f ? (k ? -INFINITY : INFINITY) : 0.f;  // both: NaN
+            }
+            drop_nonfinite<T>(x.v[d]);
           }
         }
       }

@@ -8,6 +8,8 @@
 // so a lane (row l & 31, half l >> 5) holds scores, weights, softmax state and output columns of one row and only the other half
 // shares it.  The running maximum moves, and with it the outputs, only when a score exceeds it by more than 8 powers of two.
 // Masks, and values past the slots that a wave sees, are dealt with only in blocks that reach past the wave's first row.
+#include <type_traits>
+
 #include "gemm_epilogue.h"
 #include "launch_rules.h"
 #include "paged_device.h"
@@ -25,35 +27,59 @@ template <int HD> struct PP {
   static constexpr int NF = HD / 16, ND = HD / 32;
 };
 
-// One block of 32 slots from `base` for this wave's 32 rows.  MASK: slots at or past `limit` (the lane's row) count as
-// -infinity, and values at or past `vlimit` as 0, whatever they hold.  `load(j)`, j < NLD, issues this wave's loads of a later
-// stage, spread among the products.
-template <int HD, bool MASK, int NLD, typename Load>
-__device__ __forceinline__ void prompt_block(const u4* kblk, const u4* vblk, int base, int limit, int vlimit, const u4* qh, const u4* ql,
-                                             float sc, float& mrun, float& lrun, f16v* o, const Load& load) {
+// Scores of this wave's 32 rows against a block of 32 slots.
+template <int HD>
+__device__ __forceinline__ f16v block_scores(const u4* kblk, const u4* qh, const u4* ql) {
   using P = PP<HD>;
-  const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+  const int lane = lane_anew(), h = lane >> 5, r = lane & 31;
   f16v s;
 #pragma unroll
   for (int e = 0; e < 16; ++e) s[e] = 0.f;
-  __builtin_amdgcn_s_setprio(1);  // products before the other wave's softmax
   const u4* kr = kblk + (r >> 4) * P::RUN + h * 16 + (r & 15);
 #pragma unroll
   for (int f = 0; f < P::NF; ++f) {
     const bf16x8 k = __builtin_bit_cast(bf16x8, kr[f * 32]);
     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, qh[f]), s, 0, 0, 0);
     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, ql[f]), s, 0, 0, 0);
-    if (NLD > 0 && f % (P::NF / (NLD > 0 ? NLD : 1)) == 0) {
-      __builtin_amdgcn_sched_barrier(0);
-      load(f / (P::NF / (NLD > 0 ? NLD : 1)));
-      __builtin_amdgcn_sched_barrier(0);
+  }
+  return s;
+}
+
+// Planes of weights: three carry all 24 bits of an fp32 weight (each is the 8 leading bits of what the ones before it leave),
+// two 16 (to the nearest).  The third costs a fifth of the products, and with them, at the card's power limit, a fifth of the
+// time.  It is left out where it shows least: a sum over n slots that stays in fp32 through n / 16 products is rounded by
+// 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes (measured against 64 bits, relative 2-norm: 512
+// slots 0.3e-6 with three, 2e-6 with two).
+constexpr int PLANES_2_FROM = 16384;  // slots that the workgroup's first row sees
+template <int NP>
+__device__ __forceinline__ void weight_planes(const float* p, u4* pp) {
+  if constexpr (NP == 2) {
+    to_planes<2>(p, pp);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        pp[n][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);  // the upper halves
+        if (n == 2) break;
+        x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u));
+        y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xFFFF0000u));
+      }
     }
   }
-  __builtin_amdgcn_s_setprio(0);
-  if constexpr (MASK) {
+}
+
+// The softmax update of (m, l, o) by a block's scores, whose weights are left in NP bf16 planes.  `keep`: how many of the
+// block's slots the lane's row sees (32 or more: all); score e is slot 16 (e / 8) + 8 h + e % 8.
+template <int HD, int NP>
+__device__ __forceinline__ void block_weights(f16v s, bool masked, int keep, float sc, float& mrun, float& lrun, f16v* o, u4 (*pp)[3]) {
+  using P = PP<HD>;
+  const int h = (threadIdx.x & 63) >> 5;
+  if (masked) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e)  // score e: slot 16 (e / 8) + 8 h + e % 8
-      if (base + 16 * (e >> 3) + 8 * h + (e & 7) >= limit) s[e] = -INFINITY;
+    for (int e = 0; e < 16; ++e)
+      if (16 * (e >> 3) + 8 * h + (e & 7) >= keep) s[e] = -INFINITY;
   }
   float bm = s[0];
 #pragma unroll
@@ -77,72 +103,102 @@ __device__ __forceinline__ void prompt_block(const u4* kblk, const u4* vblk, int
 #pragma unroll
   for (int e = 0; e < 16; ++e) ps += p[e];
   lrun += ps;
-  u4 pp[2][3];
-  to_planes<3>(p, pp[0]);
-  to_planes<3>(p + 8, pp[1]);
-  const u4* vr = vblk + h * HD + r;  // channels 32 d + r of slots 16 t + 8 h ..
-  if constexpr (MASK) {
-    u4 seen[2];
-    bool odd = false;
-    const auto value = [&](int d, int t) {
-      u4 v = vr[t * P::RUN + d * 32];
-      const int keep = vlimit - (base + 16 * t + 8 * h);
+  weight_planes<NP>(p, pp[0]);
+  weight_planes<NP>(p + 8, pp[1]);
+}
+
+// Outputs += weights of a block times its V, whose first operands `v` are there already (first_values).
+constexpr int VFIRST = 4;
+template <int HD>
+__device__ __forceinline__ const u4* lane_values(const u4* vblk) {  // channels 32 d + r of slots 16 t + 8 h ..: [t * RUN + 32 d]
+  return vblk + ((threadIdx.x & 63) >> 5) * HD + (threadIdx.x & 31);
+}
+template <int HD>
+__device__ __forceinline__ void first_values(const u4* vblk, u4* v) {
+  const u4* vr = lane_values<HD>(vblk);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e >= keep) v[e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
-      return v;
-    };
+  for (int i = 0; i < VFIRST; ++i) v[i] = vr[i % 2 * PP<HD>::RUN + i / 2 * 32];
+}
+template <int HD, int NP>
+__device__ __forceinline__ void block_values(const u4* vblk, const u4* v, const u4 (*pp)[3], f16v* o) {
+  using P = PP<HD>;
+  const u4* vr = lane_values<HD>(vblk);
 #pragma unroll
-    for (int d = 0; d < P::ND; ++d)
+  for (int d = 0; d < P::ND; ++d)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        odd |= any_nonfinite<bf16>(value(d, t));
-    const bool fix = __any(odd);
-    if (fix)
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 x = __builtin_bit_cast(bf16x8, 2 * d + t < VFIRST ? v[(2 * d + t) % VFIRST] : vr[t * P::RUN + d * 32]);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < NP; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
+    }
+}
+// The order of a phase's products and LDS reads: an operand is read four before its turn.
+template <int HD, int NP>
+__device__ __forceinline__ void order_products() {
+  using P = PP<HD>;
+  constexpr int NV = 2 * P::ND, NK = P::NF;
+  static_assert(NK >= VFIRST, "the reads of the last of them go with V's products");
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int s0 = base + 16 * t + 8 * h + 2 * i;
-          seen[t][i] = (s0 < limit ? 0x3F80u : 0u) | (s0 + 1 < limit ? 0x3F800000u : 0u);
-        }
+  for (int i = 0; i < NV; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+    __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);  // matrix products
+  }
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    if (i < NK - VFIRST) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+  }
+}
+// ... of a block of which the wave sees `vkeep` slots: values past them count as 0, whatever they hold, and so do infinities and
+// NaN, since a row that does not see their slot has weight 0 for it, and 0 times them is NaN.  Whether there are any: see_nonfinite
+// deals with them when all blocks are done and the registers are free for it.
+template <int HD>
+__device__ __forceinline__ bool block_values_masked(const u4* vblk, int vkeep, const u4 (*pp)[3], f16v* o) {
+  using P = PP<HD>;
+  const int h = (threadIdx.x & 63) >> 5;
+  const u4* vr = lane_values<HD>(vblk);
+  bool odd = false;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int k = vkeep - (16 * t + 8 * h);  // of this lane's eight slots
+    u4 keep;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) keep[i] = k >= 2 * i + 2 ? 0xFFFFFFFFu : k == 2 * i + 1 ? 0x0000FFFFu : 0u;
 #pragma unroll
     for (int d = 0; d < P::ND; ++d) {
-      u4 v[2];
+      u4 v = vr[t * P::RUN + d * 32] & keep;
+      odd |= any_nonfinite<bf16>(v);
+      drop_nonfinite<bf16>(v);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) v[t] = value(d, t);
-      if (fix) {
-        f16v cu, cd;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) cu[e] = cd[e] = 0.f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          u4 up, down;
-          split_nonfinite<bf16>(v[t], up, down);
-          cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, seen[t]), cu, 0, 0, 0);
-          cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), __builtin_bit_cast(bf16x8, seen[t]), cd, 0, 0, 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] += seen_nonfinite(cu[e], cd[e]);
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[t]), __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
+      for (int i = 0; i < 3; ++i)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
     }
-  } else {
-    __builtin_amdgcn_s_setprio(1);
+  }
+  return __any(odd);
+}
+// Infinities and NaN among 16 values of each channel, `v` (pool) of slots from `base` on, into the outputs of the rows that see
+// their slots: products of 1 for such a value (infinity and NaN, then -infinity and NaN) and 1 for a slot that is seen.
+template <int HD>
+__device__ __forceinline__ void see_nonfinite(const u4* v, int base, int limit, f16v* o) {
+  const int l = threadIdx.x & 63, h = l >> 5, r = l & 31;
+  u4 seen;
 #pragma unroll
-    for (int d = 0; d < P::ND; ++d)
+  for (int i = 0; i < 4; ++i) {
+    const int s0 = base + 8 * h + 2 * i;
+    seen[i] = (s0 < limit ? 0x3F80u : 0u) | (s0 + 1 < limit ? 0x3F800000u : 0u);
+  }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 v = __builtin_bit_cast(bf16x8, vr[t * P::RUN + d * 32]);
+  for (int d = 0; d < PP<HD>::ND; ++d) {
+    const u4 x = v[h * HD + 32 * d + r];
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
-      }
-    __builtin_amdgcn_s_setprio(0);
+    for (int k = 0; k < 2; ++k) {
+      f16v n;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) n[e] = 0.f;
+      n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark_nonfinite<bf16>(x, k)), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] += n[e] > 0.f ? (k ? -INFINITY : INFINITY) : 0.f;  // both: NaN
+    }
   }
 }
 
@@ -187,44 +243,53 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
       if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
   const Share sh = prompt_share<QR>(a, job);
   if (sh.r < 0) return;
-  const int r = sh.r, o0 = a.offsets[r], c = a.offsets[r + 1] - o0, n = a.kv_len[r], held = n - c;
+  const int r = sh.r, o0 = scalar_at(a.offsets, r), c = scalar_at(a.offsets + 1, r) - o0, held = scalar_at(a.kv_len, r) - c;
   const int qt = w % QT, ks = w / QT;
   const int i0 = sh.at * QR + qt * 32, i1 = min(i0 + 32, c * z.grp);  // this wave's rows [i0, i1), of c * grp
   const bool rows_ok = i0 < c * z.grp;
   const int wave_least = rows_ok ? held + i0 / z.grp + 1 : 0, wave_end = rows_ok ? held + (i1 - 1) / z.grp + 1 : 0;
   const int wg_end = held + (min(sh.at * QR + QR, c * z.grp) - 1) / z.grp + 1;
-  const int i = i0 + (lane & 31);
-  const bool qok = i < c * z.grp;
-  const int tok = qok ? i / z.grp : 0, head = kvh * z.grp + (qok ? i % z.grp : 0), limit = qok ? held + tok + 1 : 0;
   const int W = z.H * HD;
-  const size_t q_row = (size_t)o0 + tok;
+  struct Row {      // of a lane: its token, q-head, and how many slots it sees; past the rows none
+    bool there;
+    int token, head, limit;
+  };
+  const auto row_of = [&](int l) {
+    const int i = i0 + (l & 31), t = i / z.grp;
+    const bool there = i < c * z.grp;
+    return Row{there, there ? t : 0, kvh * z.grp + (there ? i - t * z.grp : 0), there ? held + t + 1 : 0};
+  };
   u4 qh[P::NF], ql[P::NF];
   {
-    const bf16* qp = (const bf16*)a.q + q_row * 2 * W + (size_t)head * HD + (lane >> 5) * 8;
+    const Row row = row_of(lane);
+    const bf16* qp = (const bf16*)a.q + (size_t)(o0 + row.token) * 2 * W + (size_t)row.head * HD + (lane >> 5) * 8;
 #pragma unroll
     for (int f = 0; f < P::NF; ++f) {
-      qh[f] = qok ? ld16(qp + f * 16) : zero16();
-      ql[f] = qok ? ld16(qp + W + f * 16) : zero16();
+      qh[f] = row.there ? ld16(qp + f * 16) : zero16();
+      ql[f] = row.there ? ld16(qp + W + f * 16) : zero16();
     }
   }
   const int* table = a.table + (size_t)r * z.row_pages;
   const int ngrp = (wg_end + 15) / 16, nall = (wg_end + P::ST - 1) / P::ST;
   const int per = (nall + a.nsplit - 1) / a.nsplit, st0 = split * per, nst = min(nall, st0 + per);  // stages [st0, nst)
   const size_t run = (size_t)(HD * 2) << z.lgP, page = 2 * run * z.Hk;
-  const char* mine0 = (const char*)a.pool + 2 * run * kvh + (w & 1 ? run : 0) + lane * 16;
+  const char* mine0 = (const char*)a.pool + 2 * run * kvh + (w & 1 ? run : 0);
   // wave w loads 16 slots of K (w even) or V of a stage; groups past the end read the last one again, and are never used, so
   // that every wave has the same number of loads under way
   const auto group = [&](int st) { return min(st * 4 + (w >> 1), ngrp - 1); };
-  int next_id = st0 < nst ? table[group(st0) * 16 >> z.lgP] : 0;
-  const char* src = mine0;
-  const auto locate = [&](int st) {  // the page of stage st, whose id is there, and the id of the stage after it
-    const int slot = group(st) * 16, id = checked_page(__builtin_amdgcn_readfirstlane(next_id), z, a.err + r);
-    src = mine0 + (size_t)id * page + (size_t)(slot & ((1 << z.lgP) - 1)) * (HD * 2);
-    next_id = table[group(min(st + 1, nst - 1)) * 16 >> z.lgP];
-  };
-  const auto issue1 = [&](int st, int j) {
-    __builtin_amdgcn_global_load_lds((const void*)(src + j * 1024),
-                                     (__attribute__((address_space(3))) void*)(lds[st % NS] + ((w & 1) * 4 + (w >> 1)) * P::RUN + j * 64), 16, 0, 0);
+  int next_id = st0 < nst ? scalar_at(table, group(st0) * 16 >> z.lgP) : 0;
+  const auto issue = [&](int u) {  // the loads of stage st0 + u, whose page id is there, and the id of the stage after it
+    const int st = st0 + u, slot = group(st) * 16, id = checked_page(next_id, z, a.err + r);
+    next_id = scalar_at(table, group(min(st + 1, nst - 1)) * 16 >> z.lgP);
+    const BufRsrc src = buf_rsrc(mine0 + (size_t)id * page + (size_t)(slot & ((1 << z.lgP) - 1)) * (HD * 2), P::RUN * 16);
+    const uint32_t at = lane_anew() * 16;
+    auto* dst = (__attribute__((address_space(3))) void*)(lds[u % NS] + ((w & 1) * 4 + (w >> 1)) * P::RUN);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 1024, 0);
+    if constexpr (LPW == 4) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 2048, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 3072, 0);
+    }
   };
 
   f16v o[P::ND];
@@ -234,45 +299,85 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float mrun = -INFINITY, lrun = 0.f;
   const float sc = 1.44269504088896341f / sqrtf((float)HD);  // scores in powers of two
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s)
-    if (st0 + s < nst) {
-      locate(st0 + s);
-#pragma unroll
-      for (int j = 0; j < LPW; ++j) issue1(st0 + s, j);
-    }
-  for (int st = st0; st < nst; ++st) {
-    // stage st has landed once at most the loads of the stages issued after it are pending
-    if (st + NS - 2 < nst) wait_vm_lgkm0<(NS - 2) * LPW>();
+  // A wave's block j: the products of the weights of block j - 1 with its V and of K with the queries, then the softmax.  So the
+  // place of stage u - 1 is free again, and is loaded with stage u + 3, only in stage u + 1: two stages are on their way.
+  constexpr int NBS = 2 / KS;                     // blocks of a wave in a stage
+  const int cnt = max(nst - st0, 0);
+  const auto keys_of = [&](int u, int b) { return lds[u % NS] + 2 * (KS == 2 ? ks : b) * P::RUN; };
+  const auto values_of = [&](int u, int b) { return keys_of(u, b) + 4 * P::RUN; };
+  const auto base_of = [&](int u, int b) { return (st0 + u) * P::ST + (KS == 2 ? ks : b) * P::KB; };
+  const auto landed = [&](int u) {                // stage u, of which all waves' loads have arrived after this
+    if (u + 1 < cnt) wait_vm_lgkm0<LPW>();
     else wait_vm_lgkm0<0>();
     asm volatile("s_barrier" ::: "memory");
-    // every wave is past stage st - 1: its place takes stage st + NS - 1
-    constexpr int NB = 2 / KS, NLD = LPW / NB;  // blocks of this wave, loads issued in each
-    const bool more = st + NS - 1 < nst;
-    if (more) locate(st + NS - 1);
+  };
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int bi = KS == 2 ? ks : b, base = st * P::ST + bi * P::KB;
-      const u4 *kb = lds[st % NS] + 2 * bi * P::RUN, *vb = kb + 4 * P::RUN;
-      const auto load = [&](int j) {
-        if (more) issue1(st + NS - 1, b * NLD + j);
-      };
-      if (rows_ok && base + P::KB <= wave_least) {  // every slot visible to every row
-        prompt_block<HD, false, NLD>(kb, vb, base, limit, wave_end, qh, ql, sc, mrun, lrun, o, load);
-      } else if (base < wave_end) {
-        prompt_block<HD, true, NLD>(kb, vb, base, limit, wave_end, qh, ql, sc, mrun, lrun, o, load);
-      } else {  // blocks past this wave's last row hold nothing it sees
-#pragma unroll
-        for (int j = 0; j < NLD; ++j) load(j);
+  for (int u = 0; u < 2; ++u)
+    if (u < cnt) issue(u);
+  landed(0);
+  f16v s;
+  u4 pp[2][3], vf[VFIRST];
+  // stages whose slots every row of the workgroup sees, then the others
+  const int wg_least = held + sh.at * QR / z.grp + 1, full = max(0, min(cnt, wg_least / P::ST - st0));
+  const auto full_stages = [&](auto planes) {
+    constexpr int NP = decltype(planes)::value;
+    for (int j = 0; j < full * NBS; ++j) {
+      const int u = j / NBS, b = j % NBS;
+      if (b == 0 && u + 2 < cnt) issue(u + 2);
+      if (j > 0) {
+        block_values<HD, NP>(values_of((j - 1) / NBS, (j - 1) % NBS), vf, pp, o);
+        s = block_scores<HD>(keys_of(u, b), qh, ql);
+        order_products<HD, NP>();
+      } else {
+        s = block_scores<HD>(keys_of(u, b), qh, ql);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      block_weights<HD, NP>(s, false, 0, sc, mrun, lrun, o, pp);
+      first_values<HD>(values_of(u, b), vf);
+      __builtin_amdgcn_sched_barrier(0);
+      if (b == NBS - 1) landed(u + 1);
+    }
+    if (full > 0) block_values<HD, NP>(values_of(full - 1, NBS - 1), vf, pp, o);
+  };
+  if (wg_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
+  else full_stages(std::integral_constant<int, 3>{});
+  const int l = lane_anew(), limit = row_of(l).limit;
+  int odd = 0;
+  for (int u = full; u < cnt; ++u) {
+    if (u + 2 < cnt) issue(u + 2);
+#pragma unroll 1
+    for (int b = 0; b < NBS; ++b) {
+      const int base = base_of(u, b);
+      if (base >= wave_end) break;
+      const bool masked = base + P::KB > wave_least;
+      s = block_scores<HD>(keys_of(u, b), qh, ql);
+      block_weights<HD, 3>(s, masked, limit - base, sc, mrun, lrun, o, pp);
+      if (masked) {
+        odd |= block_values_masked<HD>(values_of(u, b), wave_end - base, pp, o);
+      } else {
+        first_values<HD>(values_of(u, b), vf);
+        block_values<HD, 3>(values_of(u, b), vf, pp, o);
       }
     }
+    landed(u + 1);
   }
+  if (odd)  // the blocks that were masked, again: slots from the first that not all of the wave's rows see
+#pragma unroll 1
+    for (int st = st0 + full; st < nst; ++st)
+#pragma unroll 1
+      for (int b = 0; b < 4; ++b) {
+        const int base = st * P::ST + b * 16;
+        if (base / P::KB * P::KB + P::KB <= wave_least || base >= wave_end || (KS == 2 && b / 2 != ks)) continue;
+        const int id = checked_page(scalar_at(table, base >> z.lgP), z, a.err + r);
+        const char* v = (const char*)a.pool + (size_t)id * page + 2 * run * kvh + run + (size_t)(base & ((1 << z.lgP) - 1)) * (HD * 2);
+        see_nonfinite<HD>((const u4*)v, base, limit, o);
+      }
   lrun += __shfl_xor(lrun, 32, WAVE);
   if constexpr (KS == 2) {  // merge the two waves of 32 rows: the second leaves its state in LDS
     constexpr int OV = P::ND * 16;  // output values per lane
     static_assert((size_t)QT * (OV + 2) * 64 * 4 <= sizeof(lds), "merge records");
     __syncthreads();  // every wave is past its last block
-    float* rec = reinterpret_cast<float*>(&lds[0][0]) + (size_t)qt * (OV + 2) * 64 + lane;
+    float* rec = reinterpret_cast<float*>(&lds[0][0]) + (size_t)qt * (OV + 2) * 64 + l;
     if (ks == 1) {
       rec[0] = mrun;
       rec[64] = lrun;
@@ -293,16 +398,17 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * a0 + rec[(2 + d * 16 + e) * 64] * a1;
   }
-  if (!qok) return;
+  const Row row = row_of(l);
+  if (!row.there) return;
   if (a.nsplit > 1) {
-    const size_t rec = ((size_t)blockIdx.x * a.nsplit + split) * QR + qt * 32 + (lane & 31);
-    float* out = a.part + rec * HD + 4 * (lane >> 5);
+    const size_t rec = ((size_t)blockIdx.x * a.nsplit + split) * QR + qt * 32 + (l & 31);
+    float* out = a.part + rec * HD + 4 * (l >> 5);
 #pragma unroll
     for (int d = 0; d < P::ND; ++d)
 #pragma unroll
       for (int e4 = 0; e4 < 4; ++e4)
         *reinterpret_cast<f4*>(out + d * 32 + e4 * 8) = f4{o[d][4 * e4], o[d][4 * e4 + 1], o[d][4 * e4 + 2], o[d][4 * e4 + 3]};
-    if (lane < 32) {
+    if (l < 32) {
       float* ml = a.part + (size_t)gridDim.x * a.nsplit * QR * HD + 2 * rec;
       ml[0] = mrun;
       ml[1] = lrun;
@@ -310,7 +416,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     return;
   }
   const float inv = lrun == 0.f ? 0.f : 1.0f / lrun;
-  bf16* op = (bf16*)a.out + q_row * 2 * W + (size_t)head * HD + 4 * (lane >> 5);
+  bf16* op = (bf16*)a.out + (size_t)(o0 + row.token) * 2 * W + (size_t)row.head * HD + 4 * (l >> 5);
 #pragma unroll
   for (int d = 0; d < P::ND; ++d)
 #pragma unroll

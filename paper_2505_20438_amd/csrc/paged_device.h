@@ -43,6 +43,21 @@ __device__ __forceinline__ int checked_page(int id, const PagedSizes& z, int* er
   return 0;
 }
 
+// An int at a wave-uniform index that no one writes during the kernel, by a scalar load: in a scalar register, and the wait for
+// it is none for the vector loads under way.
+__device__ __forceinline__ int scalar_at(const int* table, int i) {
+  typedef const __attribute__((address_space(4))) int* ConstInt;
+  return ((ConstInt)(uintptr_t)table)[__builtin_amdgcn_readfirstlane(i)];
+}
+
+// This lane's number, formed anew: a register kept for it, or for what follows from it, through a loop that needs them all
+// would be stored in memory, and the wait for its return is one for all loads under way.
+__device__ __forceinline__ int lane_anew() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 // Whether any of the E values of 16 bytes is an infinity or NaN
 template <typename T> __device__ __forceinline__ bool any_nonfinite(const u4& v);
 template <> __device__ __forceinline__ bool any_nonfinite<bf16>(const u4& v) {
@@ -59,39 +74,33 @@ template <> __device__ __forceinline__ bool any_nonfinite<float>(const u4& v) {
 }
 
 // Rows of one product see different slots, and a value that a row does not see has weight 0, but 0 times an infinity or NaN
-// is NaN.  split_nonfinite takes such values out of v and marks them: `up` has 1 for infinity, `down` for -infinity, both for
-// NaN.  Products of the marks with the slots that a row sees count them, and what a row has seen of them is added to its sums.
-template <typename T> __device__ __forceinline__ void split_nonfinite(u4& v, u4& up, u4& down);
-template <> __device__ __forceinline__ void split_nonfinite<bf16>(u4& v, u4& up, u4& down) {
+// is NaN.  Such values are marked by a 1 in an operand for infinity (sign 0) or -infinity (sign 1), NaN in both, and taken
+// out of v; products of the marks with the slots that a row sees count them, and what a row has seen is added to its sums.
+template <typename T> __device__ __forceinline__ u4 mark_nonfinite(const u4& v, int sign) {
+  constexpr uint32_t ONE = sizeof(T) == 2 ? 0x3F80u : 0x3F800000u, EXP = sizeof(T) == 2 ? 0x7F80u : 0x7F800000u;
+  constexpr uint32_t MANT = sizeof(T) == 2 ? 0x7Fu : 0x7FFFFFu, SIGN = sizeof(T) == 2 ? 0x8000u : 0x80000000u;
+  u4 m;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    up[i] = down[i] = 0;
+    m[i] = 0;
 #pragma unroll
-    for (int h = 0; h < 32; h += 16) {
-      const uint32_t x = v[i] >> h & 0xFFFFu;
-      if ((x & 0x7F80u) != 0x7F80u) continue;
-      const bool nan = (x & 0x7Fu) != 0;
-      if (nan || !(x & 0x8000u)) up[i] |= 0x3F80u << h;
-      if (nan || (x & 0x8000u)) down[i] |= 0x3F80u << h;
-      v[i] &= ~(0xFFFFu << h);
+    for (int h = 0; h < 32; h += (int)sizeof(T) * 8) {
+      const uint32_t x = v[i] >> h;
+      if ((x & EXP) == EXP && ((x & MANT) != 0 || ((x & SIGN) != 0) == (sign != 0))) m[i] |= ONE << h;
     }
   }
+  return m;
 }
-template <> __device__ __forceinline__ void split_nonfinite<float>(u4& v, u4& up, u4& down) {
+template <typename T> __device__ __forceinline__ void drop_nonfinite(u4& v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    up[i] = down[i] = 0;
-    const uint32_t x = v[i];
-    if ((x & 0x7F800000u) != 0x7F800000u) continue;
-    const bool nan = (x & 0x7FFFFFu) != 0;
-    if (nan || !(x & 0x80000000u)) up[i] = 0x3F800000u;
-    if (nan || (x & 0x80000000u)) down[i] = 0x3F800000u;
-    v[i] = 0;
+    if constexpr (sizeof(T) == 2) {
+      if ((v[i] & 0x7F80u) == 0x7F80u) v[i] &= 0xFFFF0000u;
+      if ((v[i] & 0x7F800000u) == 0x7F800000u) v[i] &= 0x0000FFFFu;
+    } else {
+      if ((v[i] & 0x7F800000u) == 0x7F800000u) v[i] = 0;
+    }
   }
-}
-__device__ __forceinline__ float seen_nonfinite(float up, float down) {
-  const float inf = __uint_as_float(0x7F800000u);
-  return up > 0.f ? (down > 0.f ? __uint_as_float(0x7FC00000u) : inf) : (down > 0.f ? -inf : 0.f);
 }
 
 // Joins the splits' records of one query row: the weights of split s in lane s, relative to the greatest maximum; a lane's
