@@ -5,7 +5,7 @@
 //                   of each sequence, or 16 (token, q-head) pairs of packed rows; k_paged_join joins its splits.
 // k_paged_take, k_paged_give, k_paged_copy  rows take over other rows' pages, give up theirs, get new ones; pages that two rows
 //                   share are copied before one writes to them.
-// k_paged_compact   pages in use to the front of the pool (and k_paged_copy).
+// k_paged_compact   pages in use to the front of the pool (k_paged_copy moves them).
 #include <algorithm>
 
 #include "launch_rules.h"
@@ -163,25 +163,66 @@ template <typename T> __device__ __forceinline__ int lane_slot(int g) {
 
 // Waves of a workgroup take blocks in turn; queries and the softmax of a column (16 of them: lane l & 15) are fp32, weights
 // three bf16 planes (24 significant bits), queries the two of an activation row, or all fp32.
-constexpr int PATT_WAVES = 8;
+constexpr int PATT_WAVES = 4;
 template <int HD> struct PattLds {
   float o[PATT_WAVES][16][HD + 4];
   float m[PATT_WAVES][16], l[PATT_WAVES][16];
   float top[16], sum[16];
 };
 
-// One workgroup per (split, kv head, tile).  PACKED: a tile is 16 (token, q-head) pairs of a row's packed tokens, each of which
-// sees the slots up to its token's; else the q-heads of the row's newest token, which see all.  Wave w of split s takes blocks
-// 8 s + w, 8 (s + nsplit) + w, ...; a block's K is loaded as soon as the one before it is used up, its V likewise.
-template <typename T, int HD, bool PACKED>
-__global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs a) {
+// The slots of a row that are attended over; a length out of range is reported by one thread.
+__device__ __forceinline__ int slots_of(const PagedAttnArgs& a, int r, bool report) {
+  const int n = a.kv_len[r];
+  if (n < 0 || n > a.kv_max) {
+    if (report) atomicOr(a.err + r, 8);
+    return 0;
+  }
+  return a.enable[r] ? n : 0;
+}
+// One row per sequence, split: the blocks of all rows in about a.nsplit shares of the same size, so that a long row among short
+// ones has many workgroups.  Of row r, of `blocks`, they are shares `first` .. `first` + `of` - 1, `size` blocks each.
+struct RowShare {
+  int r, size, blocks, first, of;
+};
+template <typename Pick>
+__device__ __forceinline__ RowShare row_share(const PagedAttnArgs& a, int block, const Pick& pick) {
+  const int R = a.z.R, lane = threadIdx.x & 63;
+  const auto blocks = [&](int r) { return r < R ? (slots_of(a, r, false) + block - 1) / block : 0; };
+  int all = 0, most = 0, n = 0;
+  for (int r0 = 0; r0 < R; r0 += 64) {
+    n = blocks(r0 + lane);
+    all += __builtin_amdgcn_readlane(wave_scan(n), 63);
+    most = max(most, (int)group_max(row_max((float)n)));  // below 2^24: exact
+  }
+  const int whole = a.nsplit - min(R, a.nsplit / 2);  // the rows' ends are shares too
+  const int size = max(max((all + whole - 1) / whole, PAGED_LEAST_BLOCKS), (most + PAGED_MAX_SPLIT - 1) / PAGED_MAX_SPLIT);
+  int before = 0;
+  for (int r0 = 0; r0 < R; r0 += 64) {
+    const int r = r0 + lane;
+    if (R > 64) n = blocks(r);
+    const int of = r < R ? max(1, (n + size - 1) / size) : 0, end = before + wave_scan(of);
+    const uint64_t hit = __ballot(r < R && pick(r, end - of, end));
+    if (hit) {
+      const int l = __builtin_ctzll(hit), first = __builtin_amdgcn_readlane(end - of, l);
+      return RowShare{r0 + l, size, __builtin_amdgcn_readlane(n, l), first, __builtin_amdgcn_readlane(of, l)};
+    }
+    before = __builtin_amdgcn_readlane(end, 63);
+  }
+  return RowShare{-1, 0, 0, 0, 0};
+}
+
+// One workgroup per (tile, kv head, split).  PACKED: a tile is 16 (token, q-head) pairs of a row's packed tokens, each of which
+// sees the slots up to its token's; else the q-heads of the row's newest token, which see all, and splits are shares.  The waves
+// of a workgroup take its blocks in turn; a block's K is loaded as soon as the one before it is used up, its V likewise.
+template <typename T, int HD, bool PACKED, bool SPLIT>
+__global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_attn(PagedAttnArgs a) {
   using Blk = KvBlock<T, HD>;
   constexpr int NW = PATT_WAVES, E = Blk::E, B = Blk::B, NF = Blk::NF, ND = Blk::ND, KT = Blk::KT, NP = sizeof(T) == 2 ? 3 : 1;
   __shared__ PattLds<HD> sh;
   const PagedSizes& z = a.z;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g = lane >> 4;
   const int tile = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk), split = blockIdx.y;
-  const int first = split * NW + w, stride = a.nsplit * NW;
+  int first = split * NW + w, stride = (PACKED ? a.nsplit : 1) * NW, stop = 0x7FFFFFFF;  // this wave's blocks: first, first + stride, ..
   int r = tile, n, end, limit, col = c16;   // slots of the row, slots that any column sees, that this lane's column sees
   size_t q_row;                             // activation row of this lane's column
   int head;
@@ -203,6 +244,13 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
     q_row = (size_t)o + t;
     head = kvh * z.grp + (live ? col % z.grp : 0);
   } else {
+    if constexpr (SPLIT) {
+      const RowShare s = row_share(a, B, [&](int, int from, int to) { return from <= tile && tile < to; });
+      if (s.r < 0) return;
+      r = s.r;
+      first = (tile - s.first) * s.size + w;
+      stop = (tile - s.first + 1) * s.size;
+    }
     q_row = r;
     live = c16 < z.grp;
     head = kvh * z.grp + (live ? c16 : 0);
@@ -227,17 +275,8 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
       if constexpr (Act<T>::SPLIT) ql[f] = live ? ld16(p + W + 4 * E * f) : zero16();
     }
   }
-  if constexpr (!PACKED) {
-    n = a.kv_len[r];
-    const int on = a.enable[r];
-    if (n < 0 || n > a.kv_max) {
-      if (split == 0 && kvh == 0 && tid == 0) atomicOr(a.err + r, 8);
-      n = 0;
-    }
-    if (!on) n = 0;
-    end = limit = n;
-  }
-  const int nb = (end + B - 1) / B;
+  if constexpr (!PACKED) end = limit = n = slots_of(a, r, kvh == 0 && tid == 0);
+  const int nb = min((end + B - 1) / B, stop);
   const size_t run = (size_t)(HD * sizeof(T)) << z.lgP, page = 2 * run * z.Hk;
   const char* pool = (const char*)a.pool;
   const char* mine0 = pool + 2 * run * kvh;
@@ -389,7 +428,7 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
 #pragma unroll
       for (int u = 0; u < 2; ++u) v[u] += e * *reinterpret_cast<const f4*>(&sh.o[i][j][d + 4 * u]);
     }
-    if (a.nsplit == 1) {
+    if constexpr (!SPLIT) {
       const float L = sh.sum[j];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -405,11 +444,11 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
       }
       put_act8<T>(a.out, row, z.H * HD, h * HD + d, v);
     } else {
-      const size_t rec = ((size_t)blockIdx.x * a.nsplit + split) * rows + j;
+      const size_t rec = ((size_t)blockIdx.x * gridDim.y + split) * rows + j;
 #pragma unroll
       for (int u = 0; u < 2; ++u) *reinterpret_cast<f4*>(a.part + rec * HD + d + 4 * u) = v[u];
       if (d == 0) {
-        float* ml = a.part + (size_t)gridDim.x * a.nsplit * rows * HD + 2 * rec;
+        float* ml = a.part + (size_t)gridDim.x * gridDim.y * rows * HD + 2 * rec;
         ml[0] = sh.top[j];
         ml[1] = sh.sum[j];
       }
@@ -417,27 +456,33 @@ __global__ __launch_bounds__(64 * PATT_WAVES, 2) void k_paged_attn(PagedAttnArgs
   }
 }
 
-// The splits of a tile's query rows joined, a wave a row.
+// The splits of a tile's (PACKED), or of a row's, query rows joined, a wave each.  `tiles`: of the attention's launch.
 template <typename T, int HD, bool PACKED>
-__global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a, int tiles) {
   constexpr int V = HD / 64;
   const PagedSizes& z = a.z;
   const int lane = threadIdx.x & 63, rows = PACKED ? 16 : z.grp, j = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const int tile = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
-  size_t row = tile;
-  int h = kvh * z.grp + j;
+  const int x = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
+  if (j >= rows) return;
+  size_t row = x, rec, step;
+  int h = kvh * z.grp + j, ns = a.nsplit;
   if constexpr (PACKED) {
-    const Share s = find_share(z.R, tile, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
+    const Share s = find_share(z.R, x, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
     if (s.r < 0) return;
     const int o = a.offsets[s.r], c = a.offsets[s.r + 1] - o, i = s.at * 16 + j;
     if (i >= c * z.grp) return;
     row = (size_t)o + i / z.grp;
     h = kvh * z.grp + i % z.grp;
-  } else if (j >= rows) {
-    return;
+    rec = (size_t)blockIdx.x * ns * rows + j;
+    step = rows;
+  } else {
+    const RowShare s = row_share(a, KvBlock<T, HD>::B, [&](int r, int, int) { return r == x; });
+    ns = s.of;
+    rec = ((size_t)s.first * z.Hk + kvh) * rows + j;
+    step = (size_t)z.Hk * rows;
   }
   float v[V];
-  join_row<HD>(a.part, a.part + (size_t)gridDim.x * a.nsplit * rows * HD, (size_t)blockIdx.x * a.nsplit * rows + j, rows, a.nsplit, v);
+  join_row<HD>(a.part, a.part + (size_t)tiles * z.Hk * (PACKED ? ns : 1) * rows * HD, rec, step, ns, v);
 #pragma unroll
   for (int i = 0; i < V; ++i) Act<T>::put(a.out, row, z.H * HD, h * HD + lane * V + i, v[i]);
 }
@@ -514,129 +559,141 @@ __device__ __forceinline__ int block_scan(int v, int* waves, int& total) {
   total = all;
   return before + v;
 }
-// what other threads of the workgroup and its atomics wrote to global memory is seen after it
-__device__ __forceinline__ void global_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-  __syncthreads();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-}
+// Global memory that atomics of this workgroup have changed, past the CU's cache, which may hold it as it was.  After a barrier
+// (which waits for the atomics) that is all one workgroup needs: fences for other workgroups cost 2 to 4 us each here.
+__device__ __forceinline__ int changed(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // One workgroup: gives up the pages of slots that rows drop, finds out which shared pages have to be copied and how many
 // pages each row needs, and hands out the lowest free ones in the order of the rows.  A row whose page has other holders gets
-// a copy, except, where all holders write to it in this call, the lowest of them.
+// a copy, except, where all holders write to it in this call, the lowest of them.  Bound by latency: lengths, the rows' last
+// entries, their references, and the writes, one round trip to memory each, and the scans between them.
+constexpr int GIVE_PAGES = 2048;            // of the pages to give out, in LDS; those behind them in the workspace
 __global__ __launch_bounds__(GIVE_THREADS) void k_paged_give(PagedAdvanceArgs a) {
   __shared__ int ends[PAGED_MAX_ROWS];      // pages wanted by the rows up to this one
   __shared__ unsigned char copied[PAGED_MAX_ROWS];
   __shared__ int waves[GIVE_THREADS / 64];
+  __shared__ int given[GIVE_PAGES];
   const PagedSizes& z = a.z;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, P = 1 << z.lgP;
-  constexpr int PER = PAGED_MAX_ROWS / GIVE_THREADS;  // rows of a thread, one after the other
-  const int per = (z.R + GIVE_THREADS - 1) / GIVE_THREADS;
+  constexpr int PER = PAGED_MAX_ROWS / GIVE_THREADS;  // rows of a thread: tid, tid + GIVE_THREADS, ..
   int* table = a.parent ? a.taken : a.table;
-  const auto length = [&](int r) { return a.parent ? a.taken_len[r] : a.kv_len[r]; };
-  // what row r's slots change by, 0 where they cannot
-  const auto change = [&](int r, int len) { return fits(len, z) && fits((long long)len + a.count[r], z) ? a.count[r] : 0; };
-  // dropped slots: a wave a row
-  for (int r = w; r < z.R; r += GIVE_THREADS / 64) {
-    const int len = length(r), c = change(r, len);
-    if (c >= 0) continue;
-    for (int e = pages_of(len + c, z.lgP) + lane; e < pages_of(len, z.lgP); e += 64) {
-      int& entry = table[(size_t)r * z.row_pages + e];
-      if (in_pool(entry, z)) atomicSub(a.refs + entry, 1);
-      else atomicOr(a.err + r, 32);
-      entry = -1;
-    }
-  }
-  global_barrier();
-  // rows whose last page is written to and has other holders
-  int page[PER];
-  bool shared[PER];
+  const int* lengths = a.parent ? a.taken_len : a.kv_len;
+  // references of the first pages, for the search for free ones
+  const auto refs4 = [&](int p0, int* free) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) free[i] = p0 + 4 * tid + i < z.n_pages ? changed(a.refs + p0 + 4 * tid + i) : 1;
+  };
+  int first4[4];
+  refs4(0, first4);
+  // a row's length, and by how many slots it changes: 0 where it cannot
+  int len[PER], c[PER];
+  bool drops = false;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * per + i;
-    page[i] = -1;
-    shared[i] = false;
-    if (i >= per || r >= z.R) continue;
-    const int len = length(r), c = change(r, len);
-    if (!fits(len, z) || (c == 0 && a.count[r] != 0)) atomicOr(a.err + r, 8);
-    if (c > 0 && len % P > 0) {
-      const int id = table[(size_t)r * z.row_pages + len / P];
-      if (in_pool(id, z)) {
-        page[i] = id;
-        shared[i] = a.refs[id] > 1;
-        if (shared[i]) {
-          a.owner[2 * id] = 0;
-          a.owner[2 * id + 1] = z.R;
-        }
-      } else {
-        atomicOr(a.err + r, 32);
+    const int r = tid + i * GIVE_THREADS;
+    len[i] = c[i] = 0;
+    if (r >= z.R) continue;
+    len[i] = lengths[r];
+    const int want = a.count[r];
+    const bool ok = fits(len[i], z) && fits((long long)len[i] + want, z);
+    c[i] = ok ? want : 0;
+    if (!fits(len[i], z) || (!ok && want != 0)) atomicOr(a.err + r, 8);
+    drops |= c[i] < 0;
+  }
+  if (__syncthreads_or(drops)) {  // dropped slots: a wave a row
+    for (int r = w; r < z.R; r += GIVE_THREADS / 64) {
+      const int n = lengths[r], less = a.count[r];
+      if (less >= 0 || !fits(n, z) || !fits((long long)n + less, z)) continue;
+      for (int e = pages_of(n + less, z.lgP) + lane; e < pages_of(n, z.lgP); e += 64) {
+        int& entry = table[(size_t)r * z.row_pages + e];
+        if (in_pool(entry, z)) atomicSub(a.refs + entry, 1);
+        else atomicOr(a.err + r, 32);
+        entry = -1;
       }
     }
+    __syncthreads();
+    refs4(0, first4);
   }
-  global_barrier();
+  // rows whose last page is written to and has other holders
+  int page[PER], holders[PER];
+  bool any = false;
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (shared[i]) {
-      atomicAdd(a.owner + 2 * page[i], 1);
-      atomicMin(a.owner + 2 * page[i] + 1, tid * per + i);
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid + i * GIVE_THREADS;
+    page[i] = holders[i] = 0;
+    if (c[i] <= 0 || len[i] % P == 0) continue;
+    page[i] = table[(size_t)r * z.row_pages + len[i] / P];
+    if (in_pool(page[i], z)) holders[i] = changed(a.refs + page[i]);
+    else atomicOr(a.err + r, 32);
+    if (holders[i] > 1) {
+      a.owner[2 * page[i]] = 0;
+      a.owner[2 * page[i] + 1] = z.R;
+      any = true;
     }
-  global_barrier();
-  int need[PER], sum = 0, ncopy = 0;
+  }
+  bool copy[PER] = {};
+  int ncopy = 0;
+  if (__syncthreads_or(any)) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (holders[i] > 1) {
+        atomicAdd(a.owner + 2 * page[i], 1);
+        atomicMin(a.owner + 2 * page[i] + 1, tid + i * GIVE_THREADS);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (holders[i] > 1) {
+        copy[i] = changed(a.owner + 2 * page[i]) != holders[i] || changed(a.owner + 2 * page[i] + 1) != tid + i * GIVE_THREADS;
+        ncopy += copy[i];
+      }
+  }
+  // pages wanted by the rows before: GIVE_THREADS rows at a time
+  int need[PER], total = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * per + i;
-    need[i] = 0;
-    if (i >= per || r >= z.R) continue;
-    const int len = length(r), c = change(r, len);
-    const bool cp = shared[i] && !(a.owner[2 * page[i]] == a.refs[page[i]] && a.owner[2 * page[i] + 1] == r);
-    copied[r] = cp;
-    if (c > 0) need[i] = pages_of(len + c, z.lgP) - pages_of(len, z.lgP) + cp;
-    sum += need[i];
-    ncopy += cp;
+    const int r = tid + i * GIVE_THREADS;
+    need[i] = c[i] > 0 ? pages_of(len[i] + c[i], z.lgP) - pages_of(len[i], z.lgP) + copy[i] : 0;
+    if (i * GIVE_THREADS >= z.R) break;
+    int here;
+    const int end = total + block_scan(need[i], waves, here);
+    total += here;
+    if (r < z.R) {
+      ends[r] = end;
+      copied[r] = copy[i];
+    }
   }
-  int total, copies;
-  int before = block_scan(sum, waves, total) - sum;
-  const int my_copies = block_scan(ncopy, waves, copies) - ncopy;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int r = tid * per + i;
-    if (i >= per || r >= z.R) continue;
-    before += need[i];
-    ends[r] = before;
-  }
+  int copies;
+  int my_copy = block_scan(ncopy, waves, copies) - ncopy;
   // the lowest free pages, until there are enough
   int found = 0;
   for (int p0 = 0; p0 < z.n_pages && found < total; p0 += 4 * GIVE_THREADS) {
-    int free[4], n = 0;
+    int n = 0, here;
+    if (p0 > 0) refs4(p0, first4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int p = p0 + 4 * tid + i;
-      free[i] = p < z.n_pages && a.refs[p] <= 0;
-      n += free[i];
-    }
-    int here;
+    for (int i = 0; i < 4; ++i) n += first4[i] <= 0;
     int at = found + block_scan(n, waves, here) - n;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (free[i]) {
-        if (at < total) a.pages[at] = p0 + 4 * tid + i;
+      if (first4[i] <= 0) {
+        if (at < min(total, GIVE_PAGES)) given[at] = p0 + 4 * tid + i;
+        else if (at < total) a.pages[at] = p0 + 4 * tid + i;
         ++at;
       }
     found += here;
   }
   const bool enough = found >= total;
-  global_barrier();
+  __syncthreads();
+  const auto given_page = [&](int k) { return k < GIVE_PAGES ? given[k] : a.pages[k]; };
   if (enough) {
-    int at = my_copies;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int r = tid * per + i;
-      if (i >= per || r >= z.R || !copied[r]) continue;
-      a.copies[2 + 2 * at] = page[i];
-      a.copies[3 + 2 * at] = a.pages[ends[r] - need[i]];
-      atomicSub(a.refs + page[i], 1);
-      ++at;
-    }
+    for (int i = 0; i < PER; ++i)
+      if (copy[i]) {
+        a.copies[2 + 2 * my_copy] = page[i];
+        a.copies[3 + 2 * my_copy] = given_page(ends[tid + i * GIVE_THREADS] - need[i]);
+        atomicSub(a.refs + page[i], 1);
+        ++my_copy;
+      }
     for (int k = tid; k < total; k += GIVE_THREADS) {
       int lo = 0, hi = z.R - 1;  // the first row with ends > k
       while (lo < hi) {
@@ -644,38 +701,56 @@ __global__ __launch_bounds__(GIVE_THREADS) void k_paged_give(PagedAdvanceArgs a)
         if (ends[mid] > k) hi = mid;
         else lo = mid + 1;
       }
-      const int r = lo, i = k - (r ? ends[r - 1] : 0), held = pages_of(length(r), z.lgP), id = a.pages[k];
-      table[(size_t)r * z.row_pages + held + i - copied[r]] = id;
+      const int r = lo, i = k - (r ? ends[r - 1] : 0), id = given_page(k);
+      table[(size_t)r * z.row_pages + pages_of(lengths[r], z.lgP) + i - copied[r]] = id;
       a.refs[id] = 1;
     }
   }
   if (tid == 0) a.copies[0] = enough ? copies : 0;
-  __syncthreads();
+  __syncthreads();  // lengths are read above
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * per + i;
-    if (i >= per || r >= z.R) continue;
-    const int len = length(r);
-    int c = change(r, len);
-    if (c > 0 && !enough) {
+    const int r = tid + i * GIVE_THREADS;
+    if (r >= z.R) continue;
+    if (c[i] > 0 && !enough) {
       atomicOr(a.err + r, 64);
-      c = 0;
+      c[i] = 0;
     }
-    a.kv_len[r] = len + c;
-    a.start[r] = len + min(c, 0);
-    if (a.parent && fits(len, z)) a.span[r] = max(a.span[r], pages_of(len + c, z.lgP));
+    a.kv_len[r] = len[i] + c[i];
+    a.start[r] = len[i] + min(c[i], 0);
+    if (a.parent && fits(len[i], z)) a.span[r] = max(a.span[r], pages_of(len[i] + c[i], z.lgP));
   }
 }
 
-// Pages `copies` of every layer, in pieces; with `span`: the tables' entries written back.  A grid of fixed size goes round.
+// Pages `copies` of every layer, in pieces of 16 KB, by a grid of fixed size that goes round; beside them the tables: what rows
+// have taken over is written back (`span` entries of a row), or entries go by the map of the compaction.
 constexpr int COPY_THREADS = 256, COPY_PIECE = 16 * 1024;  // bytes of a workgroup at a time
-__global__ __launch_bounds__(COPY_THREADS) void k_paged_copy(PagedCopyArgs c, const int* taken, const int* span, int* table, int R,
-                                                             int row_pages) {
+struct PagedTables {
+  PagedSizes z;
+  int* table;
+  const int* taken; const int* span;
+  const int* map; const int* kv_len; int* err;
+};
+__global__ __launch_bounds__(COPY_THREADS) void k_paged_copy(PagedCopyArgs c, PagedTables t) {
   const int tid = threadIdx.x;
   const int n = c.copies[0], pieces = (c.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
-  if (span)
-    for (int r = blockIdx.x; r < R; r += gridDim.x)
-      for (int e = tid; e < span[r]; e += COPY_THREADS) table[(size_t)r * row_pages + e] = taken[(size_t)r * row_pages + e];
+  if (t.span)
+    for (int r = blockIdx.x; r < t.z.R; r += gridDim.x)
+      for (int e = tid; e < t.span[r]; e += COPY_THREADS) t.table[(size_t)r * t.z.row_pages + e] = t.taken[(size_t)r * t.z.row_pages + e];
+  if (t.map)
+    for (int r = blockIdx.x; r < t.z.R; r += gridDim.x) {
+      const int len = t.kv_len[r];
+      if (!fits(len, t.z)) {
+        if (tid == 0) atomicOr(t.err + r, 8);
+        continue;
+      }
+      int* table = t.table + (size_t)r * t.z.row_pages;
+      for (int e = tid; e < pages_of(len, t.z.lgP); e += COPY_THREADS) {
+        const int id = table[e], to = in_pool(id, t.z) ? t.map[id] : -1;
+        if (to < 0) atomicOr(t.err + r, 32);
+        else table[e] = to;
+      }
+    }
   const uint32_t items = (uint32_t)n * c.layers * pieces;  // below 2^31
   for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
     const int piece = (int)(i % pieces), layer = (int)(i / pieces % c.layers), k = (int)(i / pieces / c.layers);
@@ -696,62 +771,58 @@ __global__ __launch_bounds__(COPY_THREADS) void k_paged_copy(PagedCopyArgs c, co
   }
 }
 
-// Pages with holders move to the free places below their number, the lowest first.  One workgroup finds them, counts and map
-// follow; the tables are rewritten by k_paged_remap beside the copies.
+// Pages with holders move to the free places below their number, the lowest first.  One workgroup finds them; map and counts
+// follow.  (Up to 4,096 pages are read once.)
 __global__ __launch_bounds__(GIVE_THREADS) void k_paged_compact(PagedCompactArgs a) {
   __shared__ int waves[GIVE_THREADS / 64];
+  constexpr int TILE = 4 * GIVE_THREADS;
   const int tid = threadIdx.x, n = a.z.n_pages;
-  int mine = 0, used;
-  for (int p = tid; p < n; p += GIVE_THREADS) mine += a.refs[p] > 0;
+  const auto load = [&](int p0, int* refs) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) refs[i] = p0 + 4 * tid + i < n ? a.refs[p0 + 4 * tid + i] : 0;
+  };
+  int refs[4], mine = 0, used;
+  for (int p0 = 0; p0 < n; p0 += TILE) {
+    load(p0, refs);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine += refs[i] > 0;
+  }
   block_scan(mine, waves, used);
   int holes = 0, moves = 0;  // so far
-  for (int p0 = 0; p0 < n; p0 += 4 * GIVE_THREADS) {
-    int kind[4], h = 0, m = 0;  // 1: a free place below `used`, 2: a page that moves
+  for (int p0 = 0; p0 < n; p0 += TILE) {
+    if (n > TILE) load(p0, refs);
+    int h = 0, m = 0;  // free places below `used`, pages that move
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int p = p0 + 4 * tid + i;
-      const bool live = p < n && a.refs[p] > 0;
-      kind[i] = p >= n ? 0 : live ? (p >= used ? 2 : 0) : (p < used ? 1 : 0);
-      if (p < n) a.map[p] = live && p < used ? p : -1;
-      h += kind[i] == 1;
-      m += kind[i] == 2;
+      if (p >= n) continue;
+      a.map[p] = refs[i] > 0 && p < used ? p : -1;
+      h += refs[i] <= 0 && p < used;
+      m += refs[i] > 0 && p >= used;
     }
-    int th, tm;
-    int ah = holes + block_scan(h, waves, th) - h, am = moves + block_scan(m, waves, tm) - m;
+    int both;  // 16 bits each: a tile has 4,096
+    const int at = block_scan(h | m << 16, waves, both);
+    int ah = holes + (at & 0xFFFF) - h, am = moves + (at >> 16) - m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int p = p0 + 4 * tid + i;
-      if (kind[i] == 1) a.copies[3 + 2 * ah++] = p;
-      if (kind[i] == 2) a.copies[2 + 2 * am++] = p;
+      if (p >= n) continue;
+      if (refs[i] <= 0 && p < used) a.copies[3 + 2 * ah++] = p;
+      if (refs[i] > 0 && p >= used) a.copies[2 + 2 * am++] = p;
     }
-    holes += th;
-    moves += tm;
+    holes += both & 0xFFFF;
+    moves += both >> 16;
   }
   if (tid == 0) {
     a.copies[0] = moves;
     a.used[0] = used;
   }
-  global_barrier();
+  __syncthreads();
   for (int k = tid; k < moves; k += GIVE_THREADS) {
-    const int from = a.copies[2 + 2 * k], to = a.copies[3 + 2 * k];
+    const int from = changed(a.copies + 2 + 2 * k), to = changed(a.copies + 3 + 2 * k);
     a.map[from] = to;
     a.refs[to] = a.refs[from];
     a.refs[from] = 0;
-  }
-}
-
-// The rows' entries by the map.  A workgroup a row.
-__global__ __launch_bounds__(256) void k_paged_remap(PagedCompactArgs a) {
-  const int r = blockIdx.x, n = a.kv_len[r];
-  if (!fits(n, a.z)) {
-    if (threadIdx.x == 0) atomicOr(a.err + r, 8);
-    return;
-  }
-  int* table = a.table + (size_t)r * a.z.row_pages;
-  for (int e = threadIdx.x; e < pages_of(n, a.z.lgP); e += 256) {
-    const int id = table[e], to = in_pool(id, a.z) ? a.map[id] : -1;
-    if (to < 0) atomicOr(a.err + r, 32);
-    else table[e] = to;
   }
 }
 
@@ -765,15 +836,16 @@ int append_t(const PagedAppendArgs& a, Stream s) {
 template <typename T, int HD>
 int attention_t(const PagedAttnArgs& a, Stream s) {
   const PagedSizes& z = a.z;
-  if (a.offsets) {
-    const unsigned x = (unsigned)(paged_tiles(a.N, z.R, z.grp, 16) * z.Hk);
-    launch_k((k_paged_attn<T, HD, true>), dim3(x, a.nsplit), dim3(64 * PATT_WAVES), 0, s, a);
-    if (a.nsplit > 1) launch_k((k_paged_join<T, HD, true>), dim3(x, 4), dim3(256), 0, s, a);
-  } else {
-    const unsigned x = (unsigned)z.R * z.Hk;
-    launch_k((k_paged_attn<T, HD, false>), dim3(x, a.nsplit), dim3(64 * PATT_WAVES), 0, s, a);
-    if (a.nsplit > 1) launch_k((k_paged_join<T, HD, false>), dim3(x, (z.grp + 3) / 4), dim3(256), 0, s, a);
+  const dim3 block(64 * PATT_WAVES);
+  if constexpr (sizeof(T) == 4) if (a.offsets) {
+    const int tiles = (int)paged_tiles(a.N, z.R, z.grp, 16);
+    launch_k(a.nsplit > 1 ? k_paged_attn<T, HD, true, true> : k_paged_attn<T, HD, true, false>, dim3(tiles * z.Hk, a.nsplit), block, 0, s, a);
+    if (a.nsplit > 1) launch_k((k_paged_join<T, HD, true>), dim3(tiles * z.Hk, 4), dim3(256), 0, s, a, tiles);
+    return 0;
   }
+  const int tiles = z.R + a.nsplit;  // a share more for the end of each row
+  launch_k(a.nsplit > 0 ? k_paged_attn<T, HD, false, true> : k_paged_attn<T, HD, false, false>, dim3(tiles * z.Hk), block, 0, s, a);
+  if (a.nsplit > 0) launch_k((k_paged_join<T, HD, false>), dim3(z.R * z.Hk, (z.grp + 3) / 4), dim3(256), 0, s, a, tiles);
   return 0;
 }
 
@@ -792,14 +864,14 @@ int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, Stream s) 
 int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s) {
   if (a.parent) launch_k(k_paged_take, dim3(a.z.R), dim3(256), 0, s, a);
   launch_k(k_paged_give, dim3(1), dim3(GIVE_THREADS), 0, s, a);
-  launch_k(k_paged_copy, dim3(1024), dim3(COPY_THREADS), 0, s, c, (const int*)a.taken, (const int*)(a.parent ? a.span : nullptr), a.table, a.z.R,
-           a.z.row_pages);
+  const PagedTables t{a.z, a.table, a.taken, a.parent ? a.span : nullptr, nullptr, nullptr, nullptr};
+  launch_k(k_paged_copy, dim3(1024), dim3(COPY_THREADS), 0, s, c, t);
   return 0;
 }
 int launch_paged_compact(const PagedCompactArgs& a, const PagedCopyArgs& c, Stream s) {
   launch_k(k_paged_compact, dim3(1), dim3(GIVE_THREADS), 0, s, a);
-  launch_k(k_paged_remap, dim3(a.z.R), dim3(256), 0, s, a);
-  launch_k(k_paged_copy, dim3(2048), dim3(COPY_THREADS), 0, s, c, (const int*)nullptr, (const int*)nullptr, (int*)nullptr, 0, 0);
+  const PagedTables t{a.z, a.table, nullptr, nullptr, a.map, a.kv_len, a.err};
+  launch_k(k_paged_copy, dim3(2048), dim3(COPY_THREADS), 0, s, c, t);
   return 0;
 }
 

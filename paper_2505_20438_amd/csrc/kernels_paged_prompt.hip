@@ -204,30 +204,37 @@ __device__ __forceinline__ void see_nonfinite(const u4* v, int base, int limit, 
 
 // The rows' shares of QR query rows: those of the row with the most slots first, and of a row the last first (its keys are the
 // most), so that the workgroups that take longest start first.  Rows past the 64th in the order they have.
+struct PromptShare {
+  int r, at, offset, count, slots;  // row (< 0: none left), share of it; its packed tokens and slots
+};
 template <int QR>
-__device__ __forceinline__ Share prompt_share(const PagedAttnArgs& a, int i) {
+__device__ __forceinline__ PromptShare prompt_share(const PagedAttnArgs& a, int i) {
   const int R = a.z.R, lane = threadIdx.x & 63;
-  const auto need = [&](int r) { return max(0, (prompt_count(a, r) * a.z.grp + QR - 1) / QR); };
-  Share s{-1, 0};
-  int n = 0;
-  if (R <= 64) {
-    n = lane < R ? need(lane) : 0;
-    const int key = lane < R ? a.kv_len[lane] : -1;
-    int before = 0;
-    for (int j = 0; j < R; ++j) {
-      const int kj = __builtin_amdgcn_readlane(key, j), nj = __builtin_amdgcn_readlane(n, j);
-      before += kj > key || (kj == key && j < lane) ? nj : 0;
-    }
-    const uint64_t hit = __ballot(i >= before && i < before + n);
-    if (hit == 0) return s;
-    s.r = __builtin_ctzll(hit);
-    n = __builtin_amdgcn_readlane(n, s.r);
-    s.at = n - 1 - (i - __builtin_amdgcn_readlane(before, s.r));
-    return s;
+  const auto shares = [&](int c) { return max(0, (c * a.z.grp + QR - 1) / QR); };
+  if (R > 64) {
+    const Share s = find_share(R, i, [&](int r) { return shares(prompt_count(a, r)); });
+    if (s.r < 0) return PromptShare{-1, 0, 0, 0, 0};
+    const int o = scalar_at(a.offsets, s.r), c = scalar_at(a.offsets + 1, s.r) - o;
+    return PromptShare{s.r, shares(c) - 1 - s.at, o, c, scalar_at(a.kv_len, s.r)};
   }
-  s = find_share(R, i, need);
-  if (s.r >= 0) s.at = need(s.r) - 1 - s.at;
-  return s;
+  int o = 0, c = -1, len = -1;  // of row `lane`: one round trip for all that is asked of it
+  if (lane < R) {
+    o = a.offsets[lane];
+    const int e = a.offsets[lane + 1];
+    len = a.kv_len[lane];
+    c = o >= 0 && e >= o && e <= a.N && len <= a.kv_max && e - o <= len ? e - o : -1;
+  }
+  const int n = shares(c);
+  int before = 0;
+  for (int j = 0; j < R; ++j) {
+    const int kj = __builtin_amdgcn_readlane(len, j), nj = __builtin_amdgcn_readlane(n, j);
+    before += kj > len || (kj == len && j < lane) ? nj : 0;
+  }
+  const uint64_t hit = __ballot(i >= before && i < before + n);
+  if (hit == 0) return PromptShare{-1, 0, 0, 0, 0};
+  const int r = __builtin_ctzll(hit);
+  return PromptShare{r, __builtin_amdgcn_readlane(n, r) - 1 - (i - __builtin_amdgcn_readlane(before, r)), __builtin_amdgcn_readlane(o, r),
+                     __builtin_amdgcn_readlane(c, r), __builtin_amdgcn_readlane(len, r)};
 }
 
 template <int HD, int KS>
@@ -241,9 +248,9 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   if (blockIdx.x == 0 && split == 0)
     for (int i = threadIdx.x; i < z.R; i += 512)
       if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
-  const Share sh = prompt_share<QR>(a, job);
+  const PromptShare sh = prompt_share<QR>(a, job);
   if (sh.r < 0) return;
-  const int r = sh.r, o0 = scalar_at(a.offsets, r), c = scalar_at(a.offsets + 1, r) - o0, held = scalar_at(a.kv_len, r) - c;
+  const int r = sh.r, o0 = sh.offset, c = sh.count, held = sh.slots - c;
   const int qt = w % QT, ks = w / QT;
   const int i0 = sh.at * QR + qt * 32, i1 = min(i0 + 32, c * z.grp);  // this wave's rows [i0, i1), of c * grp
   const bool rows_ok = i0 < c * z.grp;
@@ -323,7 +330,6 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     constexpr int NP = decltype(planes)::value;
     for (int j = 0; j < full * NBS; ++j) {
       const int u = j / NBS, b = j % NBS;
-      if (b == 0 && u + 2 < cnt) issue(u + 2);
       if (j > 0) {
         block_values<HD, NP>(values_of((j - 1) / NBS, (j - 1) % NBS), vf, pp, o);
         s = block_scores<HD>(keys_of(u, b), qh, ql);
@@ -332,6 +338,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
         s = block_scores<HD>(keys_of(u, b), qh, ql);
       }
       __builtin_amdgcn_sched_barrier(0);
+      if (b == 0 && u + 2 < cnt) issue(u + 2);  // with the products under way: before them they hold back their LDS reads
       block_weights<HD, NP>(s, false, 0, sc, mrun, lrun, o, pp);
       first_values<HD>(values_of(u, b), vf);
       __builtin_amdgcn_sched_barrier(0);
@@ -441,10 +448,9 @@ __global__ __launch_bounds__(256) void k_paged_prompt_join(PagedAttnArgs a) {
   const PagedSizes& z = a.z;
   const int lane = threadIdx.x & 63, j = blockIdx.y * 4 + (threadIdx.x >> 6);
   const int job = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
-  const Share s = prompt_share<QR>(a, job);
-  if (s.r < 0) return;
-  const int o = a.offsets[s.r], c = a.offsets[s.r + 1] - o, i = s.at * QR + j;
-  if (i >= c * z.grp) return;
+  const PromptShare s = prompt_share<QR>(a, job);
+  const int o = s.offset, c = s.count, i = s.at * QR + j;
+  if (s.r < 0 || i >= c * z.grp) return;
   float v[V];
   join_row<HD>(a.part, a.part + (size_t)gridDim.x * a.nsplit * QR * HD, (size_t)blockIdx.x * a.nsplit * QR + j, QR, a.nsplit, v);
 #pragma unroll

@@ -116,9 +116,27 @@ inline long long paged_tiles(long long N, long long R, long long grp, long long 
   return std::min(N, (N * grp + (width - 1) * R) / width);
 }
 
-// Splits of the paged attention (kernels_paged.hip) for `tiles` tiles of Hk kv heads each over up to kv_max slots in blocks of
-// `block` slots: workgroups for two of them a CU, a block at least for each of a workgroup's eight waves.
-inline int paged_attn_splits(long long tiles, int Hk, int hd, int kv_max, int block) {
+// Attention of one token over pages (kernels_paged.hip): whether its slots are split over workgroups, which a second launch then
+// joins, for R rows of which the longest has kv_max slots, in blocks of 16 KB (head dim 128) of K and V.  A workgroup of four
+// waves takes about 5 us and 0.6 us for each four blocks, a join 3 to 5.  Split / not, us: 1 row of 2,000 slots of 8 heads of 128
+// 9.7 / 14.8, 8 x 1,000 10.8 / 10.4, 8 x 500 9.5 / 6.9, 1 x 700 of 64 8.1 / 6.4.  From 96 workgroups on memory is busy without
+// splits while all rows are long (32 x 2,560 51 / 50, 64 x 1,000 of 8 heads 42 / 43), and up to 128 blocks a long row among short
+// ones is no longer than 25 us.  The records of a split launch have room for PAGED_SPLIT_MAX_HEADS (row, q-head) pairs.
+constexpr int PAGED_SPLIT_MAX_ROWS = 256, PAGED_SPLIT_MAX_HEADS = 16384;
+inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block) {
+  const int blocks = (kv_max + block - 1) / block * hd / 128, pairs = R * Hk;
+  if (R > PAGED_SPLIT_MAX_ROWS || R * H > PAGED_SPLIT_MAX_HEADS) return false;
+  return blocks > 28 && (pairs < 96 || blocks > 128);
+}
+// Shares that the slots of all rows are cut into, for each kv head: workgroups for one, or with more rows up to four, whole rounds
+// over the CUs (at 8 kv heads a round is 32; 4 x 33,300 slots, us, 24 shares 78, 32 77, 40 93, 48 85, 64 77, 72 89; 16 x 8,300
+// 32 shares 92, 64 79, 96 84; 48 x 8,300 32 257, 64 237, 96 225, 128 228).  No share is less than PAGED_LEAST_BLOCKS, two for each
+// of the four waves.
+constexpr int PAGED_LEAST_BLOCKS = 8;
+inline int paged_attn_shares(int R, int Hk) { return std::max(1, 256 * std::min(4, 1 + R * Hk / 128) / Hk); }
+
+// Splits of packed rows in tiles of 16 (fp32 prompts): two workgroups a CU, eight blocks at least each.
+inline int paged_tile_splits(long long tiles, int Hk, int kv_max, int block) {
   const long long pairs = tiles * Hk;
   const int blocks = (kv_max + block - 1) / block;
   const long long most = std::max<long long>(1, std::min<long long>({(blocks + 7) / 8, 1024 / pairs, 64}));

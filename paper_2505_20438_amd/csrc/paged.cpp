@@ -112,7 +112,8 @@ int ham_op_paged_attention(const ham_paged_shape* p, const void* d_q, const void
   a.z = sizes_of(p);
   a.kv_max = kv_max; a.q = d_q; a.out = d_out; a.pool = d_pool; a.table = d_table; a.kv_len = d_kv_len; a.enable = d_enable;
   a.err = d_err; a.part = (float*)d_workspace;
-  a.nsplit = paged_attn_splits(p->rows, p->n_kv_heads, p->head_dim, kv_max, p->dtype == HAM_BF16 ? 32 : 16);
+  a.nsplit = paged_attn_split(p->rows, p->n_heads, p->n_kv_heads, p->head_dim, kv_max, p->dtype == HAM_BF16 ? 32 : 16)
+                 ? paged_attn_shares(p->rows, p->n_kv_heads) : 0;
   return launched(launch_paged_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
 }
 
@@ -133,7 +134,7 @@ int ham_op_paged_prompt(const ham_paged_shape* p, int32_t n_tokens, const void* 
   a.N = n_tokens; a.kv_max = kv_max; a.q = d_q; a.out = d_out; a.pool = d_pool; a.offsets = d_offsets; a.table = d_table;
   a.kv_len = d_kv_len; a.err = d_err; a.part = (float*)d_workspace;
   if (p->dtype == HAM_F32) {
-    a.nsplit = paged_attn_splits(paged_tiles(n_tokens, p->rows, grp, 16), p->n_kv_heads, p->head_dim, kv_max, 16);
+    a.nsplit = paged_tile_splits(paged_tiles(n_tokens, p->rows, grp, 16), p->n_kv_heads, kv_max, 16);
     return launched(launch_paged_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
   }
   const PagedPromptGrid g = paged_prompt_grid(n_tokens, p->rows, p->n_kv_heads, grp, kv_max);

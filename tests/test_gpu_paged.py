@@ -157,7 +157,7 @@ ATTENTION = [
     (BF16, 32, 8, 64, 32, [700]), (BF16, 32, 8, 128, 16, [1, 0, 15, 16, 17, 31, 32, 33]), (BF16, 32, 8, 128, 64, [4097, 1]),
     (F32, 4, 2, 64, 16, [1, 2, 15, 16, 17, 100]), (BF16, 16, 1, 128, 256, [3000, 257, 255]), (BF16, 9, 3, 64, 32, [2000, 40, 1999, 65]),
     (F32, 32, 8, 128, 32, [511, 513, 700]), (F32, 16, 1, 64, 128, [9000, 5]), (BF16, 8, 8, 128, 16, [700] * 40), (BF16, 5, 1, 64, 16, [33000]),
-    (BF16, 7, 7, 128, 32, [300, 20000]), (BF16, 32, 8, 128, 32, [4096] + [70] * 70), (F32, 3, 3, 128, 16, [2500, 0, 16])]
+    (BF16, 7, 7, 128, 32, [300, 20000]), (BF16, 8, 2, 64, 32, [9000] + [3, 0, 500] * 30), (F32, 2, 2, 64, 16, [4000, 33] * 40), (BF16, 32, 8, 128, 32, [4096] + [70] * 70), (F32, 3, 3, 128, 16, [2500, 0, 16])]
 
 
 @pytest.mark.parametrize("dtype,H,Hk,hd,P,lens", ATTENTION)

@@ -183,14 +183,16 @@ def rules():
         src, out = os.path.join(d, "r.cpp"), os.path.join(d, "r.so")
         with open(src, "w") as f:
             f.write('#include "launch_rules.h"\nextern "C" {\n'
-                    'int splits(long long tiles, int Hk, int hd, int kv_max, int block) { return ham::paged_attn_splits(tiles, Hk, hd, kv_max, block); }\n'
+                    'int split(int R, int H, int Hk, int hd, int kv_max, int block) { return ham::paged_attn_split(R, H, Hk, hd, kv_max, block); }\n'
+                    'int shares_of(int R, int Hk) { return ham::paged_attn_shares(R, Hk); }\n'
+                    'int tile_splits(long long tiles, int Hk, int kv_max, int block) { return ham::paged_tile_splits(tiles, Hk, kv_max, block); }\n'
                     'int shares(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).shares; }\n'
                     'int prompt_splits(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).splits; }\n'
                     'long long tiles(long long N, long long R, long long grp, long long width) { return ham::paged_tiles(N, R, grp, width); }\n}\n')
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc, src, "-o", out], check=True)
         r = ctypes.CDLL(out)
         r.tiles.argtypes, r.tiles.restype = [ctypes.c_longlong] * 4, ctypes.c_longlong
-        r.splits.argtypes = [ctypes.c_longlong] + [ctypes.c_int] * 4
+        r.tile_splits.argtypes = [ctypes.c_longlong] + [ctypes.c_int] * 3
         yield r
 
 
@@ -198,15 +200,34 @@ RECORDS = 1 << 15   # query rows times splits that a workspace has room for
 
 
 def test_splits_have_work_and_their_records_fit(rules):
-    for tiles in (1, 2, 3, 5, 8, 31, 32, 33, 64, 100, 4096):
+    for tiles in (1, 2, 3, 5, 8, 31, 32, 33, 64, 100, 256, 257, 4096):
         for hk, grp in ((1, 1), (1, 16), (2, 2), (3, 3), (8, 4), (8, 16), (32, 1), (64, 16), (1024, 1)):
-            for hd in (64, 128):
-                for block in (16, 32):
-                    for kv in (0, 1, 16, 33, 250, 256, 257, 700, 2560, 33300, 1 << 20, 1 << 24):
-                        n = rules.splits(tiles, hk, hd, kv, block)
-                        assert 1 <= n <= 64
-                        assert n == 1 or (n - 1) * 8 * block < kv           # every split has a block
-                        assert n == 1 or tiles * hk * n * 16 <= RECORDS
+            for kv in (0, 1, 16, 33, 250, 256, 257, 700, 2560, 33300, 1 << 20, 1 << 24):
+                n = rules.tile_splits(tiles, hk, kv, 16)
+                assert 1 <= n <= 64
+                assert n == 1 or (n - 1) * 8 * 16 < kv              # every split has a block
+                assert n == 1 or tiles * hk * n * 16 <= RECORDS
+                for hd in (64, 128):
+                    if rules.split(tiles, hk * grp, hk, hd, kv, 32):
+                        assert kv > 28 * 32 and (tiles + rules.shares_of(tiles, hk)) * hk * grp <= RECORDS
+
+
+def shares(lens, block, n):
+    """The shares of the rows' blocks as the kernel forms them: (row, first block, blocks)."""
+    nb = [-(-x // block) for x in lens]
+    size = max(-(-sum(nb) // (n - min(len(lens), n // 2))), 8, -(-max(nb) // 64))
+    return [(r, i * size, min(size, b - i * size)) for r, b in enumerate(nb) for i in range(max(1, -(-b // size)))], size
+
+
+def test_shares_of_ragged_rows_fit_the_launch():
+    g = random.Random(1)
+    for _ in range(5000):
+        lens = [g.choice((0, 1, 40, g.randint(0, 3000), g.randint(0, 40000))) for _ in range(g.choice((1, 2, 7, 64, 65, 256)))]
+        n = g.choice((1, 4, 32, 85, 256))
+        cut, size = shares(lens, 32, n)
+        assert len(cut) <= n + len(lens) and max(sum(r == x for r, _, _ in cut) for x in range(len(lens))) <= 64
+        for r, x in enumerate(lens):
+            assert sum(c for q, _, c in cut if q == r) == -(-x // 32)
 
 
 def test_prompt_splits_have_work_and_their_records_fit(rules):
