@@ -133,7 +133,11 @@ __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
 template <typename T, int HD> struct KvBlock {
   static constexpr int E = 16 / (int)sizeof(T), B = 4 * E, KT = B / 16, NF = HD / (4 * E), ND = HD / 16;
   u4 k[KT][NF], v[ND];
-  static __device__ __forceinline__ u4 ld(const char* p, bool stream) { return stream ? ld16_stream(p) : ld16(p); }
+  // STREAM: read once, past the caches, or the 256 MB of the last one keep what no one reads again (4 x 33,300 slots 89 us without)
+  template <bool STREAM> static __device__ __forceinline__ u4 ld(const char* p) {
+    if constexpr (STREAM) return ld16_stream(p);
+    else return ld16(p);
+  }
   // !there: nothing is wanted; the pool's first bytes, which no loop of these loads then needs a branch for
   template <bool STREAM> __device__ __forceinline__ void load_k(const char* ka, const char* kb, bool there, const char* pool) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -144,7 +148,7 @@ template <typename T, int HD> struct KvBlock {
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int f = 0; f < NF; ++f) k[t][f] = ld(p + (4 * f * 16 + 8 * t) * 16, STREAM);
+      for (int f = 0; f < NF; ++f) k[t][f] = ld<STREAM>(p + (4 * f * 16 + 8 * t) * 16);
   }
   template <bool STREAM> __device__ __forceinline__ void load_v(const char* va, const char* vb, bool there, const char* pool) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -153,7 +157,7 @@ template <typename T, int HD> struct KvBlock {
     else p = va + (((g & 1) << 1 | g >> 1) * HD + r) * 16;
     p = there ? p : pool;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) v[d] = ld(p + d * 256, STREAM);
+    for (int d = 0; d < ND; ++d) v[d] = ld<STREAM>(p + d * 256);
   }
 };
 // first slot, within a block, of the E that lane group g has
@@ -285,6 +289,7 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  int odd = 0;
   Blk x;
   const int least = __builtin_amdgcn_readfirstlane(limit);  // column 0 sees least
   for (int e0 = first; e0 < nb; e0 += 64 * stride) {
@@ -354,37 +359,22 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
 #pragma unroll
         for (int e = 0; e < 4; ++e) pp[0][e] = __float_as_uint(p[e]);
       if (masked) {
-        bool odd = false;
+        u4 keep;  // what lies past the slots that are seen may be NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int left = end - mine_slot - E / 4 * i;
+          keep[i] = left >= E / 4 ? 0xFFFFFFFFu : E == 8 && left == 1 ? 0x0000FFFFu : 0u;
+        }
+        bool any = false;
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-#pragma unroll
-          for (int e = 0; e < E; ++e)  // what lies past the slots that are seen may be NaN
-            if (mine_slot + e >= end) {
-              if constexpr (E == 8) x.v[d][e / 2] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-              else x.v[d][e] = 0u;
-            }
-          if constexpr (PACKED) odd |= any_nonfinite<T>(x.v[d]);
-        }
-        if (PACKED && __any(odd)) {
-          u4 seen;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (E == 8)
-              seen[i] = (mine_slot + 2 * i < limit ? 0x3F80u : 0u) | (mine_slot + 2 * i + 1 < limit ? 0x3F800000u : 0u);
-            else seen[i] = mine_slot + i < limit ? 0x3F800000u : 0u;
-          }
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              f4 n = f4{0.f, 0.f, 0.f, 0.f};
-              Frag<T>::mma(n, mark_nonfinite<T>(x.v[d], k), seen);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[d][i] += n[i] > 0.f ? (k ? -INFINITY : INFINITY) : 0.f;  // both: NaN
-            }
+          x.v[d] &= keep;
+          if constexpr (PACKED) {  // columns see different slots: not finite values are dealt with after the loop
+            any |= any_nonfinite<T>(x.v[d]);
             drop_nonfinite<T>(x.v[d]);
           }
         }
+        if constexpr (PACKED) odd |= __any(any);
       }
 #pragma unroll
       for (int d = 0; d < ND; ++d)
@@ -393,6 +383,32 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
       x.template load_v<!PACKED>(ka + run, kb + run, more, pool);
     }
   }
+  if constexpr (PACKED)
+    if (odd)  // infinities and NaN in V into the outputs of the columns that see their slots (mark_nonfinite)
+      for (int e = first; e < nb; e += stride) {
+        const int base = e * B, s0 = base + lane_slot<T>(g);
+        if (base + B <= least) continue;
+        u4 seen;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (E == 8) seen[i] = (s0 + 2 * i < limit ? 0x3F80u : 0u) | (s0 + 2 * i + 1 < limit ? 0x3F800000u : 0u);
+          else seen[i] = s0 + i < limit ? 0x3F800000u : 0u;
+        }
+        // a lane's slots lie together, in one page; those that no column sees are not looked for
+        const int id = s0 < end ? checked_page(table[s0 >> z.lgP], z, a.err + r) : 0;
+        const char* v = mine0 + (size_t)id * page + run + ((size_t)(s0 & ((1 << z.lgP) - 1)) / E * HD + c16) * 16;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const u4 x = s0 < end ? ld16(v + d * 256) : zero16();
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            f4 n = f4{0.f, 0.f, 0.f, 0.f};
+            Frag<T>::mma(n, mark_nonfinite<T>(x, k), seen);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] += n[i] > 0.f ? (k ? -INFINITY : INFINITY) : 0.f;  // both: NaN
+          }
+        }
+      }
   // per wave: maximum, sum and unnormalised outputs of each column
   l = group_sum(l);
   if (g == 0) {
@@ -837,7 +853,7 @@ template <typename T, int HD>
 int attention_t(const PagedAttnArgs& a, Stream s) {
   const PagedSizes& z = a.z;
   const dim3 block(64 * PATT_WAVES);
-  if constexpr (sizeof(T) == 4) if (a.offsets) {
+  if (a.offsets) {
     const int tiles = (int)paged_tiles(a.N, z.R, z.grp, 16);
     launch_k(a.nsplit > 1 ? k_paged_attn<T, HD, true, true> : k_paged_attn<T, HD, true, false>, dim3(tiles * z.Hk, a.nsplit), block, 0, s, a);
     if (a.nsplit > 1) launch_k((k_paged_join<T, HD, true>), dim3(tiles * z.Hk, 4), dim3(256), 0, s, a, tiles);

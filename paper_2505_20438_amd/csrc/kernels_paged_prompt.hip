@@ -47,9 +47,9 @@ __device__ __forceinline__ f16v block_scores(const u4* kblk, const u4* qh, const
 
 // Planes of weights: three carry all 24 bits of an fp32 weight (each is the 8 leading bits of what the ones before it leave),
 // two 16 (to the nearest).  The third costs a fifth of the products, and with them, at the card's power limit, a fifth of the
-// time.  It is left out where it shows least: a sum over n slots that stays in fp32 through n / 16 products is rounded by
-// 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes (measured against 64 bits, relative 2-norm: 512
-// slots 0.3e-6 with three, 2e-6 with two).
+// time (2,048 tokens at slot 30,720 1,594 / 1,880 us).  It is left out where it shows least and costs most: in launches that fill
+// the card (KS = 1), for rows that see 16,384 slots or more.  A sum over n slots that stays in fp32 through n / 16 products is
+// itself rounded by 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes.
 constexpr int PLANES_2_FROM = 16384;  // slots that the workgroup's first row sees
 template <int NP>
 __device__ __forceinline__ void weight_planes(const float* p, u4* pp) {
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     }
     if (full > 0) block_values<HD, NP>(values_of(full - 1, NBS - 1), vf, pp, o);
   };
-  if (wg_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
+  if (KS == 1 && wg_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
   else full_stages(std::integral_constant<int, 3>{});
   const int l = lane_anew(), limit = row_of(l).limit;
   int odd = 0;

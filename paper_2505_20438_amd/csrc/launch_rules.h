@@ -135,25 +135,34 @@ inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block
 constexpr int PAGED_LEAST_BLOCKS = 8;
 inline int paged_attn_shares(int R, int Hk) { return std::max(1, 256 * std::min(4, 1 + R * Hk / 128) / Hk); }
 
-// Splits of packed rows in tiles of 16 (fp32 prompts): two workgroups a CU, eight blocks at least each.
+// Packed rows, two kernels.  k_paged_attn takes (token, q-head) pairs 16 at a time, each tile's keys shared by four waves that
+// read them for themselves; k_paged_prompt (bf16) takes 256 or 128, whose keys go through LDS once.  The first fills the card with
+// few tokens, the second does with a sixteenth of the reads.  8 kv heads of 128, 4 q-heads each, us, first / second: 1 row of 64 tokens
+// 7 / 15, of 512 21 / 28, of 1,024 45 / 44, of 1,500 77 / 60; 4 x 300 21 / 22, 32 x up to 77 34 / 23; behind 8,000 slots 8 tokens
+// 16 / 26, 128 51 / 52, 256 90 / 84; behind 33,000 32 tokens 56 / 66, 64 96 / 76; 64 rows of a token behind 2,000 slots 47 / 81.
+inline bool paged_prompt_tiles(int N, int R, int Hk, int grp, int kv_max) {
+  const long long wgs = paged_tiles(N, R, grp, 16) * Hk;
+  return (long long)N * grp <= 32ll * R || (wgs <= 2048 && wgs * kv_max <= 1600 * 2048);
+}
+// Splits of a tile's slots: two workgroups a CU, eight blocks of `block` slots at least each.
 inline int paged_tile_splits(long long tiles, int Hk, int kv_max, int block) {
   const long long pairs = tiles * Hk;
   const int blocks = (kv_max + block - 1) / block;
   const long long most = std::max<long long>(1, std::min<long long>({(blocks + 7) / 8, 1024 / pairs, 64}));
   return (int)std::min<long long>(most, std::max<long long>(1, 512 / pairs));
 }
-
-// Shares of the keys within a workgroup (1 or 2) and splits over workgroups of the prompt attention (kernels_paged_prompt.hip)
+// k_paged_prompt: shares of the keys among a workgroup's waves (2: twice the workgroups, half the rows each) and splits of them
+// over workgroups.  One row, us, 1 share / 2: 1,500 tokens from the first 84 / 60, 2,048 114 / 93, and behind 8,000 slots 594 / 595 and
+// 30,720 1,594 / 1,662; 32 rows of up to 77 tokens (376 workgroups) 23 / 31.  Splits (2 shares): 512 tokens behind 8,000 slots 241
+// unsplit, 156 in two, 163 in four; 128 227, 52 in eight, 64 in 16; 64 behind 33,000 730, 76 in 16, 91 in 32.
 struct PagedPromptGrid {
   int shares, splits;
 };
 inline PagedPromptGrid paged_prompt_grid(int N, int R, int Hk, int grp, int kv_max) {
-  const long long wide = paged_tiles(N, R, grp, 256) * Hk;
-  if (wide > 128) return PagedPromptGrid{1, 1};
-  const long long narrow = paged_tiles(N, R, grp, 128) * Hk;
+  const long long wide = paged_tiles(N, R, grp, 256) * Hk, narrow = paged_tiles(N, R, grp, 128) * Hk;
+  if (wide > 256 || (wide > 128 && kv_max > 8192)) return PagedPromptGrid{1, 1};
   const long long stages = (kv_max + 63) / 64;
-  const long long splits = std::max<long long>(1, std::min<long long>({256 / narrow, stages / 4, 32}));
-  return PagedPromptGrid{2, (int)splits};
+  return PagedPromptGrid{2, (int)std::max<long long>(1, std::min<long long>({256 / narrow, stages / 4, 32}))};
 }
 
 }  // namespace ham

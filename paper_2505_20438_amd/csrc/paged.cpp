@@ -133,8 +133,8 @@ int ham_op_paged_prompt(const ham_paged_shape* p, int32_t n_tokens, const void* 
   a.z = sizes_of(p);
   a.N = n_tokens; a.kv_max = kv_max; a.q = d_q; a.out = d_out; a.pool = d_pool; a.offsets = d_offsets; a.table = d_table;
   a.kv_len = d_kv_len; a.err = d_err; a.part = (float*)d_workspace;
-  if (p->dtype == HAM_F32) {
-    a.nsplit = paged_tile_splits(paged_tiles(n_tokens, p->rows, grp, 16), p->n_kv_heads, kv_max, 16);
+  if (p->dtype == HAM_F32 || paged_prompt_tiles(n_tokens, p->rows, p->n_kv_heads, grp, kv_max)) {
+    a.nsplit = paged_tile_splits(paged_tiles(n_tokens, p->rows, grp, 16), p->n_kv_heads, kv_max, p->dtype == HAM_F32 ? 16 : 32);
     return launched(launch_paged_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
   }
   const PagedPromptGrid g = paged_prompt_grid(n_tokens, p->rows, p->n_kv_heads, grp, kv_max);

@@ -251,6 +251,11 @@ PROMPTS = [
     (BF16, 5, 1, 64, 16, [(0, 100), (33, 13)]), (BF16, 7, 7, 64, 128, [(200, 300), (0, 129)]), (BF16, 4, 2, 128, 32, [(6000, 3)]),
     (BF16, 32, 8, 128, 32, [(10, 1)] * 70 + [(0, 40)]), (BF16, 6, 1, 128, 16, [(0, 700)]), (BF16, 1, 1, 64, 16, [(0, 1)]),
     (BF16, 16, 1, 64, 64, [(31, 33), (20000, 2)]), (BF16, 32, 8, 64, 32, [(0, 1100), (50, 900), (0, 77)]),
+    # enough tokens for the kernel of long prompts: every group size, page size and form of it, splits, rows past the 64th
+    (BF16, 16, 1, 128, 256, [(1000, 2100)]), (BF16, 9, 3, 64, 32, [(40, 1900), (0, 1800), (1, 1)]), (BF16, 5, 1, 64, 16, [(0, 3300), (33, 3300)]),
+    (BF16, 7, 7, 64, 128, [(200, 2500), (0, 2300)]), (BF16, 8, 8, 128, 64, [(0, 4200)]), (BF16, 32, 8, 128, 32, [(10, 9)] * 70 + [(0, 500)]),
+    (BF16, 32, 8, 128, 16, [(0, 1), (5, 1), (16, 3), (0, 0), (100, 65), (0, 64), (0, 1000)]), (BF16, 32, 8, 128, 64, [(33000, 64)]),
+    (BF16, 16, 1, 64, 16, [(20000, 40), (17000, 130)]), (BF16, 12, 1, 128, 32, [(0, 2800)]), (BF16, 32, 8, 128, 32, [(0, 300)] * 20),
     (F32, 4, 2, 64, 16, [(0, 64)]), (F32, 8, 8, 128, 32, [(3, 40), (0, 0), (0, 17), (90, 1)]), (F32, 9, 3, 128, 64, [(0, 130), (500, 20)]),
     (F32, 16, 1, 64, 256, [(700, 9)]), (F32, 5, 1, 128, 16, [(0, 33), (4000, 2)]), (F32, 32, 8, 64, 16, [(2, 3)] * 66)]
 
@@ -286,7 +291,9 @@ def test_no_bf16_plane_of_a_prompt_is_lost(ham, dtype, H, Hk, hd, P, rows):
 
 
 @pytest.mark.parametrize("dtype,H,Hk,hd,rows", [(BF16, 8, 2, 128, [(0, 200), (50, 70)]), (BF16, 4, 4, 64, [(300, 90), (0, 33)]),
-                                                (F32, 8, 2, 64, [(0, 70), (20, 33)]), (BF16, 16, 1, 128, [(0, 20), (64, 40)])])
+                                                (F32, 8, 2, 64, [(0, 70), (20, 33)]), (BF16, 16, 1, 128, [(0, 20), (64, 40)]),
+                                                (BF16, 32, 8, 64, [(300, 1100), (0, 33)]), (BF16, 16, 1, 128, [(30, 2150), (0, 20)]),
+                                                (BF16, 32, 8, 128, [(0, 300)] * 20)])
 @pytest.mark.parametrize("bad", [float("nan"), INF, -INF])
 def test_what_is_not_finite_reaches_the_tokens_that_see_it_and_no_other(ham, dtype, H, Hk, hd, rows, bad):
     offsets, lens, N = packed(rows, 0)
@@ -302,7 +309,7 @@ def test_what_is_not_finite_reaches_the_tokens_that_see_it_and_no_other(ham, dty
         pool.append(0, at, k[None], v[None])
         out, err = prompt(ham, s, pool, q, offsets, lens)
         pool.data.copy_(good)
-        assert err == [0, 0]
+        assert err == [0] * len(rows)
         a, b = values(out, H, hd, dtype), values(clean, H, hd, dtype)
         group = slice(0, H // Hk)           # the q-heads of kv head 0
         seen = torch.zeros(N, dtype=torch.bool)
@@ -316,18 +323,51 @@ def test_what_is_not_finite_reaches_the_tokens_that_see_it_and_no_other(ham, dty
             assert torch.isnan(a[seen][:, group]).all()
 
 
-def test_prompt_rows_that_do_not_fit_are_left(ham):
-    rows = [(10, 20), (0, 30), (5, 5), (40, 9)]
+@pytest.mark.parametrize("dtype,H,rows", [(BF16, 4, [(10, 20), (0, 30), (5, 5), (40, 9)]), (F32, 4, [(10, 20), (0, 30), (5, 5), (40, 9)]),
+                                          (BF16, 32, [(10, 1000), (0, 30), (5, 5), (1040, 9)])])
+def test_prompt_rows_that_do_not_fit_are_left(ham, dtype, H, rows):
     offsets, lens, N = packed(rows, 0)
-    for dtype in (BF16, F32):
-        s, pool, g = rows_of_pages(ham, dtype, 4, 2, 64, 16, lens)
-        q, qd = queries(g, N, 4, 64, dtype)
-        want = pool.prompt(qd, offsets, lens)[0]
-        out, err = prompt(ham, s, pool, q, offsets, [30, 29, -1, 50], kv_max=49)   # fewer slots than tokens, none, more than kv_max
-        assert err == [0, 8, 8, 8] and torch.all(out[20:] == 7)
-        near(values(out, 4, 64, dtype)[:20], want[:20], dtype)
-        out, err = prompt(ham, s, pool, q, [0, 20, 10, 15, N + 1], lens)
-        assert err == [0, 8, 0, 8]
+    s, pool, g = rows_of_pages(ham, dtype, H, 2, 64, 16, lens)
+    q, qd = queries(g, N, H, 64, dtype)
+    want, n = pool.prompt(qd, offsets, lens)[0], rows[0][1]
+    # fewer slots than tokens, none, more than kv_max
+    out, err = prompt(ham, s, pool, q, offsets, [lens[0], 29, -1, lens[3] + 1], kv_max=lens[3])
+    assert err == [0, 8, 8, 8] and torch.all(out[n:] == 7)
+    near(values(out, H, 64, dtype)[:n], want[:n], dtype)
+    out, err = prompt(ham, s, pool, q, [0, n, n - 10, n - 5, N + 1], lens)
+    assert err == [0, 8, 0, 8]
+
+
+def test_a_bad_page_of_a_long_prompt_is_reported(ham):
+    rows = [(0, 600), (0, 700)]
+    offsets, lens, N = packed(rows, 0)
+    s, pool, g = rows_of_pages(ham, BF16, 32, 8, 64, 16, lens)
+    pool.data.nan_to_num_()
+    q, qd = queries(g, N, 32, 64, BF16)
+    table = [list(t) for t in pool.table]
+    table[0][20], table[1][44] = -5, 1 << 30       # the second lies behind the row's slots
+    out, err = prompt(ham, s, pool, q, offsets, lens, table=table)
+    assert err == [32, 0]
+    near(values(out, 32, 64, BF16)[600:], pool.prompt(qd, offsets, lens)[0][600:], BF16)
+
+
+def test_long_prompts_of_scores_of_minus_infinity(ham):
+    rows = [(0, 1100), (40, 60)]
+    offsets, lens, N = packed(rows, 0)
+    s, pool, g = rows_of_pages(ham, BF16, 32, 8, 64, 32, lens)
+    k, v = pool.keys_values(1, 100)
+    k[:] = -2.0 ** 70
+    k[:, 70:] = 0
+    pool.append(1, 0, k.transpose(0, 1), v.transpose(0, 1))
+    x = torch.randn(N, 2048, generator=g)
+    x[1100:] = 2.0 ** 70
+    q = act_rows(torch, x, BF16)
+    qd = from_act(torch, q, 2048, BF16).double().view(N, 32, 64)
+    out, err = prompt(ham, s, pool, q, offsets, lens)
+    got, want = values(out, 32, 64, BF16), pool.prompt(qd, offsets, lens)[0]
+    assert torch.all(got[1100:1130] == 0) and err == [0, 0]   # tokens at slots 40 .. 69 see such scores alone
+    near(got[:1100], want[:1100], BF16)
+    near(got[1130:], want[1130:], BF16)
 
 
 def test_a_prompt_is_what_its_tokens_are_one_by_one(ham):
@@ -532,6 +572,52 @@ def test_prompts_beams_and_decode_steps_captured_and_replayed(ham, dtype, hd, P)
                 ref.append(r, 0, *history[r])
             qd = values(loops[0].q, H, hd, dtype)
             near(values(loops[0].out, H, hd, dtype), ref.attention(qd, end)[0], dtype)
+
+
+def test_long_prompts_whose_pages_move(ham):
+    """Chunks of two long prompts, appended and attended over in turn with other rows forked, freed and the pool compacted between:
+    each call sees the tables that the one before has written; replayed from a graph too."""
+    s = ham.paged_shape(BF16, 3, 32, 8, 64, 32, 260, 80)
+    g = torch.Generator().manual_seed(14)
+    a, x = Loop(ham, s, 1100), [tokens(g, s, 1100) for _ in range(2)]
+    off = [i32([0, 1000, 1000, 1100]), i32([0, 30, 30, 1100])]
+    counts = [[1000, 0, 100], [30, 0, 1070]]
+    lens = [0, 0, 0]
+    kv = [[], [], []]
+    n, used = i32([0] * s.n_pages), i32([0])
+    for step in range(2):
+        a.step(x[step], off[step], None, i32(counts[step]))
+        k, v = kv_of(x[step], s)
+        o = off[step].tolist()
+        for r in range(3):
+            lens[r] += counts[step][r]
+            kv[r].append((k[o[r]:o[r + 1]], v[o[r]:o[r + 1]]))
+        first = a.out.clone()
+        for parent in ([0, 0, 2], [0, -1, 2]):   # row 1 forks row 0, and is freed
+            ham.ham_op_paged_advance(s, 1, i32(parent), i32([0, 5 if parent[1] == 0 else 0, 0]), a.kv_len, a.start, a.table, a.refs, a.pool,
+                                     a.err, a.ws, stream())
+        ham.ham_op_paged_compact(s, 1, a.kv_len, a.table, a.refs, a.pool, n, used, a.err, a.ws, stream())
+
+        def again():
+            ham.ham_op_paged_prompt(s, a.q, off[step], a.pool, a.table, a.kv_len, s.row_pages * 32, a.out, a.err, a.ws, stream())
+        a.out.zero_()
+        again()
+        assert torch.equal(a.out, first) and a.err.tolist() == [0, 0, 0] and a.kv_len.tolist() == lens
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            again()
+        for _ in range(3):
+            a.out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(a.out, first)
+    ref = Pool(ham.paged_shape(BF16, 3, 32, 8, 64, 32, 240, 80))
+    ref.table = [list(range(80 * r, 80 * r + 80)) for r in range(3)]
+    for r in range(3):
+        ref.append(r, 0, torch.cat([t[0] for t in kv[r]]), torch.cat([t[1] for t in kv[r]]))
+    want = ref.prompt(values(a.q, 32, 64, BF16), off[1].tolist(), lens)[0]
+    near(values(a.out, 32, 64, BF16), want, BF16)
 
 
 def test_two_streams_read_one_pool(ham):

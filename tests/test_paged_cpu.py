@@ -188,6 +188,7 @@ def rules():
                     'int tile_splits(long long tiles, int Hk, int kv_max, int block) { return ham::paged_tile_splits(tiles, Hk, kv_max, block); }\n'
                     'int shares(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).shares; }\n'
                     'int prompt_splits(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).splits; }\n'
+                    'int as_tiles(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_tiles(N, R, Hk, grp, kv_max); }\n'
                     'long long tiles(long long N, long long R, long long grp, long long width) { return ham::paged_tiles(N, R, grp, width); }\n}\n')
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc, src, "-o", out], check=True)
         r = ctypes.CDLL(out)
@@ -238,6 +239,14 @@ def test_prompt_splits_have_work_and_their_records_fit(rules):
                     k, n = rules.shares(N, R, hk, grp, kv), rules.prompt_splits(N, R, hk, grp, kv)
                     assert k in (1, 2) and 1 <= n <= 64 and (n == 1 or (n - 1) * 64 < kv)
                     assert n == 1 or rules.tiles(N, R, grp, 256 // k) * hk * n * (256 // k) <= RECORDS
+
+
+@pytest.mark.parametrize("N,R,Hk,grp,kv,tiles,shares,splits", [
+    (64, 1, 8, 4, 64, 1, 2, 1), (512, 1, 8, 4, 512, 1, 2, 2), (1500, 1, 8, 4, 1500, 0, 2, 1), (2048, 1, 8, 4, 32768, 0, 1, 1), (64, 64, 8, 4, 33000, 1, 1, 1),
+    (64, 1, 8, 4, 33064, 0, 2, 16), (2100, 1, 1, 16, 3100, 0, 2, 1), (13000, 7, 8, 4, 4900, 0, 1, 1), (4, 1, 8, 4, 8004, 1, 2, 31)])
+def test_kernels_of_packed_rows(rules, N, R, Hk, grp, kv, tiles, shares, splits):
+    assert rules.as_tiles(N, R, Hk, grp, kv) == tiles
+    assert rules.shares(N, R, Hk, grp, kv) == shares and rules.prompt_splits(N, R, Hk, grp, kv) == splits
 
 
 def test_tiles_do_for_every_cut_of_the_tokens(rules):
