@@ -50,7 +50,7 @@ __device__ __forceinline__ f16v block_scores(const u4* kblk, const u4* qh, const
 // time (2,048 tokens at slot 30,720 1,594 / 1,880 us).  It is left out where it shows least and costs most: in launches that fill
 // the card (KS = 1), for rows that see 16,384 slots or more.  A sum over n slots that stays in fp32 through n / 16 products is
 // itself rounded by 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes.
-constexpr int PLANES_2_FROM = 16384;  // slots that the workgroup's first row sees
+constexpr int PLANES_2_FROM = 16384;  // slots that the wave's first row sees
 template <int NP>
 __device__ __forceinline__ void weight_planes(const float* p, u4* pp) {
   if constexpr (NP == 2) {
@@ -284,10 +284,12 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   // wave w loads 16 slots of K (w even) or V of a stage; groups past the end read the last one again, and are never used, so
   // that every wave has the same number of loads under way
   const auto group = [&](int st) { return min(st * 4 + (w >> 1), ngrp - 1); };
-  int next_id = st0 < nst ? scalar_at(table, group(st0) * 16 >> z.lgP) : 0;
-  const auto issue = [&](int u) {  // the loads of stage st0 + u, whose page id is there, and the id of the stage after it
-    const int st = st0 + u, slot = group(st) * 16, id = checked_page(next_id, z, a.err + r);
-    next_id = scalar_at(table, group(min(st + 1, nst - 1)) * 16 >> z.lgP);
+  const auto page_of = [&](int st) { return st0 < nst ? scalar_at(table, group(min(st, nst - 1)) * 16 >> z.lgP) : 0; };
+  int id0 = page_of(st0), id1 = page_of(st0 + 1);
+  const auto issue = [&](int u) {  // the loads of stage st0 + u, whose page id is there, and the id of the one after the next
+    const int st = st0 + u, slot = group(st) * 16, id = checked_page(id0, z, a.err + r);
+    id0 = id1;
+    id1 = page_of(st + 2);
     const BufRsrc src = buf_rsrc(mine0 + (size_t)id * page + (size_t)(slot & ((1 << z.lgP) - 1)) * (HD * 2), P::RUN * 16);
     const uint32_t at = lane_anew() * 16;
     auto* dst = (__attribute__((address_space(3))) void*)(lds[u % NS] + ((w & 1) * 4 + (w >> 1)) * P::RUN);
@@ -324,8 +326,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   landed(0);
   f16v s;
   u4 pp[2][3], vf[VFIRST];
-  // stages whose slots every row of the workgroup sees, then the others
-  const int wg_least = held + sh.at * QR / z.grp + 1, full = max(0, min(cnt, wg_least / P::ST - st0));
+  // stages whose slots every row of the wave sees, then the others (each wave by itself: the barriers are one a stage in both)
+  const int full = max(0, min(cnt, wave_least / P::ST - st0));
   const auto full_stages = [&](auto planes) {
     constexpr int NP = decltype(planes)::value;
     for (int j = 0; j < full * NBS; ++j) {
@@ -346,7 +348,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     }
     if (full > 0) block_values<HD, NP>(values_of(full - 1, NBS - 1), vf, pp, o);
   };
-  if (KS == 1 && wg_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
+  if (KS == 1 && wave_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
   else full_stages(std::integral_constant<int, 3>{});
   const int l = lane_anew(), limit = row_of(l).limit;
   int odd = 0;
