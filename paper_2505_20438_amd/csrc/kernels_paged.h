@@ -37,6 +37,8 @@ struct PagedAttnArgs {
   PagedSizes z;
   int N, kv_max, nsplit;             // N: packed query rows; nsplit: splits of a tile, or (one row per sequence) 0 or the
                                      // shares of all rows
+  int few;                           // packed rows of up to so many (token, q-head) pairs are k_paged_attn's, those of more
+                                     // k_paged_prompt's
   const void* q; void* out;          // act rows
   const void* pool;
   const int* offsets;                // of the packed rows, or null: one query row per sequence
@@ -71,7 +73,7 @@ struct PagedCopyArgs {               // pages of `copies` in each layer
 };
 
 int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s);
-int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, Stream s);   // offsets: packed rows
+int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, long long tiles, Stream s);  // tiles: of packed rows, at most
 int launch_paged_prompt(int hd, const PagedAttnArgs& a, int key_shares, Stream s);  // bf16
 int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s);
 int launch_paged_compact(const PagedCompactArgs& a, const PagedCopyArgs& c, Stream s);

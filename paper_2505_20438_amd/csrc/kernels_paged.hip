@@ -215,6 +215,12 @@ __device__ __forceinline__ RowShare row_share(const PagedAttnArgs& a, int block,
   return RowShare{-1, 0, 0, 0, 0};
 }
 
+// Tiles of a packed row, where they are this kernel's.
+__device__ __forceinline__ int few_tiles(const PagedAttnArgs& a, int r) {
+  const int n = prompt_count(a, r) * a.z.grp;
+  return n > 0 && n <= a.few ? (n + 15) / 16 : 0;
+}
+
 // One workgroup per (tile, kv head, split).  PACKED: a tile is 16 (token, q-head) pairs of a row's packed tokens, each of which
 // sees the slots up to its token's; else the q-heads of the row's newest token, which see all, and splits are shares.  The waves
 // of a workgroup take its blocks in turn; a block's K is loaded as soon as the one before it is used up, its V likewise.
@@ -235,7 +241,7 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
     if (blockIdx.x == 0 && split == 0)
       for (int i = tid; i < z.R; i += 64 * NW)
         if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
-    const Share s = find_share(z.R, tile, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
+    const Share s = find_share(z.R, tile, [&](int i) { return few_tiles(a, i); });
     if (s.r < 0) return;
     r = s.r;
     const int o = a.offsets[r], c = a.offsets[r + 1] - o;
@@ -483,7 +489,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a, int tiles) 
   size_t row = x, rec, step;
   int h = kvh * z.grp + j, ns = a.nsplit;
   if constexpr (PACKED) {
-    const Share s = find_share(z.R, x, [&](int i) { return max(0, (prompt_count(a, i) * z.grp + 15) / 16); });
+    const Share s = find_share(z.R, x, [&](int i) { return few_tiles(a, i); });
     if (s.r < 0) return;
     const int o = a.offsets[s.r], c = a.offsets[s.r + 1] - o, i = s.at * 16 + j;
     if (i >= c * z.grp) return;
@@ -850,11 +856,11 @@ int append_t(const PagedAppendArgs& a, Stream s) {
   return 0;
 }
 template <typename T, int HD>
-int attention_t(const PagedAttnArgs& a, Stream s) {
+int attention_t(const PagedAttnArgs& a, long long packed_tiles, Stream s) {
   const PagedSizes& z = a.z;
   const dim3 block(64 * PATT_WAVES);
   if (a.offsets) {
-    const int tiles = (int)paged_tiles(a.N, z.R, z.grp, 16);
+    const int tiles = (int)packed_tiles;
     launch_k(a.nsplit > 1 ? k_paged_attn<T, HD, true, true> : k_paged_attn<T, HD, true, false>, dim3(tiles * z.Hk, a.nsplit), block, 0, s, a);
     if (a.nsplit > 1) launch_k((k_paged_join<T, HD, true>), dim3(tiles * z.Hk, 4), dim3(256), 0, s, a, tiles);
     return 0;
@@ -865,17 +871,17 @@ int attention_t(const PagedAttnArgs& a, Stream s) {
   return 0;
 }
 
-#define PAGED_DISPATCH(fn)                                                  \
+#define PAGED_DISPATCH(fn, ...)                                             \
   do {                                                                      \
-    if (hd == 64) return dtype == 1 ? fn<bf16, 64>(a, s) : fn<float, 64>(a, s);    \
-    if (hd == 128) return dtype == 1 ? fn<bf16, 128>(a, s) : fn<float, 128>(a, s); \
+    if (hd == 64) return dtype == 1 ? fn<bf16, 64>(__VA_ARGS__) : fn<float, 64>(__VA_ARGS__);    \
+    if (hd == 128) return dtype == 1 ? fn<bf16, 128>(__VA_ARGS__) : fn<float, 128>(__VA_ARGS__); \
     return -1;                                                              \
   } while (0)
 
 }  // namespace
 
-int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s) { PAGED_DISPATCH(append_t); }
-int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, Stream s) { PAGED_DISPATCH(attention_t); }
+int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s) { PAGED_DISPATCH(append_t, a, s); }
+int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, long long tiles, Stream s) { PAGED_DISPATCH(attention_t, a, tiles, s); }
 
 int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s) {
   if (a.parent) launch_k(k_paged_take, dim3(a.z.R), dim3(256), 0, s, a);

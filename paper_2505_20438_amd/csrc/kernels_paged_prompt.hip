@@ -210,7 +210,7 @@ struct PromptShare {
 template <int QR>
 __device__ __forceinline__ PromptShare prompt_share(const PagedAttnArgs& a, int i) {
   const int R = a.z.R, lane = threadIdx.x & 63;
-  const auto shares = [&](int c) { return max(0, (c * a.z.grp + QR - 1) / QR); };
+  const auto shares = [&](int c) { return c * a.z.grp > a.few ? (c * a.z.grp + QR - 1) / QR : 0; };
   if (R > 64) {
     const Share s = find_share(R, i, [&](int r) { return shares(prompt_count(a, r)); });
     if (s.r < 0) return PromptShare{-1, 0, 0, 0, 0};

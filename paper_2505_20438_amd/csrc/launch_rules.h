@@ -144,6 +144,10 @@ inline bool paged_prompt_tiles(int N, int R, int Hk, int grp, int kv_max) {
   const long long wgs = paged_tiles(N, R, grp, 16) * Hk;
   return (long long)N * grp <= 32ll * R || (wgs <= 2048 && wgs * kv_max <= 1600 * 2048);
 }
+// ... and where the second takes a call of several rows, those of up to so many pairs are the first's all the same: a new token among
+// prompts would hold a workgroup of the second for all its slots (7 rows of one token behind 8,000 slots and a prompt of 2,000: 275 us
+// in the second alone, 181 in both, the prompt by itself 95; 31 such rows 384 and 333).
+constexpr int PAGED_FEW = 32;
 // Splits of a tile's slots: two workgroups a CU, eight blocks of `block` slots at least each.
 inline int paged_tile_splits(long long tiles, int Hk, int kv_max, int block) {
   const long long pairs = tiles * Hk;

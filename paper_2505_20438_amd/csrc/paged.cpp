@@ -114,7 +114,7 @@ int ham_op_paged_attention(const ham_paged_shape* p, const void* d_q, const void
   a.err = d_err; a.part = (float*)d_workspace;
   a.nsplit = paged_attn_split(p->rows, p->n_heads, p->n_kv_heads, p->head_dim, kv_max, p->dtype == HAM_BF16 ? 32 : 16)
                  ? paged_attn_shares(p->rows, p->n_kv_heads) : 0;
-  return launched(launch_paged_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
+  return launched(launch_paged_attention(p->dtype, p->head_dim, a, 0, (hipStream_t)hip_stream));
 }
 
 int ham_op_paged_prompt(const ham_paged_shape* p, int32_t n_tokens, const void* d_q, const int32_t* d_offsets, const void* d_pool,
@@ -133,9 +133,13 @@ int ham_op_paged_prompt(const ham_paged_shape* p, int32_t n_tokens, const void* 
   a.z = sizes_of(p);
   a.N = n_tokens; a.kv_max = kv_max; a.q = d_q; a.out = d_out; a.pool = d_pool; a.offsets = d_offsets; a.table = d_table;
   a.kv_len = d_kv_len; a.err = d_err; a.part = (float*)d_workspace;
-  if (p->dtype == HAM_F32 || paged_prompt_tiles(n_tokens, p->rows, p->n_kv_heads, grp, kv_max)) {
-    a.nsplit = paged_tile_splits(paged_tiles(n_tokens, p->rows, grp, 16), p->n_kv_heads, kv_max, p->dtype == HAM_F32 ? 16 : 32);
-    return launched(launch_paged_attention(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
+  const bool all = p->dtype == HAM_F32 || paged_prompt_tiles(n_tokens, p->rows, p->n_kv_heads, grp, kv_max);
+  a.few = all ? INT32_MAX : p->rows > 1 ? PAGED_FEW : 0;
+  if (a.few > 0) {
+    const long long most = paged_tiles(n_tokens, p->rows, grp, 16), tiles = all ? most : std::min(most, PAGED_FEW / 16 * (long long)p->rows);
+    a.nsplit = paged_tile_splits(tiles, p->n_kv_heads, kv_max, p->dtype == HAM_F32 ? 16 : 32);
+    if (int rc = launched(launch_paged_attention(p->dtype, p->head_dim, a, tiles, (hipStream_t)hip_stream))) return rc;
+    if (all) return HAM_OK;
   }
   const PagedPromptGrid g = paged_prompt_grid(n_tokens, p->rows, p->n_kv_heads, grp, kv_max);
   a.nsplit = g.splits;

@@ -255,7 +255,7 @@ PROMPTS = [
     (BF16, 16, 1, 128, 256, [(1000, 2100)]), (BF16, 9, 3, 64, 32, [(40, 1900), (0, 1800), (1, 1)]), (BF16, 5, 1, 64, 16, [(0, 3300), (33, 3300)]),
     (BF16, 7, 7, 64, 128, [(200, 2500), (0, 2300)]), (BF16, 8, 8, 128, 64, [(0, 4200)]), (BF16, 32, 8, 128, 32, [(10, 9)] * 70 + [(0, 500)]),
     (BF16, 32, 8, 128, 16, [(0, 1), (5, 1), (16, 3), (0, 0), (100, 65), (0, 64), (0, 1000)]), (BF16, 32, 8, 128, 64, [(33000, 64)]),
-    (BF16, 16, 1, 64, 16, [(20000, 40), (17000, 130)]), (BF16, 12, 1, 128, 32, [(0, 2800)]), (BF16, 32, 8, 128, 32, [(0, 300)] * 20),
+    (BF16, 16, 1, 64, 16, [(20000, 40), (17000, 130)]), (BF16, 32, 8, 128, 32, [(5000, 1), (0, 1200), (33, 8), (700, 9), (0, 0), (31, 2)]), (BF16, 12, 1, 128, 32, [(0, 2800)]), (BF16, 32, 8, 128, 32, [(0, 300)] * 20),
     (F32, 4, 2, 64, 16, [(0, 64)]), (F32, 8, 8, 128, 32, [(3, 40), (0, 0), (0, 17), (90, 1)]), (F32, 9, 3, 128, 64, [(0, 130), (500, 20)]),
     (F32, 16, 1, 64, 256, [(700, 9)]), (F32, 5, 1, 128, 16, [(0, 33), (4000, 2)]), (F32, 32, 8, 64, 16, [(2, 3)] * 66)]
 
