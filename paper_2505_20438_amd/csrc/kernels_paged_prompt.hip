@@ -45,30 +45,11 @@ __device__ __forceinline__ f16v block_scores(const u4* kblk, const u4* qh, const
   return s;
 }
 
-// Planes of weights: three carry all 24 bits of an fp32 weight (each is the 8 leading bits of what the ones before it leave),
-// two 16 (to the nearest).  The third costs a fifth of the products, and with them, at the card's power limit, a fifth of the
-// time (2,048 tokens at slot 30,720 1,594 / 1,880 us).  It is left out where it shows least and costs most: in launches that fill
-// the card (KS = 1), for rows that see 16,384 slots or more.  A sum over n slots that stays in fp32 through n / 16 products is
-// itself rounded by 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes.
+// Weights enter the second product in three bf16 planes (weight_planes), all 24 bits of them, or in two.  The third costs a fifth
+// of the products, and with them, at the card's power limit, a fifth of the time.  It is left out where it shows least and costs
+// most: in launches that fill the card (KS = 1), for rows that see 16,384 slots or more.  A sum over n slots that stays in fp32
+// through n / 16 products is itself rounded by 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes.
 constexpr int PLANES_2_FROM = 16384;  // slots that the wave's first row sees
-template <int NP>
-__device__ __forceinline__ void weight_planes(const float* p, u4* pp) {
-  if constexpr (NP == 2) {
-    to_planes<2>(p, pp);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
-#pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        pp[n][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);  // the upper halves
-        if (n == 2) break;
-        x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u));
-        y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xFFFF0000u));
-      }
-    }
-  }
-}
 
 // The softmax update of (m, l, o) by a block's scores, whose weights are left in NP bf16 planes.  `keep`: how many of the
 // block's slots the lane's row sees (32 or more: all); score e is slot 16 (e / 8) + 8 h + e % 8.
