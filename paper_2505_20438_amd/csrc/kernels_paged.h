@@ -31,6 +31,7 @@ struct PagedAppendArgs {
   const float* qkv; const float* cos; const float* sin;
   const int* offsets; const int* start; const int* table;
   void* pool; void* q;               // q: act rows, or null
+  int per_step;                      // workgroups of 32 slots
   int* err;
 };
 struct PagedAttnArgs {

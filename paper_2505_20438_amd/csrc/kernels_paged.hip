@@ -17,7 +17,8 @@ namespace {
 
 // ---------------------------------------------------------------- append
 // A step is 32 slots (aligned) of a row that get new tokens.  For each step and kv head one workgroup writes K and V and, if
-// q is wanted, another rotates its q-heads; those of a step run on one XCD, whose L2 then holds the step's RoPE factors.
+// q is wanted, another rotates its q-heads (with many rows a workgroup takes several of these in turn, paged_append_groups); those
+// of a step run on one XCD, whose L2 then holds the step's RoPE factors.
 // Bound by memory.  K: a thread has 8 RoPE pairs of a slot, so that 16 lanes write 256 bytes and 4 read 128.  V: a thread has a
 // channel of the E slots that lie together; at the ends of the new tokens, where some of them are others', values one by one.
 __device__ __forceinline__ int append_count(const PagedAppendArgs& a, int r) {  // -1: does not fit
@@ -28,13 +29,13 @@ template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
   constexpr int HALF = HD / 2, E = 16 / (int)sizeof(T), B = 32;
   const PagedSizes& z = a.z;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kinds = a.q ? 2 : 1;
-  const uint32_t s8 = blockIdx.x / 8, step = s8 / (uint32_t)(kinds * z.Hk) * 8 + blockIdx.x % 8;
-  const int head = (int)(s8 % (uint32_t)(kinds * z.Hk)), kvh = head % z.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, heads = (a.q ? 2 : 1) * z.Hk;
+  const uint32_t s8 = blockIdx.x / 8, step = s8 / (uint32_t)a.per_step * 8 + blockIdx.x % 8;
   if (blockIdx.x == 0)
     for (int r = tid; r < z.R; r += 256)
       if (append_count(a, r) < 0) atomicOr(a.err + r, 8);
-  const Share sh = find_share(z.R, (int)step, [&](int r) {
+  __shared__ int scratch[10];
+  const Share sh = find_share<256>(z.R, (int)step, scratch, [&](int r) {
     const int c = append_count(a, r), s = a.start[r];
     return c > 0 ? (s + c - 1) / B - s / B + 1 : 0;
   });
@@ -43,86 +44,89 @@ __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a) {
   const int base = (s0 / B + sh.at) * B, lo = max(base, s0), hi = min(base + B, s0 + c);  // slots [lo, hi)
   const size_t ld = (size_t)(z.H + 2 * z.Hk) * HD;
   const size_t tok = (size_t)o - s0;  // packed row of slot 0
-  if (head >= z.Hk) {  // q
-    const int items = (hi - lo) * z.grp * (HALF / 8);
-    for (int q = tid; q < items; q += 256) {
-      const int i = q % (HALF / 8) * 8, hq = q / (HALF / 8), h = kvh * z.grp + hq % z.grp;
-      const size_t t = tok + lo + hq / z.grp;
-      const float* p = a.qkv + t * ld + h * HD + i;
-      f4 x[2], y[2], cs[2], sn[2];
+  for (int head = (int)(s8 % (uint32_t)a.per_step); head < heads; head += a.per_step) {
+    const int kvh = head % z.Hk;
+    if (head >= z.Hk) {  // q
+      const int items = (hi - lo) * z.grp * (HALF / 8);
+      for (int q = tid; q < items; q += 256) {
+        const int i = q % (HALF / 8) * 8, hq = q / (HALF / 8), h = kvh * z.grp + hq % z.grp;
+        const size_t t = tok + lo + hq / z.grp;
+        const float* p = a.qkv + t * ld + h * HD + i;
+        f4 x[2], y[2], cs[2], sn[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        x[u] = *reinterpret_cast<const f4*>(p + 4 * u);
-        y[u] = *reinterpret_cast<const f4*>(p + HALF + 4 * u);
-        cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
-        sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+        for (int u = 0; u < 2; ++u) {
+          x[u] = *reinterpret_cast<const f4*>(p + 4 * u);
+          y[u] = *reinterpret_cast<const f4*>(p + HALF + 4 * u);
+          cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
+          sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
+        put_act8<T>(a.q, t, z.H * HD, h * HD + i, x);
+        put_act8<T>(a.q, t, z.H * HD, h * HD + i + HALF, y);
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
-      put_act8<T>(a.q, t, z.H * HD, h * HD + i, x);
-      put_act8<T>(a.q, t, z.H * HD, h * HD + i + HALF, y);
+      continue;
     }
-    return;
-  }
-  const int* table = a.table + (size_t)r * z.row_pages;
-  const int P = 1 << z.lgP;
-  const size_t run = (size_t)P * HD;  // K, or V, of a kv head in a page
-  // where slot s's page holds the kv head, or null
-  const auto place = [&](int s) -> T* {
-    const int id = table[s >> z.lgP];
-    if ((unsigned)id >= (unsigned)z.n_pages) {
-      atomicOr(a.err + r, 32);
-      return nullptr;
-    }
-    return (T*)a.pool + ((size_t)id * z.Hk + kvh) * 2 * run;
-  };
-  const float* ksrc = a.qkv + (size_t)(z.H + kvh) * HD;
-  const float* vsrc = ksrc + (size_t)z.Hk * HD;
-  {
-    const int s = base + (w & 1) * 16 + (lane & 15), i = ((w >> 1) * 4 + (lane >> 4)) * 8;
-    if (i < HALF && s >= lo && s < hi) {
-      const size_t t = tok + s;
-      f4 x[2], y[2], cs[2], sn[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        x[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + i + 4 * u);
-        y[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + HALF + i + 4 * u);
-        cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
-        sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+    const int* table = a.table + (size_t)r * z.row_pages;
+    const int P = 1 << z.lgP;
+    const size_t run = (size_t)P * HD;  // K, or V, of a kv head in a page
+    // where slot s's page holds the kv head, or null
+    const auto place = [&](int s) -> T* {
+      const int id = table[s >> z.lgP];
+      if ((unsigned)id >= (unsigned)z.n_pages) {
+        atomicOr(a.err + r, 32);
+        return nullptr;
       }
-      T* out = place(s);
+      return (T*)a.pool + ((size_t)id * z.Hk + kvh) * 2 * run;
+    };
+    const float* ksrc = a.qkv + (size_t)(z.H + kvh) * HD;
+    const float* vsrc = ksrc + (size_t)z.Hk * HD;
+    {
+      const int s = base + (w & 1) * 16 + (lane & 15), i = ((w >> 1) * 4 + (lane >> 4)) * 8;
+      if (i < HALF && s >= lo && s < hi) {
+        const size_t t = tok + s;
+        f4 x[2], y[2], cs[2], sn[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
-      if (out != nullptr) {
-        const int at = s & (P - 1);
+        for (int u = 0; u < 2; ++u) {
+          x[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + i + 4 * u);
+          y[u] = *reinterpret_cast<const f4*>(ksrc + t * ld + HALF + i + 4 * u);
+          cs[u] = *reinterpret_cast<const f4*>(a.cos + t * HALF + i + 4 * u);
+          sn[u] = *reinterpret_cast<const f4*>(a.sin + t * HALF + i + 4 * u);
+        }
+        T* out = place(s);
 #pragma unroll
-        for (int u = 0; u < 8; u += 4) {  // of 8 channels that lie together (fp32: 4 and 4)
-          st4<T>(out + paged_k_index<E>(at, i + u, HD), x[u / 4]);
-          st4<T>(out + paged_k_index<E>(at, HALF + i + u, HD), y[u / 4]);
+        for (int u = 0; u < 2; ++u) rotate(x[u], y[u], cs[u], sn[u]);
+        if (out != nullptr) {
+          const int at = s & (P - 1);
+#pragma unroll
+          for (int u = 0; u < 8; u += 4) {  // of 8 channels that lie together (fp32: 4 and 4)
+            st4<T>(out + paged_k_index<E>(at, i + u, HD), x[u / 4]);
+            st4<T>(out + paged_k_index<E>(at, HALF + i + u, HD), y[u / 4]);
+          }
         }
       }
     }
-  }
-  for (int q = tid; q < B / E * HD; q += 256) {
-    const int d = q % HD, s = base + q / HD * E;  // slots s .. s + E - 1, in one page
-    if (s + E <= lo || s >= hi) continue;
-    float v[E];
+    for (int q = tid; q < B / E * HD; q += 256) {
+      const int d = q % HD, s = base + q / HD * E;  // slots s .. s + E - 1, in one page
+      if (s + E <= lo || s >= hi) continue;
+      float v[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = s + e >= lo && s + e < hi ? vsrc[(tok + s + e) * ld + d] : 0.f;
-    T* out = place(max(s, lo));
-    if (out == nullptr) continue;
-    out += run + paged_v_index<E>(s & (P - 1), d, HD);
-    if (s >= lo && s + E <= hi) {
-      u4 x;
-      if constexpr (E == 8) x = pack_frag_bf16(v);
-      else
+      for (int e = 0; e < E; ++e) v[e] = s + e >= lo && s + e < hi ? vsrc[(tok + s + e) * ld + d] : 0.f;
+      T* out = place(max(s, lo));
+      if (out == nullptr) continue;
+      out += run + paged_v_index<E>(s & (P - 1), d, HD);
+      if (s >= lo && s + E <= hi) {
+        u4 x;
+        if constexpr (E == 8) x = pack_frag_bf16(v);
+        else
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __float_as_uint(v[e]);
-      *reinterpret_cast<u4*>(out) = x;
-    } else {
+          for (int e = 0; e < 4; ++e) x[e] = __float_as_uint(v[e]);
+        *reinterpret_cast<u4*>(out) = x;
+      } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (s + e >= lo && s + e < hi) out[e] = from_f<T>(v[e]);
+        for (int e = 0; e < E; ++e)
+          if (s + e >= lo && s + e < hi) out[e] = from_f<T>(v[e]);
+      }
     }
   }
 }
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
     if (blockIdx.x == 0 && split == 0)
       for (int i = tid; i < z.R; i += 64 * NW)
         if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
-    const Share s = find_share(z.R, tile, [&](int i) { return few_tiles(a, i); });
+    const Share s = find_share<64 * NW>(z.R, tile, (int*)&sh, [&](int i) { return few_tiles(a, i); });
     if (s.r < 0) return;
     r = s.r;
     const int o = a.offsets[r], c = a.offsets[r + 1] - o;
@@ -485,12 +489,13 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttnArgs a, int tiles) 
   const PagedSizes& z = a.z;
   const int lane = threadIdx.x & 63, rows = PACKED ? 16 : z.grp, j = blockIdx.y * 4 + (threadIdx.x >> 6);
   const int x = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
-  if (j >= rows) return;
+  if (!PACKED && j >= rows) return;
   size_t row = x, rec, step;
   int h = kvh * z.grp + j, ns = a.nsplit;
   if constexpr (PACKED) {
-    const Share s = find_share(z.R, x, [&](int i) { return few_tiles(a, i); });
-    if (s.r < 0) return;
+    __shared__ int scratch[10];
+    const Share s = find_share<256>(z.R, x, scratch, [&](int i) { return few_tiles(a, i); });
+    if (s.r < 0 || j >= rows) return;
     const int o = a.offsets[s.r], c = a.offsets[s.r + 1] - o, i = s.at * 16 + j;
     if (i >= c * z.grp) return;
     row = (size_t)o + i / z.grp;
@@ -850,8 +855,7 @@ __global__ __launch_bounds__(GIVE_THREADS) void k_paged_compact(PagedCompactArgs
 
 template <typename T, int HD>
 int append_t(const PagedAppendArgs& a, Stream s) {
-  const long long steps = std::min<long long>(a.N, ((long long)a.N + 62ll * a.z.R) / 32);
-  const unsigned blocks = (unsigned)((steps + 7) / 8 * 8 * a.z.Hk * (a.q ? 2 : 1));
+  const unsigned blocks = (unsigned)((paged_append_steps(a.N, a.z.R) + 7) / 8 * 8 * a.per_step);
   launch_k((k_paged_append<T, HD>), dim3(blocks), dim3(256), 0, s, a);
   return 0;
 }

@@ -188,12 +188,12 @@ __device__ __forceinline__ void see_nonfinite(const u4* v, int base, int limit, 
 struct PromptShare {
   int r, at, offset, count, slots;  // row (< 0: none left), share of it; its packed tokens and slots
 };
-template <int QR>
-__device__ __forceinline__ PromptShare prompt_share(const PagedAttnArgs& a, int i) {
+template <int QR, int NT>
+__device__ __forceinline__ PromptShare prompt_share(const PagedAttnArgs& a, int i, int* scratch) {
   const int R = a.z.R, lane = threadIdx.x & 63;
   const auto shares = [&](int c) { return c * a.z.grp > a.few ? (c * a.z.grp + QR - 1) / QR : 0; };
   if (R > 64) {
-    const Share s = find_share(R, i, [&](int r) { return shares(prompt_count(a, r)); });
+    const Share s = find_share<NT>(R, i, scratch, [&](int r) { return shares(prompt_count(a, r)); });
     if (s.r < 0) return PromptShare{-1, 0, 0, 0, 0};
     const int o = scalar_at(a.offsets, s.r), c = scalar_at(a.offsets + 1, s.r) - o;
     return PromptShare{s.r, shares(c) - 1 - s.at, o, c, scalar_at(a.kv_len, s.r)};
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   if (blockIdx.x == 0 && split == 0)
     for (int i = threadIdx.x; i < z.R; i += 512)
       if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
-  const PromptShare sh = prompt_share<QR>(a, job);
+  const PromptShare sh = prompt_share<QR, 512>(a, job, (int*)lds);
   if (sh.r < 0) return;
   const int r = sh.r, o0 = sh.offset, c = sh.count, held = sh.slots - c;
   const int qt = w % QT, ks = w / QT;
@@ -431,7 +431,8 @@ __global__ __launch_bounds__(256) void k_paged_prompt_join(PagedAttnArgs a) {
   const PagedSizes& z = a.z;
   const int lane = threadIdx.x & 63, j = blockIdx.y * 4 + (threadIdx.x >> 6);
   const int job = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk);
-  const PromptShare s = prompt_share<QR>(a, job);
+  __shared__ int scratch[10];
+  const PromptShare s = prompt_share<QR, 256>(a, job, scratch);
   const int o = s.offset, c = s.count, i = s.at * QR + j;
   if (s.r < 0 || i >= c * z.grp) return;
   float v[V];

@@ -110,6 +110,16 @@ inline int kv8_attn_splits(int R, int Hk, int hd, int blocks) {
   return best;
 }
 
+// Append of N packed tokens of R rows: steps of 32 aligned slots at most, and workgroups a step, whose heads (kv heads, and with q
+// as many more for their q-heads) they take in turn.  Up to 64 rows one a head; with more of them, finding a step's row costs a
+// workgroup as much as a head's values do, so that their number is kept to APPEND_MANY.  Rows of a token, 8 kv heads of 128, us, at
+// most 8,192 / 4,096 / 2,048 of them: 256 rows 15 / 15 / 12, 512 28 / 19 / 16, 1,024 35 / 27 / 25, 4,096 134 / 119 / 119.
+inline long long paged_append_steps(long long N, long long R) { return std::min(N, (N + 62 * R) / 32); }
+constexpr int APPEND_MANY = 2048;
+inline int paged_append_groups(int N, int R, int heads) {
+  return R <= 64 ? heads : (int)std::max<long long>(1, std::min<long long>(heads, APPEND_MANY / paged_append_steps(N, R)));
+}
+
 // Shares of `width` (token, q-head) pairs, at most, of N packed tokens of R rows with grp <= width q-heads a kv head: a row's
 // last share may be partly filled, and a share has a token at least.
 inline long long paged_tiles(long long N, long long R, long long grp, long long width) {
@@ -121,12 +131,14 @@ inline long long paged_tiles(long long N, long long R, long long grp, long long 
 // waves takes about 5 us and 0.6 us for each four blocks, a join 3 to 5.  Split / not, us: 1 row of 2,000 slots of 8 heads of 128
 // 9.7 / 14.8, 8 x 1,000 10.8 / 10.4, 8 x 500 9.5 / 6.9, 1 x 700 of 64 8.1 / 6.4.  From 96 workgroups on memory is busy without
 // splits while all rows are long (32 x 2,560 51 / 50, 64 x 1,000 of 8 heads 42 / 43), and up to 128 blocks a long row among short
-// ones is no longer than 25 us.  The records of a split launch have room for PAGED_SPLIT_MAX_HEADS (row, q-head) pairs.
-constexpr int PAGED_SPLIT_MAX_ROWS = 256, PAGED_SPLIT_MAX_HEADS = 16384;
+// ones is no longer than 25 us.  With hundreds of rows, finding a share's row costs every workgroup more and short rows hide a longer
+// one: 512 rows of 300 slots and one of 8,000 183 / 153, one of 33,000 193 / 365; 512 of 5,000 1,615 / 1,570.  The records of a
+// split launch have room for PAGED_SPLIT_MAX_HEADS (row, q-head) pairs.
+constexpr int PAGED_SPLIT_MAX_HEADS = 16384;
 inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block) {
   const int blocks = (kv_max + block - 1) / block * hd / 128, pairs = R * Hk;
-  if (R > PAGED_SPLIT_MAX_ROWS || R * H > PAGED_SPLIT_MAX_HEADS) return false;
-  return blocks > 28 && (pairs < 96 || blocks > 128);
+  if (R * H > PAGED_SPLIT_MAX_HEADS) return false;
+  return blocks > 28 && (pairs < 96 || blocks > (R > 256 ? 512 : 128));
 }
 // Shares that the slots of all rows are cut into, for each kv head: workgroups for one, or with more rows up to four, whole rounds
 // over the CUs (at 8 kv heads a round is 32; 4 x 33,300 slots, us, 24 shares 78, 32 77, 40 93, 48 85, 64 77, 72 89; 16 x 8,300

@@ -91,12 +91,13 @@ int ham_op_paged_append(const ham_paged_shape* p, int32_t n_tokens, const float*
   if (n_tokens < 1 || n_tokens > (1 << 24)) return fail(HAM_EINVAL, "n_tokens must be in 1..2^24");
   if (!d_qkv || !d_cos || !d_sin || !d_offsets || !d_start || !d_table || !d_err) return fail(HAM_EINVAL, "null pointer");
   if (misaligned({d_qkv, d_cos, d_sin, d_q})) return fail(HAM_EINVAL, "buffers must be 16-byte aligned");
-  if ((std::min<long long>(n_tokens, ((long long)n_tokens + 62ll * p->rows) / 32) + 8) * p->n_kv_heads * 2 > (1 << 23))
+  if ((paged_append_steps(n_tokens, p->rows) + 8) * p->n_kv_heads * 2 > (1 << 23))
     return fail(HAM_EINVAL, "n_tokens * n_kv_heads too large for one call");
   PagedAppendArgs a{};
   a.z = sizes_of(p);
   a.N = n_tokens; a.qkv = d_qkv; a.cos = d_cos; a.sin = d_sin; a.offsets = d_offsets; a.start = d_start; a.table = d_table;
   a.pool = d_pool; a.q = d_q; a.err = d_err;
+  a.per_step = paged_append_groups(n_tokens, p->rows, p->n_kv_heads * (d_q ? 2 : 1));
   return launched(launch_paged_append(p->dtype, p->head_dim, a, (hipStream_t)hip_stream));
 }
 

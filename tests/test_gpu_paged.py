@@ -151,6 +151,13 @@ def test_append_that_does_not_fit_writes_nothing(ham):
                 assert torch.equal(dev[:, pages].cpu().view(torch.int16), pool.data[:, pages].view(torch.int16)), r
 
 
+@pytest.mark.parametrize("dtype,count", [(BF16, [i % 3 for i in range(1300)]), (F32, [0] * 1100 + [40, 0, 1] * 30), (BF16, [1] * 257),
+                                         (BF16, [0] * 4095 + [70])])
+def test_append_of_hundreds_of_rows(ham, dtype, count):
+    start = [i % 37 for i in range(len(count))]
+    test_append_writes_what_it_says_and_nothing_else(ham, dtype, 6, 3, 64, 16, start, count)
+
+
 # ---------------------------------------------------------------- attention of one token
 # dtype, q-heads, kv heads, head dim, page, slots of each row
 ATTENTION = [
@@ -167,6 +174,12 @@ def test_attention_of_one_token(ham, dtype, H, Hk, hd, P, lens):
     got, err = attend(ham, s, pool, q, lens)
     near(got, pool.attention(qd, lens)[0], dtype)
     assert err == [0] * len(lens)
+
+
+def test_a_long_row_among_hundreds(ham):
+    lens = [i % 50 for i in range(330)]
+    lens[200] = 17000
+    test_attention_of_one_token(ham, BF16, 4, 2, 128, 32, lens)
 
 
 @pytest.mark.parametrize("dtype,H,Hk,hd,P,lens", [(BF16, 32, 8, 128, 32, [33, 700, 5000]), (BF16, 16, 1, 64, 16, [200, 3000]),
@@ -278,6 +291,13 @@ def test_prompts(ham, dtype, H, Hk, hd, P, rows):
     near(values(out, H, hd, dtype)[i], want[i], dtype)
     assert err == [0] * len(rows)
     assert torch.all(out[:offsets[0]] == 7) and torch.all(out[offsets[-1]:] == 7)   # packed rows of no sequence
+
+
+@pytest.mark.parametrize("dtype,H,Hk,rows", [
+    (BF16, 4, 1, [(i % 20, 9 + i % 4) for i in range(2100)]), (BF16, 2, 2, [(0, 0)] * 1030 + [(50, 3), (0, 17)] * 10), (F32, 3, 1, [(7, i % 3) for i in range(1100)]),
+    (BF16, 16, 1, [(0, 0)] * 4000 + [(5000, 3), (100, 1)] * 3)])
+def test_prompts_of_hundreds_of_rows(ham, dtype, H, Hk, rows):
+    test_prompts(ham, dtype, H, Hk, 64, 16, rows)
 
 
 @pytest.mark.parametrize("dtype,H,Hk,hd,P,rows", [(BF16, 32, 8, 128, 32, [(0, 200), (300, 40)]), (BF16, 8, 2, 64, 16, [(2000, 9)]),

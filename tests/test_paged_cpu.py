@@ -189,10 +189,13 @@ def rules():
                     'int shares(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).shares; }\n'
                     'int prompt_splits(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).splits; }\n'
                     'int as_tiles(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_tiles(N, R, Hk, grp, kv_max); }\n'
+                    'long long append_steps(long long N, long long R) { return ham::paged_append_steps(N, R); }\n'
+                    'int append_groups(int N, int R, int heads) { return ham::paged_append_groups(N, R, heads); }\n'
                     'long long tiles(long long N, long long R, long long grp, long long width) { return ham::paged_tiles(N, R, grp, width); }\n}\n')
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc, src, "-o", out], check=True)
         r = ctypes.CDLL(out)
         r.tiles.argtypes, r.tiles.restype = [ctypes.c_longlong] * 4, ctypes.c_longlong
+        r.append_steps.argtypes, r.append_steps.restype = [ctypes.c_longlong] * 2, ctypes.c_longlong
         r.tile_splits.argtypes = [ctypes.c_longlong] + [ctypes.c_int] * 3
         yield r
 
@@ -256,6 +259,20 @@ def test_tiles_do_for_every_cut_of_the_tokens(rules):
         counts = [g.choice((0, 1, 2, g.randint(0, 200))) for _ in range(g.randint(1, 12))]
         need = sum(-(-c * grp // width) for c in counts)
         assert need <= rules.tiles(max(1, sum(counts)), len(counts), grp, width)
+
+
+def test_appends_of_many_rows_have_workgroups_for_every_step(rules):
+    g = random.Random(4)
+    for _ in range(5000):
+        rows = [(g.randint(0, 99), g.choice((0, 1, g.randint(0, 200)))) for _ in range(g.randint(1, 200))]
+        N = max(1, sum(c for _, c in rows))
+        need = sum((s + c - 1) // 32 - s // 32 + 1 for s, c in rows if c)
+        assert need <= rules.append_steps(N, len(rows))
+    for R in (1, 64, 65, 300, 4096):
+        for N in (1, 64, 65, 1000, 5000, 1 << 24):
+            for heads in (1, 2, 16, 2048):
+                n = rules.append_groups(N, R, heads)
+                assert 1 <= n <= heads and (R > 64 or n == heads)
 
 
 # ---------------------------------------------------------------- the reference
