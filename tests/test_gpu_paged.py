@@ -474,6 +474,18 @@ def test_many_rows_and_pages(ham):
     b.advance([0] * R, [1] * R)            # all rows share row 0's pages, then write: one keeps the page
 
 
+def test_pools_of_many_pages(ham):
+    g = random.Random(5)
+    R = 300
+    b = Books(ham, ham.paged_shape(BF16, R, 1, 1, 64, 16, 36000, 130), 1)
+    b.advance(None, [g.choice((0, 1700, 2000, 2033)) for _ in range(R)])
+    b.advance([g.choice((r, r, r, -1)) for r in range(R)], [g.choice((0, 1, 40, -300)) for _ in range(R)])   # holes all over, filled from the front
+    b.compact()
+    b.advance(None, [1] * R)
+    b.advance([-1] * 290 + list(range(290, R)), [0] * R)   # the pages of a few rows, far behind
+    b.compact()
+
+
 def test_rows_of_impossible_state_are_left(ham):
     s, pool, g = rows_of_pages(ham, BF16, 2, 1, 64, 16, [20, 30, 40, 0])
     b = Books(ham, s, 1, pool)
