@@ -75,7 +75,7 @@ struct PagedCopyArgs {               // pages of `copies` in each layer
 
 int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s);
 int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, long long tiles, Stream s);  // tiles: of packed rows, at most
-int launch_paged_prompt(int hd, const PagedAttnArgs& a, int key_shares, Stream s);  // bf16
+int launch_paged_prompt(int hd, const PagedAttnArgs& a, int key_shares, int waves, Stream s);  // bf16
 int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s);
 int launch_paged_compact(const PagedCompactArgs& a, const PagedCopyArgs& c, Stream s);
 

@@ -1,13 +1,18 @@
 // Causal attention of packed bf16 prompts over their pages (layout: kernels_paged.h).
 //
 // A row's c tokens times the grp q-heads of a kv head are c * grp query rows in the order of the tokens; 32 of them, whatever
-// the group, are one wave's operand.  A workgroup of eight waves has QR = 256 / KS of them, its waves' keys in KS shares; 64 slots
-// at a time land in LDS straight from the pages, in the order of the pool, which is that of the operands.  Both products are
+// the group, are one wave's operand.  A workgroup of NW waves has QR = 32 NW / KS of them, its waves' keys in KS shares; 8 NW slots
+// at a time (a stage) land in LDS straight from the pages, in the order of the pool, which is that of the operands.  Both products are
 // 32x32x16 matrix instructions with the query row in the lane index:
 //   S^T = K Q^T (A = K rows, B = Q rows)  and  O^T = V^T P^T (A = V^T rows, B = P rows),
 // so a lane (row l & 31, half l >> 5) holds scores, weights, softmax state and output columns of one row and only the other half
 // shares it.  The running maximum moves, and with it the outputs, only when a score exceeds it by more than 8 powers of two.
 // Masks, and values past the slots that a wave sees, are dealt with only in blocks that reach past the wave's first row.
+//
+// Bound by the matrix cores at the card's power limit: 2,048 tokens of 32 heads of 128 behind 30,720 slots 1,581 to 1,640 us, 1.3 PFLOP/s
+// of the products that are executed (K Q^T for two planes of the queries, P V for two of the weights), a library's 8,192^3 product
+// 1.4; 7 prompts of 500 to 4,001 tokens 706 to 740 us, 1.1 to 1.2 (three planes of the weights: softmax, and planes, on the vector
+// units are the rest).  With three planes and no softmax the first took 1,612 us, with softmax and no products 767, with both 1,922.
 #include <type_traits>
 
 #include "gemm_epilogue.h"
@@ -21,8 +26,8 @@ namespace {
 typedef float f16v __attribute__((ext_vector_type(16)));
 
 template <int HD> struct PP {
-  static constexpr int NW = 8, KB = 32, ST = 64, NS = 4;           // waves; slots of a block, of a stage; stages in the ring
-  static constexpr int RUN = 2 * HD, STAGE = 8 * RUN;              // 16-byte units of 16 slots of K or V; of a stage: 4 K, 4 V
+  static constexpr int KB = 32, NS = 4;                            // slots of a block; stages in the ring
+  static constexpr int RUN = 2 * HD;                               // 16-byte units of 16 slots of K or V: a stage is NW / 2 of each
   static constexpr int LPW = RUN / 64;                             // a wave's loads of a stage: one run
   static constexpr int NF = HD / 16, ND = HD / 32;
 };
@@ -218,18 +223,19 @@ __device__ __forceinline__ PromptShare prompt_share(const PagedAttnArgs& a, int 
                      __builtin_amdgcn_readlane(c, r), __builtin_amdgcn_readlane(len, r)};
 }
 
-template <int HD, int KS>
-__global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
+template <int HD, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_paged_prompt(PagedAttnArgs a) {
   using P = PP<HD>;
-  constexpr int NS = P::NS, LPW = P::LPW, QT = P::NW / KS, QR = 32 * QT;
-  __shared__ u4 lds[NS][P::STAGE];
+  constexpr int NS = P::NS, LPW = P::LPW, QT = NW / KS, QR = 32 * QT;
+  constexpr int SR = NW / 2, ST = 16 * SR;  // a stage: runs of K, slots
+  __shared__ u4 lds[NS][NW * P::RUN];
   const PagedSizes& z = a.z;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int job = (int)(blockIdx.x / (uint32_t)z.Hk), kvh = (int)(blockIdx.x % (uint32_t)z.Hk), split = blockIdx.y;
   if (blockIdx.x == 0 && split == 0)
-    for (int i = threadIdx.x; i < z.R; i += 512)
+    for (int i = threadIdx.x; i < z.R; i += 64 * NW)
       if (prompt_count(a, i) < 0) atomicOr(a.err + i, 8);
-  const PromptShare sh = prompt_share<QR, 512>(a, job, (int*)lds);
+  const PromptShare sh = prompt_share<QR, 64 * NW>(a, job, (int*)lds);
   if (sh.r < 0) return;
   const int r = sh.r, o0 = sh.offset, c = sh.count, held = sh.slots - c;
   const int qt = w % QT, ks = w / QT;
@@ -258,13 +264,13 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     }
   }
   const int* table = a.table + (size_t)r * z.row_pages;
-  const int ngrp = (wg_end + 15) / 16, nall = (wg_end + P::ST - 1) / P::ST;
+  const int ngrp = (wg_end + 15) / 16, nall = (wg_end + ST - 1) / ST;
   const int per = (nall + a.nsplit - 1) / a.nsplit, st0 = split * per, nst = min(nall, st0 + per);  // stages [st0, nst)
   const size_t run = (size_t)(HD * 2) << z.lgP, page = 2 * run * z.Hk;
   const char* mine0 = (const char*)a.pool + 2 * run * kvh + (w & 1 ? run : 0);
   // wave w loads 16 slots of K (w even) or V of a stage; groups past the end read the last one again, and are never used, so
   // that every wave has the same number of loads under way
-  const auto group = [&](int st) { return min(st * 4 + (w >> 1), ngrp - 1); };
+  const auto group = [&](int st) { return min(st * SR + (w >> 1), ngrp - 1); };
   const auto page_of = [&](int st) { return st0 < nst ? scalar_at(table, group(min(st, nst - 1)) * 16 >> z.lgP) : 0; };
   int id0 = page_of(st0), id1 = page_of(st0 + 1);
   const auto issue = [&](int u) {  // the loads of stage st0 + u, whose page id is there, and the id of the one after the next
@@ -273,7 +279,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
     id1 = page_of(st + 2);
     const BufRsrc src = buf_rsrc(mine0 + (size_t)id * page + (size_t)(slot & ((1 << z.lgP) - 1)) * (HD * 2), P::RUN * 16);
     const uint32_t at = lane_anew() * 16;
-    auto* dst = (__attribute__((address_space(3))) void*)(lds[u % NS] + ((w & 1) * 4 + (w >> 1)) * P::RUN);
+    auto* dst = (__attribute__((address_space(3))) void*)(lds[u % NS] + ((w & 1) * SR + (w >> 1)) * P::RUN);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 0, 0);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 1024, 0);
     if constexpr (LPW == 4) {
@@ -291,11 +297,11 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   const float sc = 1.44269504088896341f / sqrtf((float)HD);  // scores in powers of two
   // A wave's block j: the products of the weights of block j - 1 with its V and of K with the queries, then the softmax.  So the
   // place of stage u - 1 is free again, and is loaded with stage u + 3, only in stage u + 1: two stages are on their way.
-  constexpr int NBS = 2 / KS;                     // blocks of a wave in a stage
+  constexpr int NBS = SR / 2 / KS;                     // blocks of a wave in a stage
   const int cnt = max(nst - st0, 0);
   const auto keys_of = [&](int u, int b) { return lds[u % NS] + 2 * (KS == 2 ? ks : b) * P::RUN; };
-  const auto values_of = [&](int u, int b) { return keys_of(u, b) + 4 * P::RUN; };
-  const auto base_of = [&](int u, int b) { return (st0 + u) * P::ST + (KS == 2 ? ks : b) * P::KB; };
+  const auto values_of = [&](int u, int b) { return keys_of(u, b) + SR * P::RUN; };
+  const auto base_of = [&](int u, int b) { return (st0 + u) * ST + (KS == 2 ? ks : b) * P::KB; };
   const auto landed = [&](int u) {                // stage u, of which all waves' loads have arrived after this
     if (u + 1 < cnt) wait_vm_lgkm0<LPW>();
     else wait_vm_lgkm0<0>();
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
   f16v s;
   u4 pp[2][3], vf[VFIRST];
   // stages whose slots every row of the wave sees, then the others (each wave by itself: the barriers are one a stage in both)
-  const int full = max(0, min(cnt, wave_least / P::ST - st0));
+  const int full = max(0, min(cnt, wave_least / ST - st0));
   const auto full_stages = [&](auto planes) {
     constexpr int NP = decltype(planes)::value;
     for (int j = 0; j < full * NBS; ++j) {
@@ -355,8 +361,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_prompt(PagedAttnArgs a) {
 #pragma unroll 1
     for (int st = st0 + full; st < nst; ++st)
 #pragma unroll 1
-      for (int b = 0; b < 4; ++b) {
-        const int base = st * P::ST + b * 16;
+      for (int b = 0; b < SR; ++b) {
+        const int base = st * ST + b * 16;
         if (base / P::KB * P::KB + P::KB <= wave_least || base >= wave_end || (KS == 2 && b / 2 != ks)) continue;
         const int id = checked_page(scalar_at(table, base >> z.lgP), z, a.err + r);
         const char* v = (const char*)a.pool + (size_t)id * page + 2 * run * kvh + run + (size_t)(base & ((1 << z.lgP) - 1)) * (HD * 2);
@@ -441,19 +447,19 @@ __global__ __launch_bounds__(256) void k_paged_prompt_join(PagedAttnArgs a) {
   for (int k = 0; k < V; ++k) Act<bf16>::put(a.out, (size_t)o + i / z.grp, z.H * HD, (kvh * z.grp + i % z.grp) * HD + lane * V + k, v[k]);
 }
 
-template <int HD, int KS>
+template <int HD, int KS, int NW>
 void prompt_t(const PagedAttnArgs& a, Stream s) {
-  constexpr int QR = 256 / KS;
+  constexpr int QR = 32 * NW / KS;
   const unsigned x = (unsigned)(paged_tiles(a.N, a.z.R, a.z.grp, QR) * a.z.Hk);
-  launch_k((k_paged_prompt<HD, KS>), dim3(x, a.nsplit), dim3(512), 0, s, a);
+  launch_k((k_paged_prompt<HD, KS, NW>), dim3(x, a.nsplit), dim3(64 * NW), 0, s, a);
   if (a.nsplit > 1) launch_k((k_paged_prompt_join<HD, QR>), dim3(x, QR / 4), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
-int launch_paged_prompt(int hd, const PagedAttnArgs& a, int ks, Stream s) {
-  if (hd == 64) ks == 2 ? prompt_t<64, 2>(a, s) : prompt_t<64, 1>(a, s);
-  else if (hd == 128) ks == 2 ? prompt_t<128, 2>(a, s) : prompt_t<128, 1>(a, s);
+int launch_paged_prompt(int hd, const PagedAttnArgs& a, int ks, int nw, Stream s) {
+  if (hd == 64) ks == 2 ? prompt_t<64, 2, 8>(a, s) : nw == 8 ? prompt_t<64, 1, 8>(a, s) : prompt_t<64, 1, 4>(a, s);
+  else if (hd == 128) ks == 2 ? prompt_t<128, 2, 8>(a, s) : nw == 8 ? prompt_t<128, 1, 8>(a, s) : prompt_t<128, 1, 4>(a, s);
   else return -1;
   return 0;
 }

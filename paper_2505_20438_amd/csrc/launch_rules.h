@@ -167,18 +167,28 @@ inline int paged_tile_splits(long long tiles, int Hk, int kv_max, int block) {
   const long long most = std::max<long long>(1, std::min<long long>({(blocks + 7) / 8, 1024 / pairs, 64}));
   return (int)std::min<long long>(most, std::max<long long>(1, 512 / pairs));
 }
-// k_paged_prompt: shares of the keys among a workgroup's waves (2: twice the workgroups, half the rows each) and splits of them
-// over workgroups.  One row, us, 1 share / 2: 1,500 tokens from the first 84 / 60, 2,048 114 / 93, and behind 8,000 slots 594 / 595 and
-// 30,720 1,594 / 1,662; 32 rows of up to 77 tokens (376 workgroups) 23 / 31.  Splits (2 shares): 512 tokens behind 8,000 slots 241
-// unsplit, 156 in two, 163 in four; 128 227, 52 in eight, 64 in 16; 64 behind 33,000 730, 76 in 16, 91 in 32.
+// k_paged_prompt: shares of the keys among a workgroup's waves (2: twice the workgroups, half the rows each), splits of them over
+// workgroups, waves of a workgroup: 8, or (1 share) 4, of which two are on a CU and begin and end at times of their own, but load the
+// keys twice.  Splits (2 shares), us: 512 tokens behind 8,000 slots 241 unsplit, 156 in two, 163 in four; 128 227, 52 in eight, 64 in
+// 16; 64 behind 33,000 730, 76 in 16, 91 in 32.  2 shares / 1 of 4 waves, up to one round of workgroups of 256 rows: 1,500 tokens from the
+// first 68 / 78, 2,048 100 / 104, 2 x 700 47 / 48, 1,000 behind 4,000 slots 180 / 207; but 4 x 400 49 / 42, 5 x 300 45 / 37, 1,500 behind
+// 4,000 300 / 270, 6 x 250 276 / 247.  8 waves / 4, `rounds` of the 8's: 2,048 behind 30,720 (1) 1,632 / 1,716, 1,500 behind 16,000 (0.7)
+// 805 / 850, 32 x 60 (0.9) 34 / 31; from the first 2,500 (1.2) 161 / 141, 3,000 (1.5) 190 / 178, 3,500 (1.7) 229 / 239, 4,000 (2) 302 / 309,
+// 5,000 (2.4) 452 / 428, 6,000 (2.9) 621 / 597, 16,000 (7.8) 3,939 / 3,959, 16 x 1,000 (7.8) 417 / 400, 8 x 600 (2.3) 105 / 94; 4,000 of head
+// dim 64 (2) 179 / 167.
 struct PagedPromptGrid {
   int shares, splits;
 };
 inline PagedPromptGrid paged_prompt_grid(int N, int R, int Hk, int grp, int kv_max) {
   const long long wide = paged_tiles(N, R, grp, 256) * Hk, narrow = paged_tiles(N, R, grp, 128) * Hk;
-  if (wide > 256 || (wide > 128 && kv_max > 8192)) return PagedPromptGrid{1, 1};
+  const bool alike = N < kv_max / 2 || N / 2 > kv_max;  // most slots are held already, or several rows: no long rows to pair with short
+  if (wide > 256 || (wide > 128 && (kv_max > 8192 || alike))) return PagedPromptGrid{1, 1};
   const long long stages = (kv_max + 63) / 64;
   return PagedPromptGrid{2, (int)std::max<long long>(1, std::min<long long>({256 / narrow, stages / 4, 32}))};
+}
+inline int paged_prompt_waves(int N, int Hk, int grp, int hd, int kv_max) {  // of 1 share
+  const double rounds = (double)N * grp * Hk / (256 * 256);
+  return (rounds <= 1 && kv_max > 8192) || (hd == 128 && rounds > 1.5 && rounds <= 2) ? 8 : 4;
 }
 
 }  // namespace ham

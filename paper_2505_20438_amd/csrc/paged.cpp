@@ -144,7 +144,8 @@ int ham_op_paged_prompt(const ham_paged_shape* p, int32_t n_tokens, const void* 
   }
   const PagedPromptGrid g = paged_prompt_grid(n_tokens, p->rows, p->n_kv_heads, grp, kv_max);
   a.nsplit = g.splits;
-  return launched(launch_paged_prompt(p->head_dim, a, g.shares, (hipStream_t)hip_stream));
+  return launched(launch_paged_prompt(p->head_dim, a, g.shares, paged_prompt_waves(n_tokens, p->n_kv_heads, grp, p->head_dim, kv_max),
+                                      (hipStream_t)hip_stream));
 }
 
 int ham_op_paged_advance(const ham_paged_shape* p, int32_t n_layers, const int32_t* d_parent, const int32_t* d_count,

@@ -293,6 +293,15 @@ def test_prompts(ham, dtype, H, Hk, hd, P, rows):
     assert torch.all(out[:offsets[0]] == 7) and torch.all(out[offsets[-1]:] == 7)   # packed rows of no sequence
 
 
+# the long prompts' kernel with workgroups of 8 waves: one round of them behind many slots, two rounds; of 4: many, several rows
+@pytest.mark.parametrize("H,Hk,hd,P,rows", [
+    (16, 8, 64, 64, [(8000, 2100), (0, 900)]), (16, 8, 128, 16, [(8100, 2100), (33, 1)]), (8, 1, 128, 32, [(9000, 4100)]), (16, 8, 128, 256, [(0, 7000)]),
+    (9, 3, 128, 16, [(0, 7300)]), (32, 8, 64, 16, [(5, 400), (0, 420), (0, 0), (70, 380), (31, 411)]), (7, 7, 128, 128, [(0, 8200)]),
+    (16, 8, 128, 32, [(2100, 3000)])])
+def test_prompts_of_either_number_of_waves(ham, H, Hk, hd, P, rows):
+    test_prompts(ham, BF16, H, Hk, hd, P, rows)
+
+
 @pytest.mark.parametrize("dtype,H,Hk,rows", [
     (BF16, 4, 1, [(i % 20, 9 + i % 4) for i in range(2100)]), (BF16, 2, 2, [(0, 0)] * 1030 + [(50, 3), (0, 17)] * 10), (F32, 3, 1, [(7, i % 3) for i in range(1100)]),
     (BF16, 16, 1, [(0, 0)] * 4000 + [(5000, 3), (100, 1)] * 3)])

@@ -188,6 +188,7 @@ def rules():
                     'int tile_splits(long long tiles, int Hk, int kv_max, int block) { return ham::paged_tile_splits(tiles, Hk, kv_max, block); }\n'
                     'int shares(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).shares; }\n'
                     'int prompt_splits(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_grid(N, R, Hk, grp, kv_max).splits; }\n'
+                    'int waves(int N, int Hk, int grp, int hd, int kv_max) { return ham::paged_prompt_waves(N, Hk, grp, hd, kv_max); }\n'
                     'int as_tiles(int N, int R, int Hk, int grp, int kv_max) { return ham::paged_prompt_tiles(N, R, Hk, grp, kv_max); }\n'
                     'long long append_steps(long long N, long long R) { return ham::paged_append_steps(N, R); }\n'
                     'int append_groups(int N, int R, int heads) { return ham::paged_append_groups(N, R, heads); }\n'
@@ -250,6 +251,13 @@ def test_prompt_splits_have_work_and_their_records_fit(rules):
 def test_kernels_of_packed_rows(rules, N, R, Hk, grp, kv, tiles, shares, splits):
     assert rules.as_tiles(N, R, Hk, grp, kv) == tiles
     assert rules.shares(N, R, Hk, grp, kv) == shares and rules.prompt_splits(N, R, Hk, grp, kv) == splits
+
+
+@pytest.mark.parametrize("N,R,Hk,grp,kv,hd,shares,waves", [
+    (2048, 1, 8, 4, 32768, 128, 1, 8), (1500, 1, 8, 4, 17500, 64, 1, 8), (2500, 1, 8, 4, 2500, 128, 1, 4), (4000, 1, 8, 4, 4000, 128, 1, 8),
+    (4000, 1, 8, 4, 4000, 64, 1, 4), (1600, 4, 8, 4, 400, 128, 1, 4), (1500, 1, 8, 4, 5500, 128, 1, 4), (1500, 6, 8, 4, 4250, 64, 1, 4), (12452, 7, 8, 4, 4001, 128, 1, 4)])
+def test_waves_of_long_prompts(rules, N, R, Hk, grp, kv, hd, shares, waves):
+    assert rules.shares(N, R, Hk, grp, kv) == shares and rules.waves(N, Hk, grp, hd, kv) == waves
 
 
 def test_tiles_do_for_every_cut_of_the_tokens(rules):
