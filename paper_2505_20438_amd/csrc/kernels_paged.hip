@@ -520,10 +520,13 @@ __device__ __forceinline__ bool fits(long long slots, const PagedSizes& z) { ret
 __device__ __forceinline__ bool in_pool(int id, const PagedSizes& z) { return (unsigned)id < (unsigned)z.n_pages; }
 
 // With `parent`: a row takes over the entries of another as they were, -1 for what it had beyond them; pages count the rows
-// that hold them.  The tables are written back at the end (k_paged_copy), when every row has been read.  A workgroup a row.
-__global__ __launch_bounds__(256) void k_paged_take(PagedAdvanceArgs a) {
+// that hold them.  The tables are written back at the end (k_paged_copy), when every row has been read.
+struct Taken {
+  int from, now, old;  // the row whose entries are taken over (or -1), their number, that of the row's own
+};
+__device__ __forceinline__ Taken take_length(const PagedAdvanceArgs& a, int r, bool first) {  // `first`: the thread that reports
   const PagedSizes& z = a.z;
-  const int r = blockIdx.x, tid = threadIdx.x, had = a.kv_len[r];
+  const int had = a.kv_len[r];
   int from = a.parent[r], len = 0, old = 0;
   bool bad = false;
   if (!fits(had, z)) {            // nothing is known of the row's pages: it stays as it is
@@ -543,28 +546,32 @@ __global__ __launch_bounds__(256) void k_paged_take(PagedAdvanceArgs a) {
     }
   }
   const int now = fits(len, z) ? pages_of(len, z.lgP) : 0;
-  if (tid == 0) {
+  if (first) {
     if (bad) atomicOr(a.err + r, 8);
     a.taken_len[r] = len;
     a.span[r] = max(old, now);
   }
-  const int* mine = a.table + (size_t)r * z.row_pages;
-  const int* theirs = a.table + (size_t)max(from, 0) * z.row_pages;
-  int* out = a.taken + (size_t)r * z.row_pages;
-  for (int e = tid; e < max(old, now); e += 256) {
-    const int id = e < now ? theirs[e] : -1;
-    out[e] = id;
-    if (from == r) continue;
-    if (e < old) {
-      const int was = mine[e];
-      if (in_pool(was, z)) atomicSub(a.refs + was, 1);
-      else atomicOr(a.err + r, 32);
-    }
-    if (e < now) {
-      if (in_pool(id, z)) atomicAdd(a.refs + id, 1);
-      else atomicOr(a.err + r, 32);
-    }
+  return Taken{from, now, old};
+}
+__device__ __forceinline__ void take_entry(const PagedAdvanceArgs& a, int r, const Taken& t, int e) {  // e < max(old, now)
+  const PagedSizes& z = a.z;
+  const int id = e < t.now ? a.table[(size_t)max(t.from, 0) * z.row_pages + e] : -1;
+  a.taken[(size_t)r * z.row_pages + e] = id;
+  if (t.from == r) return;
+  if (e < t.old) {
+    const int was = a.table[(size_t)r * z.row_pages + e];
+    if (in_pool(was, z)) atomicSub(a.refs + was, 1);
+    else atomicOr(a.err + r, 32);
   }
+  if (e < t.now) {
+    if (in_pool(id, z)) atomicAdd(a.refs + id, 1);
+    else atomicOr(a.err + r, 32);
+  }
+}
+__global__ __launch_bounds__(256) void k_paged_take(PagedAdvanceArgs a) {  // a workgroup a row
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const Taken t = take_length(a, r, tid == 0);
+  for (int e = tid; e < max(t.old, t.now); e += 256) take_entry(a, r, t, e);
 }
 
 constexpr int GIVE_THREADS = 1024;
@@ -635,7 +642,9 @@ __device__ __forceinline__ int lanes_before(uint64_t mask) {  // of the mask's
 // a copy, except, where all holders write to it in this call, the lowest of them.  Bound by latency: lengths, the rows' last
 // entries, their references, and the writes, one round trip to memory each, and the scans between them.
 constexpr int GIVE_PAGES = 2048;            // of the pages to give out, in LDS; those behind them in the workspace
-template <int CHUNKS>
+// TAKE: up to TAKE_ENTRIES table entries are taken over here, a launch less (32 rows of beams, 16 layers, 20 us for 22).
+constexpr int TAKE_ENTRIES = 4 * GIVE_THREADS;
+template <int CHUNKS, bool TAKE>
 __global__ __launch_bounds__(GIVE_THREADS) void k_paged_give(PagedAdvanceArgs a) {
   __shared__ int ends[PAGED_MAX_ROWS];      // pages wanted by the rows up to this one
   __shared__ unsigned char copied[PAGED_MAX_ROWS];
@@ -646,6 +655,18 @@ __global__ __launch_bounds__(GIVE_THREADS) void k_paged_give(PagedAdvanceArgs a)
   constexpr int PER = PAGED_MAX_ROWS / GIVE_THREADS;  // rows of a thread: tid, tid + GIVE_THREADS, ..
   int* table = a.parent ? a.taken : a.table;
   const int* lengths = a.parent ? a.taken_len : a.kv_len;
+  if constexpr (TAKE) {
+    __shared__ Taken taken[GIVE_THREADS];
+    if (tid < z.R) taken[tid] = take_length(a, tid, true);
+    __syncthreads();
+    const int entries = z.R * z.row_pages;
+#pragma unroll
+    for (int i = 0; i < TAKE_ENTRIES / GIVE_THREADS; ++i) {
+      const int at = tid + i * GIVE_THREADS, r = at / z.row_pages, e = at - r * z.row_pages;
+      if (at < entries && e < max(taken[r].old, taken[r].now)) take_entry(a, r, taken[r], e);
+    }
+    __syncthreads();
+  }
   // references of the first pages, for the search for free ones
   const auto load_refs = [&](int p0, int* refs) {
     page_refs<CHUNKS, true>(a.refs, p0, z.n_pages, 1, refs);
@@ -930,8 +951,10 @@ int launch_paged_append(int dtype, int hd, const PagedAppendArgs& a, Stream s) {
 int launch_paged_attention(int dtype, int hd, const PagedAttnArgs& a, long long tiles, Stream s) { PAGED_DISPATCH(attention_t, a, tiles, s); }
 
 int launch_paged_advance(const PagedAdvanceArgs& a, const PagedCopyArgs& c, Stream s) {
-  if (a.parent) launch_k(k_paged_take, dim3(a.z.R), dim3(256), 0, s, a);
-  launch_k(a.z.n_pages > FEW_PAGES ? k_paged_give<16> : k_paged_give<4>, dim3(1), dim3(GIVE_THREADS), 0, s, a);
+  const bool many = a.z.n_pages > FEW_PAGES, take = a.parent && a.z.R <= GIVE_THREADS && (long long)a.z.R * a.z.row_pages <= TAKE_ENTRIES;
+  if (a.parent && !take) launch_k(k_paged_take, dim3(a.z.R), dim3(256), 0, s, a);
+  launch_k(many ? take ? k_paged_give<16, true> : k_paged_give<16, false> : take ? k_paged_give<4, true> : k_paged_give<4, false>, dim3(1),
+           dim3(GIVE_THREADS), 0, s, a);
   const PagedTables t{a.z, a.table, a.taken, a.parent ? a.span : nullptr, nullptr, nullptr, nullptr};
   launch_k(k_paged_copy, dim3(1024), dim3(COPY_THREADS), 0, s, c, t);
   return 0;

@@ -495,6 +495,16 @@ def test_pools_of_many_pages(ham):
     b.compact()
 
 
+@pytest.mark.parametrize("rows,row_pages,n_pages", [(4, 1000, 5000), (1000, 4, 3500), (1, 4096, 4100), (5, 819, 4000), (5, 820, 4000)])
+def test_rows_that_share_pages_of_tables_of_either_size(ham, rows, row_pages, n_pages):
+    g = random.Random(rows)
+    b = Books(ham, ham.paged_shape(F32, rows, 1, 1, 64, 16, n_pages, row_pages), 1)
+    cap = row_pages * 16
+    b.advance(None, [g.randrange(cap // 2) for _ in range(rows)])
+    for _ in range(4):
+        b.advance([g.choice((r, g.randrange(rows), g.randrange(rows), -1)) for r in range(rows)], [g.choice((0, 1, 17, -5, cap // 3)) for _ in range(rows)])
+
+
 def test_rows_of_impossible_state_are_left(ham):
     s, pool, g = rows_of_pages(ham, BF16, 2, 1, 64, 16, [20, 30, 40, 0])
     b = Books(ham, s, 1, pool)
