@@ -129,16 +129,20 @@ inline long long paged_tiles(long long N, long long R, long long grp, long long 
 // Attention of one token over pages (kernels_paged.hip): whether its slots are split over workgroups, which a second launch then
 // joins, for R rows of which the longest has kv_max slots, in blocks of 16 KB (head dim 128) of K and V.  A workgroup of four
 // waves takes about 5 us and 0.6 us for each four blocks, a join 3 to 5.  Split / not, us: 1 row of 2,000 slots of 8 heads of 128
-// 9.7 / 14.8, 8 x 1,000 10.8 / 10.4, 8 x 500 9.5 / 6.9, 1 x 700 of 64 8.1 / 6.4.  From 96 workgroups on memory is busy without
-// splits while all rows are long (32 x 2,560 51 / 50, 64 x 1,000 of 8 heads 42 / 43), and up to 128 blocks a long row among short
-// ones is no longer than 25 us.  With hundreds of rows, finding a share's row costs every workgroup more and short rows hide a longer
-// one: 512 rows of 300 slots and one of 8,000 183 / 153, one of 33,000 193 / 365; 512 of 5,000 1,615 / 1,570.  The records of a
-// split launch have room for PAGED_SPLIT_MAX_HEADS (row, q-head) pairs.
+// 9.7 / 14.8, 8 x 1,000 10.8 / 10.4, 8 x 500 9.5 / 6.9, 1 x 700 of 64 8.1 / 6.4.  With more workgroups memory is busy without
+// splits while all rows are long, and they pay for rows of different lengths: (row, kv head) pairs of 80 blocks each / of 80 down
+// to 20: bf16 96 27.7 / 29.7 and 19.5 / 28.4, 128 35.2 / 34.6 and 23.2 / 29.2, 160 46.0 / 38.1 and 28.1 / 30.4; of 48 blocks 128
+// 25.1 / 22.7 and 17.3 / 19.1; fp32 of head dim 64, of 80 blocks, 160 44.4 / 45.7 and 28.6 / 40.3, 192 52.3 / 47.0 and 32.5 /
+// 40.2. Past 128 blocks a long row among short ones would hold its workgroup for more than 25 us.  With hundreds of rows, finding
+// a share's row costs every workgroup more and short rows hide a longer one: 512 rows of 300 slots and one of 8,000 183 / 153, one
+// of 33,000 193 / 365; 512 of 5,000 1,615 / 1,570.  The records of a split launch have room for PAGED_SPLIT_MAX_HEADS (row,
+// q-head) pairs.
 constexpr int PAGED_SPLIT_MAX_HEADS = 16384;
 inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block) {
   const int blocks = (kv_max + block - 1) / block * hd / 128, pairs = R * Hk;
   if (R * H > PAGED_SPLIT_MAX_HEADS) return false;
-  return blocks > 28 && (pairs < 96 || blocks > (R > 256 ? 512 : 128));
+  const int few = block == 16 ? 160 : blocks > 60 ? 128 : 95;  // blocks of 16 slots: fp32
+  return blocks > 28 && (pairs <= few || blocks > (R > 256 ? 512 : 128));
 }
 // Shares that the slots of all rows are cut into, for each kv head: workgroups for one, or with more rows up to four, whole rounds
 // over the CUs (at 8 kv heads a round is 32; 4 x 33,300 slots, us, 24 shares 78, 32 77, 40 93, 48 85, 64 77, 72 89; 16 x 8,300
