@@ -352,6 +352,11 @@ def test_what_is_not_finite_reaches_the_tokens_that_see_it_and_no_other(ham, dty
             assert torch.isnan(a[seen][:, group]).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), -INF])
+def test_what_is_not_finite_in_workgroups_of_eight_waves(ham, bad):
+    test_what_is_not_finite_reaches_the_tokens_that_see_it_and_no_other(ham, BF16, 16, 8, 128, [(0, 7000)], bad)
+
+
 @pytest.mark.parametrize("dtype,H,rows", [(BF16, 4, [(10, 20), (0, 30), (5, 5), (40, 9)]), (F32, 4, [(10, 20), (0, 30), (5, 5), (40, 9)]),
                                           (BF16, 32, [(10, 1000), (0, 30), (5, 5), (1040, 9)])])
 def test_prompt_rows_that_do_not_fit_are_left(ham, dtype, H, rows):
