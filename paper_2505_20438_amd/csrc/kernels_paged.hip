@@ -188,9 +188,9 @@ __device__ __forceinline__ int slots_of(const PagedAttnArgs& a, int r, bool repo
   return a.enable[r] ? n : 0;
 }
 // One row per sequence, split: the blocks of all rows in about a.nsplit shares of the same size, so that a long row among short
-// ones has many workgroups.  Of row r, of `blocks`, they are shares `first` .. `first` + `of` - 1, `size` blocks each.
+// ones has many workgroups.  Of row r they are shares `first` .. `first` + `of` - 1, `size` blocks each.
 struct RowShare {
-  int r, size, blocks, first, of;
+  int r, size, first, of;
 };
 template <typename Pick>
 __device__ __forceinline__ RowShare row_share(const PagedAttnArgs& a, int block, const Pick& pick) {
@@ -212,11 +212,11 @@ __device__ __forceinline__ RowShare row_share(const PagedAttnArgs& a, int block,
     const uint64_t hit = __ballot(r < R && pick(r, end - of, end));
     if (hit) {
       const int l = __builtin_ctzll(hit), first = __builtin_amdgcn_readlane(end - of, l);
-      return RowShare{r0 + l, size, __builtin_amdgcn_readlane(n, l), first, __builtin_amdgcn_readlane(of, l)};
+      return RowShare{r0 + l, size, first, __builtin_amdgcn_readlane(of, l)};
     }
     before = __builtin_amdgcn_readlane(end, 63);
   }
-  return RowShare{-1, 0, 0, 0, 0};
+  return RowShare{-1, 0, 0, 0};
 }
 
 // Tiles of a packed row, where they are this kernel's.

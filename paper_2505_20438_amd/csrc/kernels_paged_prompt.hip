@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_prompt(PagedAttnArgs a) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 1024, 0);
     if constexpr (LPW == 4) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 2048, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 3072, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, dst, 16, at, 0, 3 * 1024, 0);
     }
   };
 
