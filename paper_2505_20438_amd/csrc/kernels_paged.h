@@ -6,7 +6,6 @@
 namespace ham {
 
 constexpr int PAGED_MAX_GROUP = 16;   // q-heads of a kv head: the columns of a 16-wide matrix product
-constexpr int PAGED_MAX_SPLIT = 64;   // splits of a row's slots (the join holds one a lane)
 constexpr int PAGED_MAX_RECORDS = 1 << 15;  // query rows times splits of a split launch (launch_rules.h keeps below it)
 
 // A layer's pool is [n_pages][n_kv_heads][2: K, V][P * hd] values of the storage type.  With E = 16 bytes of values:

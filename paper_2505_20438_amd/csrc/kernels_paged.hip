@@ -196,14 +196,14 @@ template <typename Pick>
 __device__ __forceinline__ RowShare row_share(const PagedAttnArgs& a, int block, const Pick& pick) {
   const int R = a.z.R, lane = threadIdx.x & 63;
   const auto blocks = [&](int r) { return r < R ? (slots_of(a, r, false) + block - 1) / block : 0; };
-  int all = 0, most = 0, n = 0;
+  long long all = 0;
+  int most = 0, n = 0;
   for (int r0 = 0; r0 < R; r0 += 64) {
     n = blocks(r0 + lane);
     all += __builtin_amdgcn_readlane(wave_scan(n), 63);
     most = max(most, (int)group_max(row_max((float)n)));  // below 2^24: exact
   }
-  const int whole = a.nsplit - min(R, a.nsplit / 2);  // the rows' ends are shares too
-  const int size = max(max((all + whole - 1) / whole, PAGED_LEAST_BLOCKS), (most + PAGED_MAX_SPLIT - 1) / PAGED_MAX_SPLIT);
+  const int size = paged_share_size(all, most, R, a.nsplit);
   int before = 0;
   for (int r0 = 0; r0 < R; r0 += 64) {
     const int r = r0 + lane;

@@ -150,6 +150,16 @@ inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block
 // of the four waves.
 constexpr int PAGED_LEAST_BLOCKS = 8;
 inline int paged_attn_shares(int R, int Hk) { return std::max(1, 256 * std::min(4, 1 + R * Hk / 128) / Hk); }
+// Blocks of a share, where R rows have `all` together and the longest `most`: R + shares workgroups do for all rows, and no row has
+// more than PAGED_MAX_SPLIT of them.  4,096 rows of 2^24 slots are 2^32 blocks of 16: the sum has 64 bits, the division 32, for which
+// 2^32 counts as one less (that gives no share more: with shares of ceil((2^32 - 1) / n) blocks, 2^32 hold n whole ones at most).
+constexpr int PAGED_MAX_SPLIT = 64;  // splits of a row's slots (the join holds one a lane)
+constexpr int paged_share_size(long long all, int most, int R, int shares) {
+  const unsigned whole = (unsigned)(shares - (R < shares / 2 ? R : shares / 2));  // the rows' ends are shares too
+  const unsigned n = all < 0xFFFFFFFFll ? (unsigned)all : 0xFFFFFFFFu;
+  const int size = (int)(n / whole + (n % whole != 0)), least = (most + PAGED_MAX_SPLIT - 1) / PAGED_MAX_SPLIT;
+  return size < least ? (least < PAGED_LEAST_BLOCKS ? PAGED_LEAST_BLOCKS : least) : size < PAGED_LEAST_BLOCKS ? PAGED_LEAST_BLOCKS : size;
+}
 
 // Packed rows, two kernels.  k_paged_attn takes (token, q-head) pairs 16 at a time, each tile's keys shared by four waves that
 // read them for themselves; k_paged_prompt (bf16) takes 256 or 128, whose keys go through LDS once.  The first fills the card with
