@@ -318,9 +318,7 @@ int ham_op_paged_attention(const ham_paged_shape* shape, const void* d_q, const 
  * already: row r's c tokens are the last c of its kv_len[r] slots, and token i of them
  * sees the slots up to its own, kv_len - c + i, those before the packed tokens
  * included.  An infinity or NaN in K or V reaches the tokens that see its slot and no
- * other (in K it may make them NaN).  Numbers as in ham_op_paged_attention, but that
- * weights are sums of two bf16 values (16 bits) in calls with more than about 1,000
- * tokens of 32 heads for the tokens that see 16,384 slots or more.
+ * other (in K it may make them NaN).  Numbers as in ham_op_paged_attention.
  *  d_q, d_out  act rows [n_tokens][n_heads*head_dim]
  *  kv_max      host upper bound of kv_len; with n_tokens, rows and heads it chooses
  *              the split of the work and so the order of the sums */

@@ -364,7 +364,7 @@ __global__ __launch_bounds__(64 * PATT_WAVES, HD == 64 ? 4 : 2) void k_paged_att
         l += p[e];
       }
       u4 pp[NP];
-      if constexpr (NP == 3) weight_planes<3>(p, pp);
+      if constexpr (NP == 3) weight_planes(p, pp);
       else
 #pragma unroll
         for (int e = 0; e < 4; ++e) pp[0][e] = __float_as_uint(p[e]);

@@ -9,12 +9,10 @@
 // shares it.  The running maximum moves, and with it the outputs, only when a score exceeds it by more than 8 powers of two.
 // Masks, and values past the slots that a wave sees, are dealt with only in blocks that reach past the wave's first row.
 //
-// Bound by the matrix cores at the card's power limit: 2,048 tokens of 32 heads of 128 behind 30,720 slots 1,581 to 1,640 us, 1.3 PFLOP/s
-// of the products that are executed (K Q^T for two planes of the queries, P V for two of the weights), a library's 8,192^3 product
-// 1.4; 7 prompts of 500 to 4,001 tokens 706 to 740 us, 1.1 to 1.2 (three planes of the weights: softmax, and planes, on the vector
-// units are the rest).  With three planes and no softmax the first took 1,612 us, with softmax and no products 767, with both 1,922.
-#include <type_traits>
-
+// Bound by the matrix cores at the card's power limit: 2,048 tokens of 32 heads of 128 behind 30,720 slots 1,890 to 1,915 us, 1.4 PFLOP/s
+// of the products that are executed (K Q^T for two planes of the queries, P V for three of the weights), as a library's 8,192^3
+// product; 7 prompts of 500 to 4,001 tokens 704 to 740 us, 1.1 to 1.2 (softmax, and planes, on the vector units are the rest).
+// Without softmax the first took 1,612 us, without products 767; two planes of the weights, 16 bits, 1,590.
 #include "gemm_epilogue.h"
 #include "launch_rules.h"
 #include "paged_device.h"
@@ -50,15 +48,9 @@ __device__ __forceinline__ f16v block_scores(const u4* kblk, const u4* qh, const
   return s;
 }
 
-// Weights enter the second product in three bf16 planes (weight_planes), all 24 bits of them, or in two.  The third costs a fifth
-// of the products, and with them, at the card's power limit, a fifth of the time.  It is left out where it shows least and costs
-// most: in launches that fill the card (KS = 1), for rows that see 16,384 slots or more.  A sum over n slots that stays in fp32
-// through n / 16 products is itself rounded by 2^-25 sqrt(n / 32) of the output, 0.7e-6 at 16,384 slots, beside 2e-6 of two planes.
-constexpr int PLANES_2_FROM = 16384;  // slots that the wave's first row sees
-
-// The softmax update of (m, l, o) by a block's scores, whose weights are left in NP bf16 planes.  `keep`: how many of the
-// block's slots the lane's row sees (32 or more: all); score e is slot 16 (e / 8) + 8 h + e % 8.
-template <int HD, int NP>
+// The softmax update of (m, l, o) by a block's scores, whose weights are left in three bf16 planes, all 24 bits of them.  `keep`:
+// how many of the block's slots the lane's row sees (32 or more: all); score e is slot 16 (e / 8) + 8 h + e % 8.
+template <int HD>
 __device__ __forceinline__ void block_weights(f16v s, bool masked, int keep, float sc, float& mrun, float& lrun, f16v* o, u4 (*pp)[3]) {
   using P = PP<HD>;
   const int h = (threadIdx.x & 63) >> 5;
@@ -89,8 +81,8 @@ __device__ __forceinline__ void block_weights(f16v s, bool masked, int keep, flo
 #pragma unroll
   for (int e = 0; e < 16; ++e) ps += p[e];
   lrun += ps;
-  weight_planes<NP>(p, pp[0]);
-  weight_planes<NP>(p + 8, pp[1]);
+  weight_planes(p, pp[0]);
+  weight_planes(p + 8, pp[1]);
 }
 
 // Outputs += weights of a block times its V, whose first operands `v` are there already (first_values).
@@ -105,7 +97,7 @@ __device__ __forceinline__ void first_values(const u4* vblk, u4* v) {
 #pragma unroll
   for (int i = 0; i < VFIRST; ++i) v[i] = vr[i % 2 * PP<HD>::RUN + i / 2 * 32];
 }
-template <int HD, int NP>
+template <int HD>
 __device__ __forceinline__ void block_values(const u4* vblk, const u4* v, const u4 (*pp)[3], f16v* o) {
   using P = PP<HD>;
   const u4* vr = lane_values<HD>(vblk);
@@ -115,11 +107,11 @@ __device__ __forceinline__ void block_values(const u4* vblk, const u4* v, const 
     for (int t = 0; t < 2; ++t) {
       const bf16x8 x = __builtin_bit_cast(bf16x8, 2 * d + t < VFIRST ? v[(2 * d + t) % VFIRST] : vr[t * P::RUN + d * 32]);
 #pragma unroll
-      for (int i = 0; i < NP; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
+      for (int i = 0; i < 3; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, pp[t][i]), o[d], 0, 0, 0);
     }
 }
 // The order of a phase's products and LDS reads: an operand is read four before its turn.
-template <int HD, int NP>
+template <int HD>
 __device__ __forceinline__ void order_products() {
   using P = PP<HD>;
   constexpr int NV = 2 * P::ND, NK = P::NF;
@@ -127,7 +119,7 @@ __device__ __forceinline__ void order_products() {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
-    __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);  // matrix products
+    __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);  // matrix products
   }
 #pragma unroll
   for (int i = 0; i < NK; ++i) {
@@ -315,28 +307,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_prompt(PagedAttnArgs a) {
   u4 pp[2][3], vf[VFIRST];
   // stages whose slots every row of the wave sees, then the others (each wave by itself: the barriers are one a stage in both)
   const int full = max(0, min(cnt, wave_least / ST - st0));
-  const auto full_stages = [&](auto planes) {
-    constexpr int NP = decltype(planes)::value;
-    for (int j = 0; j < full * NBS; ++j) {
-      const int u = j / NBS, b = j % NBS;
-      if (j > 0) {
-        block_values<HD, NP>(values_of((j - 1) / NBS, (j - 1) % NBS), vf, pp, o);
-        s = block_scores<HD>(keys_of(u, b), qh, ql);
-        order_products<HD, NP>();
-      } else {
-        s = block_scores<HD>(keys_of(u, b), qh, ql);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (b == 0 && u + 2 < cnt) issue(u + 2);  // with the products under way: before them they hold back their LDS reads
-      block_weights<HD, NP>(s, false, 0, sc, mrun, lrun, o, pp);
-      first_values<HD>(values_of(u, b), vf);
-      __builtin_amdgcn_sched_barrier(0);
-      if (b == NBS - 1) landed(u + 1);
+  for (int j = 0; j < full * NBS; ++j) {
+    const int u = j / NBS, b = j % NBS;
+    if (j > 0) {
+      block_values<HD>(values_of((j - 1) / NBS, (j - 1) % NBS), vf, pp, o);
+      s = block_scores<HD>(keys_of(u, b), qh, ql);
+      order_products<HD>();
+    } else {
+      s = block_scores<HD>(keys_of(u, b), qh, ql);
     }
-    if (full > 0) block_values<HD, NP>(values_of(full - 1, NBS - 1), vf, pp, o);
-  };
-  if (KS == 1 && wave_least >= PLANES_2_FROM) full_stages(std::integral_constant<int, 2>{});
-  else full_stages(std::integral_constant<int, 3>{});
+    __builtin_amdgcn_sched_barrier(0);
+    if (b == 0 && u + 2 < cnt) issue(u + 2);  // with the products under way: before them they hold back their LDS reads
+    block_weights<HD>(s, false, 0, sc, mrun, lrun, o, pp);
+    first_values<HD>(values_of(u, b), vf);
+    __builtin_amdgcn_sched_barrier(0);
+    if (b == NBS - 1) landed(u + 1);
+  }
+  if (full > 0) block_values<HD>(values_of(full - 1, NBS - 1), vf, pp, o);
   const int l = lane_anew(), limit = row_of(l).limit;
   int odd = 0;
   for (int u = full; u < cnt; ++u) {
@@ -347,12 +334,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_prompt(PagedAttnArgs a) {
       if (base >= wave_end) break;
       const bool masked = base + P::KB > wave_least;
       s = block_scores<HD>(keys_of(u, b), qh, ql);
-      block_weights<HD, 3>(s, masked, limit - base, sc, mrun, lrun, o, pp);
+      block_weights<HD>(s, masked, limit - base, sc, mrun, lrun, o, pp);
       if (masked) {
         odd |= block_values_masked<HD>(values_of(u, b), wave_end - base, pp, o);
       } else {
         first_values<HD>(values_of(u, b), vf);
-        block_values<HD, 3>(values_of(u, b), vf, pp, o);
+        block_values<HD>(values_of(u, b), vf, pp, o);
       }
     }
     landed(u + 1);

@@ -186,10 +186,10 @@ inline int paged_tile_splits(long long tiles, int Hk, int kv_max, int block) {
 // keys twice.  Splits (2 shares), us: 512 tokens behind 8,000 slots 241 unsplit, 156 in two, 163 in four; 128 227, 52 in eight, 64 in
 // 16; 64 behind 33,000 730, 76 in 16, 91 in 32.  2 shares / 1 of 4 waves, up to one round of workgroups of 256 rows: 1,500 tokens from the
 // first 68 / 78, 2,048 100 / 104, 2 x 700 47 / 48, 1,000 behind 4,000 slots 180 / 207; but 4 x 400 49 / 42, 5 x 300 45 / 37, 1,500 behind
-// 4,000 300 / 270, 6 x 250 276 / 247.  8 waves / 4, `rounds` of the 8's: 2,048 behind 30,720 (1) 1,632 / 1,716, 1,500 behind 16,000 (0.7)
-// 805 / 850, 32 x 60 (0.9) 34 / 31; from the first 2,500 (1.2) 161 / 141, 3,000 (1.5) 190 / 178, 3,500 (1.7) 229 / 239, 4,000 (2) 302 / 309,
-// 5,000 (2.4) 452 / 428, 6,000 (2.9) 621 / 597, 16,000 (7.8) 3,939 / 3,959, 16 x 1,000 (7.8) 417 / 400, 8 x 600 (2.3) 105 / 94; 4,000 of head
-// dim 64 (2) 179 / 167.
+// 4,000 300 / 270, 6 x 250 276 / 247.  8 waves / 4, `rounds` of the 8's: 2,048 behind 30,720 (1) 1,895 / 1,960, 1,500 behind 16,000 (0.7)
+// 835 / 900 (but of head dim 64 1,184 / 1,148 and 571 / 506), 32 x 60 (0.9) 34 / 31; from the first 2,500 (1.2) 161 / 141, 3,000 (1.5)
+// 190 / 178, 3,500 (1.7) 229 / 239, 4,000 (2) 302 / 309, 5,000 (2.4) 452 / 428, 6,000 (2.9) 621 / 597, 16,000 (7.8) 3,939 / 3,959,
+// 16 x 1,000 (7.8) 417 / 400, 8 x 600 (2.3) 105 / 94; 4,000 of head dim 64 (2) 179 / 167.
 struct PagedPromptGrid {
   int shares, splits;
 };

@@ -150,24 +150,18 @@ template <typename T> __device__ __forceinline__ void drop_nonfinite(u4& v) {
   }
 }
 
-// Eight fp32 values as bf16 planes.  Three: each is the 8 leading bits of what the ones before it leave, 24 bits in all.  Two: 16
-// bits, to the nearest.  (What a plane leaves of a value as a 2-term bf16 dot product, one instruction for two, is slower: 7
-// packed prompts 780 us for 731.)
-template <int NP>
+// Eight fp32 values as three bf16 planes, each the 8 leading bits of what the ones before it leave: 24 bits in all.  (What a plane
+// leaves of a value as a 2-term bf16 dot product, one instruction for two, is slower: 7 packed prompts 780 us for 731.)
 __device__ __forceinline__ void weight_planes(const float* p, u4* pp) {
-  if constexpr (NP == 2) {
-    to_planes<2>(p, pp);
-  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
+  for (int i = 0; i < 4; ++i) {
+    uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        pp[n][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);  // the upper halves
-        if (n == 2) break;
-        x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u));
-        y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xFFFF0000u));
-      }
+    for (int n = 0; n < 3; ++n) {
+      pp[n][i] = __builtin_amdgcn_perm(y, x, 0x07060302u);  // the upper halves
+      if (n == 2) break;
+      x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u));
+      y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xFFFF0000u));
     }
   }
 }
