@@ -306,7 +306,8 @@ int ham_op_paged_append(const ham_paged_shape* shape, int32_t n_tokens, const fl
  *   out[r, h] = softmax_j(q[r, h] . K[r, h/(H/Hkv), j] / sqrt(hd)) V[...], j < kv_len[r].
  * A row without slots (kv_len or enable 0), or whose scores are all -infinity, gets
  * zeros.  Softmax statistics and sums are fp32; bf16 weights are sums of three bf16
- * values (24 bits).  K is finite: an infinity in it may make the rows that see it NaN.
+ * values (24 bits).  An infinity in K or V may make the rows that see it NaN (in V, in its
+ * channel).
  *  d_q, d_out  act rows [rows][n_heads*head_dim]
  *  kv_max      host upper bound of kv_len; it chooses the split of the slots over
  *              workgroups and so the order of the sums */
@@ -318,7 +319,7 @@ int ham_op_paged_attention(const ham_paged_shape* shape, const void* d_q, const 
  * already: row r's c tokens are the last c of its kv_len[r] slots, and token i of them
  * sees the slots up to its own, kv_len - c + i, those before the packed tokens
  * included.  An infinity or NaN in K or V reaches the tokens that see its slot and no
- * other (in K it may make them NaN).  Numbers as in ham_op_paged_attention.
+ * other; an infinity may make them NaN.  Numbers as in ham_op_paged_attention.
  *  d_q, d_out  act rows [n_tokens][n_heads*head_dim]
  *  kv_max      host upper bound of kv_len; with n_tokens, rows and heads it chooses
  *              the split of the work and so the order of the sums */
