@@ -279,7 +279,7 @@ typedef struct ham_paged_shape {
   int32_t head_dim;   /* 64 or 128 */
   int32_t page_slots; /* 16, 32, 64, 128 or 256 */
   int32_t n_pages;    /* of the pool, 1..2^22 */
-  int32_t row_pages;  /* table entries of a row; row_pages * page_slots <= 2^24 */
+  int32_t row_pages;  /* table entries of a row; row_pages * page_slots <= 2^24, rows * row_pages <= 2^28 */
 } ham_paged_shape;
 
 /* Bytes of a layer's pool, and of the workspace that any call of this shape needs; 0
@@ -296,8 +296,8 @@ size_t ham_op_paged_workspace_bytes(const ham_paged_shape* shape);
  *  d_q           act rows [n_tokens][n_heads*head_dim]: the rotated q, or NULL
  * K and V are rounded to the storage type; of the pages nothing but the new slots is
  * written.  HAM_EINVAL on a bad shape, null or misaligned (16 bytes) pointer, n_tokens
- * outside 1..2^24, or n_tokens * n_kv_heads past one launch (2^26); HAM_ENOMEM if the
- * pool is too small. */
+ * outside 1..2^24, or n_tokens * n_kv_heads past 2^27; HAM_ENOMEM if the pool is too
+ * small. */
 int ham_op_paged_append(const ham_paged_shape* shape, int32_t n_tokens, const float* d_qkv, const float* d_cos,
                         const float* d_sin, const int32_t* d_offsets, const int32_t* d_start, const int32_t* d_table,
                         void* d_pool, size_t pool_bytes, void* d_q, int32_t* d_err, void* hip_stream);
@@ -322,7 +322,10 @@ int ham_op_paged_attention(const ham_paged_shape* shape, const void* d_q, const 
  * other; an infinity may make them NaN.  Numbers as in ham_op_paged_attention.
  *  d_q, d_out  act rows [n_tokens][n_heads*head_dim]
  *  kv_max      host upper bound of kv_len; with n_tokens, rows and heads it chooses
- *              the split of the work and so the order of the sums */
+ *              the split of the work and so the order of the sums
+ * n_tokens in 1..2^24, of which a launch takes up to 2^22 tiles of 16 (token, q-head)
+ * pairs: with grp = n_heads / n_kv_heads, n_kv_heads * min(n_tokens, (n_tokens * grp +
+ * 15 * rows) / 16). */
 int ham_op_paged_prompt(const ham_paged_shape* shape, int32_t n_tokens, const void* d_q, const int32_t* d_offsets,
                         const void* d_pool, size_t pool_bytes, const int32_t* d_table, const int32_t* d_kv_len,
                         int32_t kv_max, void* d_out, int32_t* d_err, void* d_workspace, size_t workspace_bytes,
@@ -344,7 +347,8 @@ int ham_op_paged_prompt(const ham_paged_shape* shape, int32_t n_tokens, const vo
  * there are none); table entries that the row no longer holds are -1, those behind them
  * are left.  8 in d_err: a parent outside -1..rows-1 or of an impossible length (the
  * row keeps its own), a count that leaves less than 0 or more than row_pages *
- * page_slots slots (it is taken as 0). */
+ * page_slots slots (it is taken as 0).
+ * n_layers in 1..1024, rows * n_layers * (page bytes / 16 KB, rounded up) below 2^31. */
 int ham_op_paged_advance(const ham_paged_shape* shape, int32_t n_layers, const int32_t* d_parent, const int32_t* d_count,
                          int32_t* d_kv_len, int32_t* d_start, int32_t* d_table, int32_t* d_refs, void* d_pool,
                          size_t pool_bytes, int32_t* d_err, void* d_workspace, size_t workspace_bytes, void* hip_stream);
@@ -354,7 +358,8 @@ int ham_op_paged_advance(const ham_paged_shape* shape, int32_t n_layers, const i
  * references and tables follow.
  *  d_map     int32 [n_pages]: the new place of each page, -1 for free ones
  *  d_n_used  int32 [1]: U
- * The pages from U on keep what they held. */
+ * The pages from U on keep what they held.
+ * n_layers in 1..1024, n_pages * n_layers * (page bytes / 16 KB, rounded up) below 2^31. */
 int ham_op_paged_compact(const ham_paged_shape* shape, int32_t n_layers, const int32_t* d_kv_len, int32_t* d_table,
                          int32_t* d_refs, void* d_pool, size_t pool_bytes, int32_t* d_map, int32_t* d_n_used,
                          int32_t* d_err, void* d_workspace, size_t workspace_bytes, void* hip_stream);

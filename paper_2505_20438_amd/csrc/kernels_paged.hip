@@ -918,7 +918,7 @@ __global__ __launch_bounds__(GIVE_THREADS) void k_paged_compact(PagedCompactArgs
 
 template <typename T, int HD>
 int append_t(const PagedAppendArgs& a, Stream s) {
-  const unsigned blocks = (unsigned)((paged_append_steps(a.N, a.z.R) + 7) / 8 * 8 * a.per_step);
+  const unsigned blocks = (unsigned)paged_append_workgroups(a.N, a.z.R, a.z.Hk * (a.q ? 2 : 1));
   launch_k((k_paged_append<T, HD>), dim3(blocks), dim3(256), 0, s, a);
   return 0;
 }

@@ -119,6 +119,11 @@ constexpr int APPEND_MANY = 2048;
 inline int paged_append_groups(int N, int R, int heads) {
   return R <= 64 ? heads : (int)std::max<long long>(1, std::min<long long>(heads, APPEND_MANY / paged_append_steps(N, R)));
 }
+// Workgroups of a launch: steps in eights, one for each XCD.  A launch has fewer than 2^24 workgroups of 256 threads; a call of up to
+// 2^27 (token, kv head) pairs stays below: up to 64 rows N / 32 + 132 steps at most, of 2 Hk heads, and with more rows a step has
+// one workgroup as soon as there are many.
+inline long long paged_append_workgroups(int N, int R, int heads) { return (paged_append_steps(N, R) + 7) / 8 * 8 * paged_append_groups(N, R, heads); }
+inline bool paged_append_fits(long long N, int Hk) { return N * Hk <= 1 << 27; }
 
 // Shares of `width` (token, q-head) pairs, at most, of N packed tokens of R rows with grp <= width q-heads a kv head: a row's
 // last share may be partly filled, and a share has a token at least.

@@ -91,7 +91,7 @@ int ham_op_paged_append(const ham_paged_shape* p, int32_t n_tokens, const float*
   if (n_tokens < 1 || n_tokens > (1 << 24)) return fail(HAM_EINVAL, "n_tokens must be in 1..2^24");
   if (!d_qkv || !d_cos || !d_sin || !d_offsets || !d_start || !d_table || !d_err) return fail(HAM_EINVAL, "null pointer");
   if (misaligned({d_qkv, d_cos, d_sin, d_q})) return fail(HAM_EINVAL, "buffers must be 16-byte aligned");
-  if ((paged_append_steps(n_tokens, p->rows) + 8) * p->n_kv_heads * 2 > (1 << 23))
+  if (!paged_append_fits(n_tokens, p->n_kv_heads))
     return fail(HAM_EINVAL, "n_tokens * n_kv_heads too large for one call");
   PagedAppendArgs a{};
   a.z = sizes_of(p);

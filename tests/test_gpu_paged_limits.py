@@ -5,7 +5,8 @@ Marked ``gpu``: needs an MI355X and ``libham.so`` built in-tree.
 import pytest
 import torch
 
-from synth.configs import F32
+from synth.configs import BF16, F32
+from tests.paged_ref import places
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -49,3 +50,24 @@ def test_attention_of_rows_with_2_31_blocks_together(ham):
         want[i] = total.double() / slots
     assert err.tolist() == [0] * R
     assert torch.all((out.cpu().double() - want).abs() <= 2.0 ** -22 * want.abs())
+
+
+def test_append_of_a_token_of_4096_rows_with_1024_kv_heads(ham):
+    """Row r's token goes to slot r % 16 of page r // 16.  Angles are 0: rotated rows are the rows themselves, rounded."""
+    R, H, hd, P = 4096, 1024, 64, 16
+    s = ham.paged_shape(BF16, R, H, H, hd, P, R // P, 1)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    qkv = torch.randn(R, 3, H, hd, generator=g, device=DEV)
+    one, r = torch.ones(R, hd // 2, device=DEV), torch.arange(R + 1, dtype=torch.int32, device=DEV)
+    pool = torch.full((R // P, H, 2, P * hd), float("nan"), dtype=torch.bfloat16, device=DEV)
+    q, err = torch.zeros(R, 2 * H * hd, dtype=torch.bfloat16, device=DEV), torch.zeros(R, dtype=torch.int32, device=DEV)
+    ham.ham_op_paged_append(s, qkv.view(R, -1), one, torch.zeros_like(one), r, r[:R] % P, (r[:R] // P).view(R, 1), pool, q, err,
+                            torch.cuda.current_stream().cuda_stream)
+    assert int(err.abs().max()) == 0
+    k_at, v_at = (t.to(DEV) for t in places(P, hd, 8))
+    kv = qkv[:, 1:].bfloat16().view(R // P, P, 2, H, hd)
+    for j, at in ((0, k_at), (1, v_at)):
+        got = pool[:, :, j][:, :, at].permute(0, 2, 1, 3)          # [page][slot][kv head][channel]
+        assert torch.equal(got, kv[:, :, j])
+    hi = qkv[:, 0].reshape(R, -1).bfloat16()
+    assert torch.equal(q, torch.cat([hi, (qkv[:, 0].reshape(R, -1) - hi.float()).bfloat16()], 1))
