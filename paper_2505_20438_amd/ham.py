@@ -7,6 +7,7 @@ It fails loudly when the compiled library is missing: there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -340,20 +341,29 @@ def _refuse(rows: int, names: str, tensors) -> None:
             raise HamError(HAM_EINVAL, f"{name} must be on the current device")
 
 
+@functools.lru_cache(None)
+def _types(dtype: int):
+    """Types of fp32, int32 and stored values."""
+    import torch
+    return torch.float32, torch.int32, torch.bfloat16 if dtype == HAM_BF16 else torch.float32
+
+
 def _fits_exactly(tensors) -> bool:
-    """_fits of tensors that hold just what the call reads and writes."""
+    """_fits of tensors that hold just what the call reads and writes: (tensor, bytes or 0 for any number, type or None for any)."""
     device = tensors[0][0].get_device()
-    for t, need, size in tensors:
-        if need and t.nbytes != need or size and t.itemsize != size or t.get_device() != device or not t.is_contiguous():
+    for t, need, kind in tensors:
+        if need and t.nbytes != need or kind and t.dtype is not kind or t.get_device() != device or not t.is_contiguous():
             return False
     return device >= 0 and device == _current_device()
 
 
 def _refuse_inexact(names: str, tensors) -> None:
-    for name, (t, need, _) in zip(names.split(), tensors):
+    for name, (t, need, kind) in zip(names.split(), tensors):
         if need and t.nbytes != need:
             raise HamError(HAM_EINVAL, f"{name} holds {t.nbytes} bytes, the call needs {need}")
-    _refuse(1, names, tensors)
+        if kind and t.dtype is not kind:
+            raise HamError(HAM_EINVAL, f"{name} holds values of {t.dtype}, the call reads {kind}")
+    _refuse(1, names, [(t, need, 0) for t, need, _ in tensors])
 
 
 def ham_op_kv8_append(shape: HamKv8Shape, qkv, cos, sin, start, count, cache, q, err, stream: int, n_tokens=None) -> None:
@@ -463,12 +473,11 @@ def ham_op_paged_append(shape: HamPagedShape, qkv, cos, sin, offsets, start, tab
     None."""
     rows, hd, H = shape.rows, shape.head_dim, shape.n_heads
     n = qkv.shape[0] if qkv.dim() else 0
-    es = 2 if shape.dtype == HAM_BF16 else 4
-    i4 = 4 * rows
-    args = ((qkv, n * (H + 2 * shape.n_kv_heads) * hd * 4, 4), (cos, n * hd * 2, 4), (sin, n * hd * 2, 4), (offsets, i4 + 4, 4),
-            (start, i4, 4), (table, i4 * shape.row_pages, 4), (pool, _pool_bytes(shape), es), (err, i4, 4))
+    i4, (f32, i32, kind) = 4 * rows, _types(shape.dtype)
+    args = ((qkv, n * (H + 2 * shape.n_kv_heads) * hd * 4, f32), (cos, n * hd * 2, f32), (sin, n * hd * 2, f32), (offsets, i4 + 4, i32),
+            (start, i4, i32), (table, i4 * shape.row_pages, i32), (pool, _pool_bytes(shape), kind), (err, i4, i32))
     if q is not None:
-        args += ((q, n * H * hd * 4, es),)
+        args += ((q, n * H * hd * 4, kind),)
     if not _fits_exactly(args):
         _refuse_inexact("qkv cos sin offsets start table pool err q", args)
     _check(load_library().ham_op_paged_append(
@@ -478,10 +487,9 @@ def ham_op_paged_append(shape: HamPagedShape, qkv, cos, sin, offsets, start, tab
 
 def ham_op_paged_attention(shape: HamPagedShape, q, pool, table, kv_len, enable, kv_max: int, out, err, workspace, stream: int) -> None:
     """Attention of one act row per sequence over its pages of a layer's pool."""
-    i4, act = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4
-    es = 2 if shape.dtype == HAM_BF16 else 4
-    args = ((q, act, es), (pool, _pool_bytes(shape), es), (table, i4 * shape.row_pages, 4), (kv_len, i4, 4), (enable, i4, 4), (out, act, es), (err, i4, 4),
-            (workspace, 0, 0))
+    i4, act, (_, i32, kind) = 4 * shape.rows, shape.rows * shape.n_heads * shape.head_dim * 4, _types(shape.dtype)
+    args = ((q, act, kind), (pool, _pool_bytes(shape), kind), (table, i4 * shape.row_pages, i32), (kv_len, i4, i32), (enable, i4, i32),
+            (out, act, kind), (err, i4, i32), (workspace, 0, None))
     if not _fits_exactly(args):
         _refuse_inexact("q pool table kv_len enable out err workspace", args)
     _check(load_library().ham_op_paged_attention(
@@ -493,10 +501,9 @@ def ham_op_paged_prompt(shape: HamPagedShape, q, offsets, pool, table, kv_len, k
     """Causal attention of packed act rows, the last offsets[r + 1] - offsets[r] of the kv_len[r] slots of each row, over their
     pages of a layer's pool."""
     i4, n = 4 * shape.rows, q.shape[0] if q.dim() else 0
-    act = n * shape.n_heads * shape.head_dim * 4
-    es = 2 if shape.dtype == HAM_BF16 else 4
-    args = ((q, act, es), (offsets, i4 + 4, 4), (pool, _pool_bytes(shape), es), (table, i4 * shape.row_pages, 4), (kv_len, i4, 4), (out, act, es),
-            (err, i4, 4), (workspace, 0, 0))
+    act, (_, i32, kind) = n * shape.n_heads * shape.head_dim * 4, _types(shape.dtype)
+    args = ((q, act, kind), (offsets, i4 + 4, i32), (pool, _pool_bytes(shape), kind), (table, i4 * shape.row_pages, i32), (kv_len, i4, i32),
+            (out, act, kind), (err, i4, i32), (workspace, 0, None))
     if not _fits_exactly(args):
         _refuse_inexact("q offsets pool table kv_len out err workspace", args)
     _check(load_library().ham_op_paged_prompt(
@@ -508,11 +515,11 @@ def ham_op_paged_advance(shape: HamPagedShape, n_layers: int, parent, count, kv_
                          stream: int) -> None:
     """Rows take over the pages of rows ``parent`` (or None: their own), then get ``count`` more slots, or fewer; in place.
     ``pool`` holds n_layers layers' pools."""
-    i4 = 4 * shape.rows
-    args = ((count, i4, 4), (kv_len, i4, 4), (start, i4, 4), (table, i4 * shape.row_pages, 4), (refs, 4 * shape.n_pages, 4),
-            (pool, _pool_bytes(shape, n_layers), 0), (err, i4, 4), (workspace, 0, 0))
+    i4, i32 = 4 * shape.rows, _types(shape.dtype)[1]
+    args = ((count, i4, i32), (kv_len, i4, i32), (start, i4, i32), (table, i4 * shape.row_pages, i32), (refs, 4 * shape.n_pages, i32),
+            (pool, _pool_bytes(shape, n_layers), None), (err, i4, i32), (workspace, 0, None))
     if parent is not None:
-        args += ((parent, i4, 4),)
+        args += ((parent, i4, i32),)
     if not _fits_exactly(args):
         _refuse_inexact("count kv_len start table refs pool err workspace parent", args)
     _check(load_library().ham_op_paged_advance(
@@ -523,9 +530,9 @@ def ham_op_paged_advance(shape: HamPagedShape, n_layers: int, parent, count, kv_
 
 def ham_op_paged_compact(shape: HamPagedShape, n_layers: int, kv_len, table, refs, pool, map, used, err, workspace, stream: int) -> None:
     """Pages in use to the front of the pool: ``map`` int32 [n_pages] their new places, ``used`` int32 [1] their number."""
-    i4 = 4 * shape.rows
-    args = ((kv_len, i4, 4), (table, i4 * shape.row_pages, 4), (refs, 4 * shape.n_pages, 4), (pool, _pool_bytes(shape, n_layers), 0),
-            (map, 4 * shape.n_pages, 4), (used, 4, 4), (err, i4, 4), (workspace, 0, 0))
+    i4, i32 = 4 * shape.rows, _types(shape.dtype)[1]
+    args = ((kv_len, i4, i32), (table, i4 * shape.row_pages, i32), (refs, 4 * shape.n_pages, i32),
+            (pool, _pool_bytes(shape, n_layers), None), (map, 4 * shape.n_pages, i32), (used, 4, i32), (err, i4, i32), (workspace, 0, None))
     if not _fits_exactly(args):
         _refuse_inexact("kv_len table refs pool map used err workspace", args)
     _check(load_library().ham_op_paged_compact(
