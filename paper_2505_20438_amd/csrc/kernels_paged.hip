@@ -593,8 +593,11 @@ __device__ __forceinline__ int block_scan(int v, int* waves, int& total) {
   total = all;
   return before + v;
 }
-// Global memory that atomics of this workgroup have changed, past the CU's cache, which may hold it as it was.  After a barrier
-// (which waits for the atomics) that is all one workgroup needs: fences for other workgroups cost 2 to 4 us each here.
+// Global memory that atomics of this workgroup have changed before a barrier.  Atomics are done in the L2, and these loads go there
+// past the CU's cache, which may hold the value as it was.  The barrier orders the two for threads of one workgroup; it does not wait
+// for the atomics.  It need not: the workgroup's waves are on one CU, whose requests for an address reach the L2 in the order in which
+// they were issued.  (Compiled for threadgroup split, where waves of a workgroup may be on two CUs, the barrier does come with a wait
+// for vector memory.)  Work of several workgroups would need fences for the whole GPU, 2 to 4 us each here.
 __device__ __forceinline__ int changed(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // The pages from p0 on, CHUNKS times 64 to a wave: chunk k is pages page_at(p0, k) of its lanes.  All loads are under way at once.
 // CHUNKS is 16 in pools of more than FEW_PAGES, where tiles follow one another, else 4, which leaves less to do for each wave (give /
