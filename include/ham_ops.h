@@ -258,7 +258,8 @@ int ham_op_kv8_attention(const ham_kv8_shape* shape, const void* d_q, const void
  * Packed rows.  New tokens of all sequences follow one another, n_tokens rows in
  * all; row r's are d_offsets[r] .. d_offsets[r + 1] - 1 (int32 [rows + 1], not
  * descending, within 0..n_tokens; a row may have none).  Rows of the arrays before
- * the first and behind the last are neither read nor written.
+ * the first and behind the last are neither read nor written.  Where offsets descend,
+ * a row of the call has 8 in d_err, and other rows that overlap may be done in part.
  *
  * Errors on the device: d_err[r] (int32 [rows], in/out, bits are only set).  8: a
  * length, count or offset that does not fit; the row is then one without slots (the

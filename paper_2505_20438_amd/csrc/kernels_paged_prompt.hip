@@ -324,6 +324,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_prompt(PagedAttnArgs a) {
     if (b == NBS - 1) landed(u + 1);
   }
   if (full > 0) block_values<HD>(values_of(full - 1, NBS - 1), vf, pp, o);
+  // At head dim 128 the forms of four waves and of two key shares have six registers too few.  None is stored or loaded in the loop
+  // above; of four waves one is loaded again in each stage below, with a wait for the stages on their way: one to five stages of a
+  // workgroup, by the group.
   const int l = lane_anew(), limit = row_of(l).limit;
   int odd = 0;
   for (int u = full; u < cnt; ++u) {

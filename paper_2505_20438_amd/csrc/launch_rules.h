@@ -150,9 +150,9 @@ inline bool paged_attn_split(int R, int H, int Hk, int hd, int kv_max, int block
   return blocks > 28 && (pairs <= few || blocks > (R > 256 ? 512 : 128));
 }
 // Shares that the slots of all rows are cut into, for each kv head: workgroups for one, or with more rows up to four, whole rounds
-// over the CUs (at 8 kv heads a round is 32; 4 x 33,300 slots, us, 24 shares 78, 32 77, 40 93, 48 85, 64 77, 72 89; 16 x 8,300
-// 32 shares 92, 64 79, 96 84; 48 x 8,300 32 257, 64 237, 96 225, 128 228).  No share is less than PAGED_LEAST_BLOCKS, two for each
-// of the four waves.
+// over the CUs (at 8 kv heads a round is 32; rows of so many slots down to 0.8 times as many, us: 4 x 33,300 24 shares 78, 32 77, 40 93,
+// 48 85, 64 77, 72 89; 16 x 8,300 32 shares 92, 64 79, 96 84; 48 x 8,300 32 257, 64 237, 96 225, 128 228).  No share is less than
+// PAGED_LEAST_BLOCKS, two for each of the four waves.
 constexpr int PAGED_LEAST_BLOCKS = 8;
 inline int paged_attn_shares(int R, int Hk) { return std::max(1, 256 * std::min(4, 1 + R * Hk / 128) / Hk); }
 // Blocks of a share, where R rows have `all` together and the longest `most`: R + shares workgroups do for all rows, and no row has
@@ -169,8 +169,9 @@ constexpr int paged_share_size(long long all, int most, int R, int shares) {
 // Packed rows, two kernels.  k_paged_attn takes (token, q-head) pairs 16 at a time, each tile's keys shared by four waves that
 // read them for themselves; k_paged_prompt (bf16) takes 256 or 128, whose keys go through LDS once.  The first fills the card with
 // few tokens, the second does with a sixteenth of the reads.  8 kv heads of 128, 4 q-heads each, us, first / second: 1 row of 64 tokens
-// 7 / 15, of 512 21 / 28, of 1,024 45 / 44, of 1,500 77 / 60; 4 x 300 21 / 22, 32 x up to 77 34 / 23; behind 8,000 slots 8 tokens
-// 16 / 26, 128 51 / 52, 256 90 / 84; behind 33,000 32 tokens 56 / 66, 64 96 / 76; 64 rows of a token behind 2,000 slots 47 / 81.
+// 7 / 15, of 512 21 / 28, of 1,024 45 / 44, of 1,500 77 / 60; 4 x 300 41 / 31, 4 of 300 down to 38 21 / 22, 32 of 77 down to 10 34 / 23;
+// behind 8,000 slots 8 tokens 16 / 26, 128 51 / 52, 256 90 / 84; behind 33,000 32 tokens 56 / 66, 64 96 / 76; 64 rows of a token behind
+// 0 to 2,000 slots 43 / 79, behind 2,000 each 93 / 108.
 inline bool paged_prompt_tiles(int N, int R, int Hk, int grp, int kv_max) {
   const long long wgs = paged_tiles(N, R, grp, 16) * Hk;
   return (long long)N * grp <= 32ll * R || (wgs <= 2048 && wgs * kv_max <= 1600 * 2048);
