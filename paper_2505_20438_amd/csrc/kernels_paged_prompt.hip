@@ -9,7 +9,7 @@
 // shares it.  The running maximum moves, and with it the outputs, only when a score exceeds it by more than 8 powers of two.
 // Masks, and values past the slots that a wave sees, are dealt with only in blocks that reach past the wave's first row.
 //
-// Bound by the matrix cores at the card's power limit: 2,048 tokens of 32 heads of 128 behind 30,720 slots 1,890 to 1,915 us, 1.4 PFLOP/s
+// Bound by the matrix cores at the card's power limit: 2,048 tokens of 32 heads of 128 behind 30,720 slots 1,890 to 1,950 us, 1.4 PFLOP/s
 // of the products that are executed (K Q^T for two planes of the queries, P V for three of the weights), as a library's 8,192^3
 // product; 7 prompts of 500 to 4,001 tokens 704 to 740 us, 1.1 to 1.2 (softmax, and planes, on the vector units are the rest).
 // Without softmax the first took 1,612 us, without products 767; two planes of the weights, 16 bits, 1,590.
